@@ -433,6 +433,17 @@ int32_t arckv_prefill_attention_noalloc(const void* k_pool, const void* v_pool, 
                                         int32_t num_kv_heads, int32_t head_dim, float scale,
                                         int64_t ws_bytes, void* stream);
 
+/* arckv_prefill_attention that also writes lse: device fp32 [n_q][num_q_heads], for every query row
+ * and head the natural logarithm of sum_j exp(scale * q . K[j]) over the keys it attends to (what
+ * arckv_attention_weights takes).  out is the same bits; EINVAL also for a NULL lse. */
+int32_t arckv_prefill_attention_lse(const void* k_pool, const void* v_pool, const void* q, void* out,
+                                    float* lse, const int32_t* block_tables, int32_t bt_stride,
+                                    const int32_t* cu_q, const int32_t* seq_lens, int32_t n_reqs,
+                                    int64_t n_q, int64_t num_blocks, const int32_t* work,
+                                    int64_t n_work, int64_t n_combine, int32_t tile_cols,
+                                    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                    float scale, void* workspace, int64_t ws_bytes, void* stream);
+
 /* ---------------------------------------------------------------------------------------
  * Device: the producer of the computed tokens' Q/K/V (the attention inputs of a prefill;
  * Sec. 4 serves Qwen3-14B, whose public configuration fixes the details): projection of the
@@ -484,6 +495,51 @@ int32_t arckv_qkv_rope_to_pool(const void* x, const void* w_qkv, int64_t n_token
                                double rope_theta, void* workspace, int64_t ws_bytes, void* q_out,
                                void* k_pool, void* v_pool, int64_t num_blocks,
                                const int32_t* slot_mapping, void* stream);
+
+/* ---------------------------------------------------------------------------------------
+ * Device: the 4-bit KV cache.  K and V of a token are kept as MXFP4 (the OCP Microscaling
+ * format): for every 32 consecutive dimensions 32 E2M1 codes (sign; magnitudes 0, 0.5, 1, 1.5,
+ * 2, 3, 4, 6) and one E8M0 byte b, the scale 2^(b-127).  17 D / 16 bytes per token and head, K and
+ * V together, against 4 D in bf16.
+ *   b - 127 = the smallest e in [-125, 125] with max|x| <= 7 * 2^e (125 if there is none);
+ *   code = the nearest of the magnitudes times 2^e, ties to the even code, at most 6 * 2^e.
+ * Every stored value is exact in bf16.  A group with an infinity or a NaN has b = 255 and reads
+ * back as NaN.
+ * Pool layout ARCKV_LAYOUT_MX4: [num_blocks][num_kv_heads][17 D bytes], one pool for K and V; the
+ * bytes of a block of a head are K codes [16][D/2] (low half of byte i: dimension 2 i), V codes
+ * [2][D/2][8] (byte j of pair i of half a: dimensions 2 i, 2 i + 1 of token 8 a + j), K scales
+ * [16][D/32], V scales [D/32][16].  Slots and block tables as for layout V1.
+ * ------------------------------------------------------------------------------------- */
+#define ARCKV_LAYOUT_MX4 2
+
+/* Bytes of a pool in layout MX4 (-1 on bad sizes). */
+int64_t arckv_mx4_pool_bytes(int64_t num_blocks, int32_t num_kv_heads, int32_t head_dim);
+
+/* pool[slot[t]] <- (k_new[t], v_new[t]) in 4 bits, t < n_tokens.  kv_pool: device, layout MX4.
+ * Rows, slots, requirements, errors and what happens to slots outside the pool or given twice (one
+ * token's K bytes and V bytes win, not always the same token's: callers give equal rows) as
+ * for arckv_kv_scatter; num_blocks at most 2^27, n_tokens at most 2^31 - 1. */
+int32_t arckv_kv_scatter_mx4(void* kv_pool, const void* k_new, const void* v_new,
+                             const int32_t* slot_mapping, int64_t n_tokens, int64_t num_blocks,
+                             int32_t num_kv_heads, int32_t head_dim, void* stream);
+
+/* The way back: (k_out[t], v_out[t]) <- pool[slot[t]] as bf16 rows [n_tokens][num_kv_heads]
+ * [head_dim] (16-byte aligned; exact).  Rows of a slot outside the pool are zero. */
+int32_t arckv_kv_gather_mx4(const void* kv_pool, void* k_out, void* v_out, const int32_t* slot_mapping,
+                            int64_t n_tokens, int64_t num_blocks, int32_t num_kv_heads,
+                            int32_t head_dim, void* stream);
+
+/* Attention over the 4-bit cache: arckv_prefill_attention with K and V the values that kv_pool
+ * (device, layout MX4) stands for.  Plans, arguments, requirements and errors as there (any bf16
+ * address for q and out, the same plan for both formats); lse (may be NULL) as for
+ * arckv_prefill_attention_lse; num_blocks at most 2^27. */
+int32_t arckv_prefill_attention_mx4(const void* kv_pool, const void* q, void* out, float* lse,
+                                    const int32_t* block_tables, int32_t bt_stride,
+                                    const int32_t* cu_q, const int32_t* seq_lens, int32_t n_reqs,
+                                    int64_t n_q, int64_t num_blocks, const int32_t* work,
+                                    int64_t n_work, int64_t n_combine, int32_t tile_cols,
+                                    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                    float scale, void* workspace, int64_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -31,12 +31,14 @@ Contents, each module citing the passage of the paper it follows:
 * ``qkv`` -- the producer of the computed tokens' Q/K/V: projection of their
   hidden states and rotary position embedding (Sec. 4 serves Qwen3-14B; the
   layer details are this project's reading of the public model configuration).
+* ``mx4`` -- the 4-bit form of cached K/V (Sec. 2: the cache's memory is what limits how
+  many prefixes it keeps): quantisation, the pool image and the way back.
 
 Parity status: every function here is pinned by ``tests/test_oracle_*.py``
 against values fixed by the mathematics or by hand-derived traces; none is
 "parity unpinned".
 """
 
-from . import blockhash, arc, lru, planner, kvpool, attention, qkv  # noqa: F401
+from . import blockhash, arc, lru, planner, kvpool, attention, qkv, mx4  # noqa: F401
 
-__all__ = ["blockhash", "arc", "lru", "planner", "kvpool", "attention", "qkv"]
+__all__ = ["blockhash", "arc", "lru", "planner", "kvpool", "attention", "qkv", "mx4"]

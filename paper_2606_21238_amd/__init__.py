@@ -370,6 +370,35 @@ def kv_scatter(k_pool, v_pool, k_new, v_new, slot_mapping, stream=None):
                                       hkv, d, C.c_void_p(_stream(stream))), "arckv_kv_scatter")
 
 
+def mx4_pool_bytes(num_blocks: int, num_kv_heads: int, head_dim: int) -> int:
+    return int(lib().arckv_mx4_pool_bytes(num_blocks, num_kv_heads, head_dim))
+
+
+def _mx4_rows(kv_pool, k, v, slot_mapping):
+    """Checked C arguments of kv_scatter_mx4 / kv_gather_mx4."""
+    n, hkv, d = (int(x) for x in k.shape)
+    if tuple(v.shape) != (n, hkv, d):
+        raise ValueError("K and V rows must be [n_tokens, num_kv_heads, head_dim]")
+    if kv_pool.dim() != 3 or tuple(kv_pool.shape[1:]) != (hkv, 17 * d):
+        raise ValueError("kv_pool must be [blocks, Hkv, 17 D] bytes")
+    if slot_mapping.numel() != n:
+        raise ValueError("slot_mapping must hold one slot per token")
+    return (_dev(kv_pool, 8, "kv_pool"), _dev(k, 16, "K rows"), _dev(v, 16, "V rows"),
+            _dev(slot_mapping, 32, "slot_mapping"), n, int(kv_pool.shape[0]), hkv, d)
+
+
+def kv_scatter_mx4(kv_pool, k_new, v_new, slot_mapping, stream=None):
+    """pool[slot[t]] <- (k_new[t], v_new[t]) in 4 bits; kv_pool uint8 [blocks, Hkv, 17 D]."""
+    _lib.check(lib().arckv_kv_scatter_mx4(*_mx4_rows(kv_pool, k_new, v_new, slot_mapping),
+                                          C.c_void_p(_stream(stream))), "arckv_kv_scatter_mx4")
+
+
+def kv_gather_mx4(kv_pool, slot_mapping, k_out, v_out, stream=None):
+    """(k_out[t], v_out[t]) [n, Hkv, D] <- the values that pool[slot[t]] stands for, bf16."""
+    _lib.check(lib().arckv_kv_gather_mx4(*_mx4_rows(kv_pool, k_out, v_out, slot_mapping),
+                                         C.c_void_p(_stream(stream))), "arckv_kv_gather_mx4")
+
+
 def qkv_rope(x, w_qkv, cu_q, seq_lens, num_q_heads: int, num_kv_heads: int, rope_theta: float,
              q_out, k_out, v_out, workspace, stream=None):
     """Projection + rotary embedding of the computed tokens (arckv_qkv_rope).  Device tensors:
@@ -464,35 +493,71 @@ def unpack_prepared(packed: np.ndarray, d: dict, prefix_lens, hit_blocks):
 def _attention_args(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work, n_work: int,
                     n_combine: int, tile_cols: int, scale: float):
     """Checked C arguments of the attention calls, up to (excluding) the workspace."""
-    n_q, hq, d = int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
+    d = int(q.shape[2])
     nb, hkv = int(k_pool.shape[0]), int(k_pool.shape[1])
+    if tuple(k_pool.shape) != (nb, hkv, 16, d) or tuple(v_pool.shape) != (nb, hkv, d, 16):
+        raise ValueError("pools must be [blocks, Hkv, 16, D] (K) and [blocks, Hkv, D, 16] (V)")
+    return (_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"),
+            *_batch_args(q, out, block_tables, cu_q, seq_lens, work, n_work, n_combine, tile_cols, scale, nb, hkv))
+
+
+def _batch_args(q, out, block_tables, cu_q, seq_lens, work, n_work, n_combine, tile_cols, scale, nb, hkv):
+    """The part of _attention_args that does not depend on the pools' format."""
+    n_q, hq, d = int(q.shape[0]), int(q.shape[1]), int(q.shape[2])
     n_reqs = int(seq_lens.shape[0])
     if tuple(out.shape) != (n_q, hq, d):
         raise ValueError("out must have the shape of q")
-    if tuple(k_pool.shape) != (nb, hkv, 16, d) or tuple(v_pool.shape) != (nb, hkv, d, 16):
-        raise ValueError("pools must be [blocks, Hkv, 16, D] (K) and [blocks, Hkv, D, 16] (V)")
     if block_tables.dim() != 2 or int(block_tables.shape[0]) != n_reqs or cu_q.numel() != n_reqs + 1:
         raise ValueError("block_tables must be [n_reqs, stride] and cu_q [n_reqs + 1]")
     if work.dim() != 2 or int(work.shape[1]) != WORK_INTS or int(work.shape[0]) < n_work + n_combine:
         raise ValueError("work must be [>= n_work + n_combine, 8]")
-    return (_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"), _dev(q, 16, "q"), _dev(out, 16, "out"),
-            _dev(block_tables, 32, "block_tables"), int(block_tables.shape[1]), _dev(cu_q, 32, "cu_q"),
-            _dev(seq_lens, 32, "seq_lens"), n_reqs, n_q, nb, _dev(work, 32, "work"), n_work, n_combine,
-            int(tile_cols), hq, hkv, d, float(scale))
+    return (_dev(q, 16, "q"), _dev(out, 16, "out"), _dev(block_tables, 32, "block_tables"),
+            int(block_tables.shape[1]), _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), n_reqs, n_q, nb,
+            _dev(work, 32, "work"), n_work, n_combine, int(tile_cols), hq, hkv, d, float(scale))
+
+
+def _workspace(workspace, ws_bytes: int):
+    if ws_bytes and (workspace is None or workspace.numel() * workspace.element_size() < ws_bytes):
+        raise ValueError("workspace smaller than ws_bytes")
+    return C.c_void_p(0) if workspace is None else _dev(workspace, None, "workspace")
+
+
+def _lse(lse, q):
+    """The device address of lse, fp32 [n_q, Hq] (None: NULL)."""
+    if lse is None:
+        return C.c_void_p(0)
+    if tuple(lse.shape) != tuple(q.shape[:2]) or not lse.is_floating_point():
+        raise ValueError("lse must be fp32 [n_q, Hq]")
+    return _dev(lse, 32, "lse")
 
 
 def prefill_attention(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work, n_work: int,
                       n_combine: int, tile_cols: int, scale: float, workspace=None, ws_bytes: int = 0,
-                      stream=None):
+                      stream=None, lse=None):
     """Device tensors: pools (layout V1), q/out [n_q, Hq, D] bf16, block_tables [n, stride] int32,
-    cu_q [n+1], seq_lens [n], work [n_work + n_combine, 8] int32, workspace (bytes >= ws_bytes)."""
+    cu_q [n+1], seq_lens [n], work [n_work + n_combine, 8] int32, workspace (bytes >= ws_bytes).
+    lse (optional): fp32 [n_q, Hq], receives log sum_j exp(scale q . K[j]) of every row and head."""
     args = _attention_args(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work, n_work, n_combine,
                            tile_cols, scale)
-    if ws_bytes and (workspace is None or workspace.numel() * workspace.element_size() < ws_bytes):
-        raise ValueError("workspace smaller than ws_bytes")
-    ws = C.c_void_p(0) if workspace is None else _dev(workspace, None, "workspace")
-    _lib.check(lib().arckv_prefill_attention(*args, ws, int(ws_bytes), C.c_void_p(_stream(stream))),
-               "arckv_prefill_attention")
+    tail = (_workspace(workspace, ws_bytes), int(ws_bytes), C.c_void_p(_stream(stream)))
+    if lse is None:
+        _lib.check(lib().arckv_prefill_attention(*args, *tail), "arckv_prefill_attention")
+    else:
+        _lib.check(lib().arckv_prefill_attention_lse(*args[:4], _lse(lse, q), *args[4:], *tail),
+                   "arckv_prefill_attention_lse")
+
+
+def prefill_attention_mx4(kv_pool, q, out, block_tables, cu_q, seq_lens, work, n_work: int, n_combine: int,
+                          tile_cols: int, scale: float, workspace=None, ws_bytes: int = 0, stream=None, lse=None):
+    """prefill_attention over the 4-bit cache: kv_pool uint8 [blocks, Hkv, 17 D] (layout MX4)."""
+    hkv, d = int(kv_pool.shape[1]), int(q.shape[2])
+    if kv_pool.dim() != 3 or int(kv_pool.shape[2]) != 17 * d:
+        raise ValueError("kv_pool must be [blocks, Hkv, 17 D] bytes")
+    args = _batch_args(q, out, block_tables, cu_q, seq_lens, work, n_work, n_combine, tile_cols, scale,
+                       int(kv_pool.shape[0]), hkv)
+    _lib.check(lib().arckv_prefill_attention_mx4(_dev(kv_pool, 8, "kv_pool"), *args[:2], _lse(lse, q), *args[2:],
+                                                 _workspace(workspace, ws_bytes), int(ws_bytes),
+                                                 C.c_void_p(_stream(stream))), "arckv_prefill_attention_mx4")
 
 
 def prefill_attention_noalloc(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work, n_work: int,

@@ -77,6 +77,13 @@ _SIGS = {
     "arckv_cache_snapshot": (i32, [vp, i32, P_u64, P_i32, i64, P_i64]),
     "arckv_pool_bytes": (i64, [i64, i32, i32]),
     "arckv_kv_scatter": (i32, [vp, vp, vp, vp, vp, i64, i64, i32, i32, vp]),
+    "arckv_prefill_attention_lse": (i32, [vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, i64, i64, vp, i64, i64,
+                                          i32, i32, i32, i32, f32, vp, i64, vp]),
+    "arckv_prefill_attention_mx4": (i32, [vp, vp, vp, vp, vp, i32, vp, vp, i32, i64, i64, vp, i64, i64,
+                                          i32, i32, i32, i32, f32, vp, i64, vp]),
+    "arckv_mx4_pool_bytes": (i64, [i64, i32, i32]),
+    "arckv_kv_scatter_mx4": (i32, [vp, vp, vp, vp, i64, i64, i32, i32, vp]),
+    "arckv_kv_gather_mx4": (i32, [vp, vp, vp, vp, i64, i64, i32, i32, vp]),
     "arckv_qkv_rope": (i32, [vp, vp, i64, i32, i32, i32, i32, vp, vp, i32, f64, vp, i64, vp, vp, vp, vp]),
     "arckv_qkv_rope_to_pool": (i32, [vp, vp, i64, i32, i32, i32, i32, vp, vp, i32, f64, vp, i64, vp, vp, vp,
                                       i64, vp, vp]),

@@ -213,3 +213,5 @@ extern "C" int32_t arckv_kv_scatter(void* k_pool, void* v_pool, const void* k_ne
   if (e != hipSuccess) return arckv::fail(ARCKV_EDEVICE, "kv_scatter: %s", hipGetErrorString(e));
   return ARCKV_OK;
 }
+
+#include "kv_mx4.hpp"

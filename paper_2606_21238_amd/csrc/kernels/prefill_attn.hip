@@ -66,6 +66,7 @@ constexpr int kStages = 4;                         // K/V tiles resident in LDS 
 constexpr int kBK = 64;        // keys per K/V tile (4 blocks of 16)
 constexpr float kLazy = 8.0f;  // rescale O only when a column max grows by > 2^8
 constexpr float kLazySum = 256.0f;  // 2^kLazy
+constexpr float kLn2 = 0.6931471805599453f;   // sums are kept to base 2 and leave as natural logarithms
 
 struct Work {
   int32_t req, kvh, col_start, kv_start, kv_end, slot, pad0, pad1;
@@ -178,7 +179,8 @@ __global__ __launch_bounds__(512, 1) void prefill_attn_list_kernel(
     const int32_t* __restrict__ block_tables, int bt_stride,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, int n_reqs,
     const Work* __restrict__ work, int64_t n_q, int64_t num_blocks, int hq, int hkv,
-    float scale_log2, float* __restrict__ ws_o, float* __restrict__ ws_lse, int64_t ws_slots) {
+    float scale_log2, float* __restrict__ ws_o, float* __restrict__ ws_lse, int64_t ws_slots,
+    float* __restrict__ lse_out) {
   constexpr int kThreads = 512;
   constexpr int kCW = 4;                         // column waves of 32 columns
   constexpr int kCols = kCW * 32;                // query columns of a narrow tile
@@ -610,7 +612,7 @@ __global__ __launch_bounds__(512, 1) void prefill_attn_list_kernel(
     // (the row sum pairs lanes l and l ^ 32, so every lane of the wave takes part)
     const float lt_sum = sum_halves(l_run);
     const float inv = lt_sum > 0.f ? 1.f / lt_sum : 0.f;
-    const float lse = lt_sum > 0.f ? m_run + __log2f(lt_sum) : -INFINITY;
+    const float lse = lt_sum > 0.f ? m_run + __log2f(lt_sum) : lt_sum == 0.f ? -INFINITY : lt_sum;   // a NaN stays
     if (kh == 0 && cval) {
       if (it.slot < 0) {
         uint16_t* dst = out + (static_cast<int64_t>(it.q0 + col / G) * hq + it.kvh * G + col % G) * D;
@@ -623,6 +625,8 @@ __global__ __launch_bounds__(512, 1) void prefill_attn_list_kernel(
             for (int j = 0; j < 4; ++j) v[j] = o[md][4 * r4 + j] * inv;
             store_out<ANY>(dst + md * 32 + 8 * r4 + 4 * hg, __builtin_convertvector(v, bf16x4_t));
           }
+        if (lse_out != nullptr && hg == 0)
+          lse_out[static_cast<int64_t>(it.q0 + col / G) * hq + it.kvh * G + col % G] = lse * kLn2;
       } else if (it.slot < ws_slots) {
         const int local = cw * 32 + l32;
         float* po = ws_o + (static_cast<int64_t>(it.slot) * kCols + local) * D;
@@ -678,7 +682,8 @@ __global__ __launch_bounds__(512, PAIRED ? 4 : 1) void prefill_attn_pp_kernel(
     const int32_t* __restrict__ block_tables, int bt_stride,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, int n_reqs,
     const Work* __restrict__ work, int64_t n_q, int64_t num_blocks, int hq, int hkv,
-    float scale_log2, float* __restrict__ ws_o, float* __restrict__ ws_lse, int64_t ws_slots) {
+    float scale_log2, float* __restrict__ ws_o, float* __restrict__ ws_lse, int64_t ws_slots,
+    float* __restrict__ lse_out) {
   constexpr int kThreads = 512;
   constexpr int kCols = arckv::kWideCols;
   static_assert(kCols == 8 * 32, "8 waves of 32 columns");
@@ -1076,13 +1081,15 @@ __global__ __launch_bounds__(512, PAIRED ? 4 : 1) void prefill_attn_pp_kernel(
   // ---- epilogue: O^T register r of block md holds dim 32 md + 8 (r / 4) + 4 hg + r % 4 ------
   const float lt = sum_halves(l_run);
   const float inv = lt > 0.f ? 1.f / lt : 0.f;
-  const float lse = lt > 0.f ? m_run + __log2f(lt) : -INFINITY;
+  const float lse = lt > 0.f ? m_run + __log2f(lt) : lt == 0.f ? -INFINITY : lt;   // a NaN stays
 #pragma unroll
   for (int md = 0; md < DM; ++md) o[md] *= inv;
   // the lane's column: PAIRED has no registers to hold it through the loops
   const int le = PAIRED ? lane_now() : lane, r32 = le & 31, he = le >> 5;
   const int ce = w.col_start + wave * 32 + r32;
   const bool ve = ce < ncols && (q0 + ce / G) < n_q;
+  if (lse_out != nullptr && w.slot < 0 && ve && he == 0)
+    lse_out[static_cast<int64_t>(q0 + ce / G) * hq + w.kvh * G + ce % G] = lse * kLn2;
   if (w.slot < 0 && ncols - w.col_start <= kCols / 2) {
     // half of the tile or less (no second group): straight from registers, 34 prompts of 21 tokens
     // 15.2 us against 15.9 through LDS; on full tiles the same stores took 4 us per item
@@ -1172,7 +1179,7 @@ template <int D>
 __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
     uint16_t* __restrict__ out, const Work* __restrict__ items, const int32_t* __restrict__ cu_q,
     int n_reqs, int64_t n_q, int hq, int G, int tile_cols, const float* __restrict__ ws_o,
-    const float* __restrict__ ws_lse, int64_t ws_slots) {
+    const float* __restrict__ ws_lse, int64_t ws_slots, float* __restrict__ lse_out) {
   __shared__ float wt[kCombineMaxSplits][kCombineCols];  // lse of a batch of pieces, then weights
   __shared__ float mx[kCombineCols], inv[kCombineCols];
   const Work w = items[blockIdx.x];  // {req, kvh, col_start, slot0, n_splits}
@@ -1260,7 +1267,13 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
       for (int k = 0; k < PER; ++k) acc[k] += wt[s][(tid + k * kCombineThreads) / D4] * v[k];
     }
   }
-  if (tid < kCombineCols) inv[tid] = wsum_part > 0.f ? 1.f / wsum_part : 0.f;
+  if (tid < kCombineCols) {
+    inv[tid] = wsum_part > 0.f ? 1.f / wsum_part : 0.f;
+    const int col = w.col_start + c0 + tid;
+    if (lse_out != nullptr && c0 + tid < tile_cols && col < ncols && q0 + col / G < n_q)
+      lse_out[static_cast<int64_t>(q0 + col / G) * hq + w.kvh * G + col % G] =
+          wsum_part > 0.f ? (mx[tid] + __log2f(wsum_part)) * kLn2 : wsum_part == 0.f ? -INFINITY : wsum_part;
+  }
   __syncthreads();
 #pragma unroll
   for (int k = 0; k < PER; ++k) {
@@ -1279,27 +1292,57 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(
 
 namespace {
 
-int32_t prefill_attention(const void* k_pool, const void* v_pool, const void* q, void* out,
+// What every attention call checks of its sizes.
+int32_t check_attention(const char* fn, int32_t n_reqs, int64_t n_q, int64_t num_blocks, int64_t n_work,
+                        int64_t n_combine, int32_t tile_cols, int32_t num_q_heads, int32_t num_kv_heads,
+                        int32_t head_dim, int32_t bt_stride, float scale, int64_t ws_bytes) {
+  if (num_q_heads < 1 || num_kv_heads < 1 || num_q_heads % num_kv_heads != 0 || n_reqs < 0 ||
+      n_q < 0 || num_blocks < 0 || n_work < 0 || n_combine < 0 || ws_bytes < 0 || bt_stride < 0 ||
+      !std::isfinite(scale) || scale <= 0.f)
+    return arckv::fail(ARCKV_EINVAL, "%s: bad sizes or scale", fn);
+  const int G = num_q_heads / num_kv_heads;
+  if (head_dim != 64 && head_dim != 128)
+    return arckv::fail(ARCKV_EUNSUPPORTED, "%s: head_dim %d not in {64,128}", fn, head_dim);
+  if (G != 1 && G != 2 && G != 4 && G != 5 && G != 8)
+    return arckv::fail(ARCKV_EUNSUPPORTED, "%s: group size %d not in {1,2,4,5,8}", fn, G);
+  if (tile_cols != arckv::kWideCols && tile_cols != arckv::kNarrowCols)
+    return arckv::fail(ARCKV_EINVAL, "%s: tile_cols %d is not a planned width", fn, tile_cols);
+  if (tile_cols == arckv::kNarrowCols && n_work % arckv::kListItems != 0)
+    return arckv::fail(ARCKV_EINVAL, "%s: a narrow plan has lists of %d items; n_work %lld", fn,
+                       arckv::kListItems, (long long)n_work);
+  if (n_work > INT32_MAX || n_combine > INT32_MAX)
+    return arckv::fail(ARCKV_EINVAL, "%s: too many work items", fn);
+  return ARCKV_OK;
+}
+
+// The merge of the tiles that a plan split.
+int32_t combine_splits(const char* fn, uint16_t* out, float* lse, const Work* items, int64_t n_combine,
+                       const int32_t* cu_q, int32_t n_reqs, int64_t n_q, int32_t hq, int G, int32_t head_dim,
+                       int32_t tile_cols, const float* ws_o, const float* ws_lse, int64_t ws_slots, hipStream_t st) {
+  if (n_combine == 0) return ARCKV_OK;
+  const dim3 grid(static_cast<unsigned>(n_combine), static_cast<unsigned>(tile_cols / kCombineCols));
+  if (head_dim == 64)
+    hipLaunchKernelGGL(attn_combine_kernel<64>, grid, dim3(kCombineThreads), 0, st, out, items,
+                       cu_q, n_reqs, n_q, hq, G, tile_cols, ws_o, ws_lse, ws_slots, lse);
+  else
+    hipLaunchKernelGGL(attn_combine_kernel<128>, grid, dim3(kCombineThreads), 0, st, out, items,
+                       cu_q, n_reqs, n_q, hq, G, tile_cols, ws_o, ws_lse, ws_slots, lse);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return arckv::fail(ARCKV_EDEVICE, "%s: combine: %s", fn, hipGetErrorString(e));
+  return ARCKV_OK;
+}
+
+int32_t prefill_attention(const void* k_pool, const void* v_pool, const void* q, void* out, float* lse,
                           const int32_t* block_tables, int32_t bt_stride, const int32_t* cu_q,
                           const int32_t* seq_lens, int32_t n_reqs, int64_t n_q, int64_t num_blocks,
                           const int32_t* work, int64_t n_work, int64_t n_combine, int32_t tile_cols,
                           int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float scale,
                           void* workspace, int64_t ws_bytes, void* stream, hipEvent_t ev_begin,
                           hipEvent_t ev_mid, hipEvent_t ev_end) {
-  if (num_q_heads < 1 || num_kv_heads < 1 || num_q_heads % num_kv_heads != 0 || n_reqs < 0 ||
-      n_q < 0 || num_blocks < 0 || n_work < 0 || n_combine < 0 || ws_bytes < 0 || bt_stride < 0 ||
-      !std::isfinite(scale) || scale <= 0.f)
-    return arckv::fail(ARCKV_EINVAL, "prefill_attention: bad sizes or scale");
+  const int32_t rc = check_attention("prefill_attention", n_reqs, n_q, num_blocks, n_work, n_combine, tile_cols,
+                                     num_q_heads, num_kv_heads, head_dim, bt_stride, scale, ws_bytes);
+  if (rc != ARCKV_OK) return rc;
   const int G = num_q_heads / num_kv_heads;
-  if (head_dim != 64 && head_dim != 128)
-    return arckv::fail(ARCKV_EUNSUPPORTED, "prefill_attention: head_dim %d not in {64,128}", head_dim);
-  if (G != 1 && G != 2 && G != 4 && G != 5 && G != 8)
-    return arckv::fail(ARCKV_EUNSUPPORTED, "prefill_attention: group size %d not in {1,2,4,5,8}", G);
-  if (tile_cols != arckv::kWideCols && tile_cols != arckv::kNarrowCols)
-    return arckv::fail(ARCKV_EINVAL, "prefill_attention: tile_cols %d is not a planned width", tile_cols);
-  if (tile_cols == arckv::kNarrowCols && n_work % arckv::kListItems != 0)
-    return arckv::fail(ARCKV_EINVAL, "prefill_attention: a narrow plan has lists of %d items; n_work %lld",
-                       arckv::kListItems, (long long)n_work);
   if (n_work == 0 && n_combine == 0) {  // nothing to run; the events still mark the stream
     for (hipEvent_t ev : {ev_begin, ev_mid, ev_end})
       if (ev != nullptr && hipEventRecord(ev, static_cast<hipStream_t>(stream)) != hipSuccess)
@@ -1309,8 +1352,6 @@ int32_t prefill_attention(const void* k_pool, const void* v_pool, const void* q,
   if (k_pool == nullptr || v_pool == nullptr || q == nullptr || out == nullptr ||
       block_tables == nullptr || cu_q == nullptr || seq_lens == nullptr || work == nullptr)
     return arckv::fail(ARCKV_EINVAL, "prefill_attention: NULL pointer");
-  if (n_work > INT32_MAX || n_combine > INT32_MAX)
-    return arckv::fail(ARCKV_EINVAL, "prefill_attention: too many work items");
   const int64_t slot_bytes = static_cast<int64_t>(tile_cols) * (head_dim + 1) * 4;
   const int64_t ws_slots = workspace != nullptr ? ws_bytes / slot_bytes : 0;
   if (n_combine > 0 && ws_slots == 0)
@@ -1339,23 +1380,23 @@ int32_t prefill_attention(const void* k_pool, const void* v_pool, const void* q,
     if (tile_cols == arckv::kWideCols && any_align)                                            \
       hipLaunchKernelGGL((prefill_attn_pp_kernel<DD, GG, false, true>), grid, dim3(512), 0, st, kp, vp, qp, op, \
                          block_tables, bt_stride, cu_q, seq_lens, n_reqs, wk, n_q, num_blocks, \
-                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots);      \
+                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots, lse);      \
     else if (tile_cols == arckv::kWideCols && DD == 64 && n_work % 2 == 1)                     \
       hipLaunchKernelGGL((prefill_attn_pp_kernel<DD, GG, DD == 64, false>), grid, dim3(512), 0, st, kp, vp, qp, op, \
                          block_tables, bt_stride, cu_q, seq_lens, n_reqs, wk, n_q, num_blocks, \
-                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots);      \
+                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots, lse);      \
     else if (tile_cols == arckv::kWideCols)                                                    \
       hipLaunchKernelGGL((prefill_attn_pp_kernel<DD, GG, false, false>), grid, dim3(512), 0, st, kp, vp, qp, op, \
                          block_tables, bt_stride, cu_q, seq_lens, n_reqs, wk, n_q, num_blocks, \
-                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots);      \
+                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots, lse);      \
     else if (any_align)                                                                        \
       hipLaunchKernelGGL((prefill_attn_list_kernel<DD, GG, true>), list_grid, dim3(512), 0, st, kp, vp, qp, \
                          op, block_tables, bt_stride, cu_q, seq_lens, n_reqs, wk, n_q, num_blocks, \
-                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots);      \
+                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots, lse);      \
     else                                                                                       \
       hipLaunchKernelGGL((prefill_attn_list_kernel<DD, GG, false>), list_grid, dim3(512), 0, st, kp, vp, qp, \
                          op, block_tables, bt_stride, cu_q, seq_lens, n_reqs, wk, n_q, num_blocks, \
-                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots);      \
+                         num_q_heads, num_kv_heads, scale_log2, ws_o, ws_lse, ws_slots, lse);      \
   } while (0)
     if (head_dim == 64) {
       switch (G) {
@@ -1380,18 +1421,10 @@ int32_t prefill_attention(const void* k_pool, const void* v_pool, const void* q,
       return arckv::fail(ARCKV_EDEVICE, "prefill_attention: %s", hipGetErrorString(e));
   }
   if (!record(ev_mid)) return arckv::fail(ARCKV_EDEVICE, "prefill_attention: event record failed");
-  if (n_combine > 0 && any_rows) {
-    const dim3 grid(static_cast<unsigned>(n_combine), static_cast<unsigned>(tile_cols / kCombineCols));
-    const Work* items = wk + n_work;
-    if (head_dim == 64)
-      hipLaunchKernelGGL(attn_combine_kernel<64>, grid, dim3(kCombineThreads), 0, st, op, items,
-                         cu_q, n_reqs, n_q, num_q_heads, G, tile_cols, ws_o, ws_lse, ws_slots);
-    else
-      hipLaunchKernelGGL(attn_combine_kernel<128>, grid, dim3(kCombineThreads), 0, st, op, items,
-                         cu_q, n_reqs, n_q, num_q_heads, G, tile_cols, ws_o, ws_lse, ws_slots);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess)
-      return arckv::fail(ARCKV_EDEVICE, "attn_combine: %s", hipGetErrorString(e));
+  if (any_rows) {
+    const int32_t cs = combine_splits("prefill_attention", op, lse, wk + n_work, n_combine, cu_q, n_reqs, n_q, num_q_heads,
+                                      G, head_dim, tile_cols, ws_o, ws_lse, ws_slots, st);
+    if (cs != ARCKV_OK) return cs;
   }
   if (!record(ev_end)) return arckv::fail(ARCKV_EDEVICE, "prefill_attention: event record failed");
   return ARCKV_OK;
@@ -1422,7 +1455,20 @@ extern "C" int32_t arckv_prefill_attention(const void* k_pool, const void* v_poo
                                            int32_t num_q_heads, int32_t num_kv_heads,
                                            int32_t head_dim, float scale, void* workspace,
                                            int64_t ws_bytes, void* stream) {
-  return prefill_attention(k_pool, v_pool, q, out, block_tables, bt_stride, cu_q, seq_lens, n_reqs,
+  return prefill_attention(k_pool, v_pool, q, out, nullptr, block_tables, bt_stride, cu_q, seq_lens, n_reqs,
+                           n_q, num_blocks, work, n_work, n_combine, tile_cols, num_q_heads,
+                           num_kv_heads, head_dim, scale, workspace, ws_bytes, stream, nullptr,
+                           nullptr, nullptr);
+}
+
+extern "C" int32_t arckv_prefill_attention_lse(
+    const void* k_pool, const void* v_pool, const void* q, void* out, float* lse, const int32_t* block_tables,
+    int32_t bt_stride, const int32_t* cu_q, const int32_t* seq_lens, int32_t n_reqs, int64_t n_q,
+    int64_t num_blocks, const int32_t* work, int64_t n_work, int64_t n_combine, int32_t tile_cols,
+    int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float scale, void* workspace,
+    int64_t ws_bytes, void* stream) {
+  if (lse == nullptr && n_work > 0) return arckv::fail(ARCKV_EINVAL, "prefill_attention_lse: NULL lse");
+  return prefill_attention(k_pool, v_pool, q, out, lse, block_tables, bt_stride, cu_q, seq_lens, n_reqs,
                            n_q, num_blocks, work, n_work, n_combine, tile_cols, num_q_heads,
                            num_kv_heads, head_dim, scale, workspace, ws_bytes, stream, nullptr,
                            nullptr, nullptr);
@@ -1434,7 +1480,7 @@ extern "C" int32_t arckv_prefill_attention_timed(
     int64_t num_blocks, const int32_t* work, int64_t n_work, int64_t n_combine, int32_t tile_cols,
     int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim, float scale, void* workspace,
     int64_t ws_bytes, void* stream, void* ev_begin, void* ev_mid, void* ev_end) {
-  return prefill_attention(k_pool, v_pool, q, out, block_tables, bt_stride, cu_q, seq_lens, n_reqs,
+  return prefill_attention(k_pool, v_pool, q, out, nullptr, block_tables, bt_stride, cu_q, seq_lens, n_reqs,
                            n_q, num_blocks, work, n_work, n_combine, tile_cols, num_q_heads,
                            num_kv_heads, head_dim, scale, workspace, ws_bytes, stream,
                            static_cast<hipEvent_t>(ev_begin), static_cast<hipEvent_t>(ev_mid),
@@ -1503,8 +1549,10 @@ extern "C" int32_t arckv_prefill_attention_noalloc(
     const int32_t rc = device_scratch(static_cast<hipStream_t>(stream), &ws);
     if (rc != ARCKV_OK) return rc;
   }
-  return prefill_attention(k_pool, v_pool, q, out, block_tables, bt_stride, cu_q, seq_lens, n_reqs,
+  return prefill_attention(k_pool, v_pool, q, out, nullptr, block_tables, bt_stride, cu_q, seq_lens, n_reqs,
                            n_q, num_blocks, work, n_work, n_combine, tile_cols, num_q_heads,
                            num_kv_heads, head_dim, scale, ws, ws_bytes, stream, nullptr, nullptr,
                            nullptr);
 }
+
+#include "attn_mx4.hpp"

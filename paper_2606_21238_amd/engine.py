@@ -39,17 +39,31 @@ class PrefillEngine:
                  num_phys: int, scratch: int, policy: str = "arc", initial_order=None,
                  ref_order: str = "tail_first", device: str = "cuda", num_cus: int | None = None,
                  pool_fill: int = -1, victim_window: int = 1, intra_batch_reuse: bool = True,
-                 frc_p: float = 0.0):
+                 frc_p: float = 0.0, kv_format: str = "bf16", private_blocks: int = 0):
+        """kv_format: "bf16" (k_pool / v_pool, layout V1) or "mx4" (kv_pool: K and V in 4 bits,
+        layout MX4).  private_blocks: blocks num_phys .. num_phys + private_blocks - 1 of the pools
+        that the block cache does not manage (a caller's own, e.g. for evicted sessions)."""
         import torch
+        if kv_format not in ("bf16", "mx4"):
+            raise ValueError(f"kv_format {kv_format!r} is not bf16 or mx4")
+        if private_blocks < 0:
+            raise ValueError("private_blocks must not be negative")
         self.hq, self.hkv, self.d = num_q_heads, num_kv_heads, head_dim
         self.scale = head_dim ** -0.5
         self.device = torch.device(device)
         self.num_phys = num_phys
+        self.num_blocks = num_phys + private_blocks
+        self.kv_format = kv_format
+        self.k_pool = self.v_pool = self.kv_pool = None
         # pools hold bf16 bit patterns; the fill (0xFFFF, a NaN pattern) marks untouched slots
-        self.k_pool = torch.full((num_phys, num_kv_heads, 16, head_dim), pool_fill, dtype=torch.int16,
-                                 device=self.device)
-        self.v_pool = torch.full((num_phys, num_kv_heads, head_dim, 16), pool_fill, dtype=torch.int16,
-                                 device=self.device)
+        if kv_format == "bf16":
+            self.k_pool = torch.full((self.num_blocks, num_kv_heads, 16, head_dim), pool_fill, dtype=torch.int16,
+                                     device=self.device)
+            self.v_pool = torch.full((self.num_blocks, num_kv_heads, head_dim, 16), pool_fill, dtype=torch.int16,
+                                     device=self.device)
+        else:                   # every byte the fill's low one: scales of 0xFF read back as NaN too
+            self.kv_pool = torch.full((self.num_blocks, num_kv_heads, 17 * head_dim), pool_fill & 0xFF,
+                                      dtype=torch.uint8, device=self.device)
         self.cache = BlockCache(policy, capacity, num_phys, scratch, initial_order, ref_order, victim_window,
                                 intra_batch_reuse, frc_p)
         if num_cus is None:
@@ -192,10 +206,27 @@ class PrefillEngine:
         if tuple(k_new.shape) != shape or tuple(v_new.shape) != shape or not (
                 k_new.is_contiguous() and v_new.is_contiguous()) or k_new.element_size() != 2:
             raise ValueError(f"k_new / v_new must be contiguous 16-bit {shape}")
-        _lib.check(lib().arckv_kv_scatter(self.k_pool.data_ptr(), self.v_pool.data_ptr(), k_new.data_ptr(),
-                                          v_new.data_ptr(), db.slot_mapping.data_ptr(), db.n_tokens,
-                                          self.num_phys, self.hkv, self.d, self._stream(stream)),
-                   "arckv_kv_scatter")
+        tail = (k_new.data_ptr(), v_new.data_ptr(), db.slot_mapping.data_ptr(), db.n_tokens, self.num_blocks,
+                self.hkv, self.d, self._stream(stream))
+        if self.kv_format == "mx4":
+            _lib.check(lib().arckv_kv_scatter_mx4(self.kv_pool.data_ptr(), *tail), "arckv_kv_scatter_mx4")
+        else:
+            _lib.check(lib().arckv_kv_scatter(self.k_pool.data_ptr(), self.v_pool.data_ptr(), *tail),
+                       "arckv_kv_scatter")
+
+    def gather(self, slots, k_out, v_out, stream=None):
+        """The K and V rows [n, Hkv, D] that a 4-bit pool holds for `slots` (device int32 [n]), as bf16."""
+        if self.kv_format != "mx4":
+            raise ValueError("gather reads a 4-bit pool (kv_format mx4)")
+        shape = (int(slots.numel()), self.hkv, self.d)
+        for a in (k_out, v_out):
+            if tuple(a.shape) != shape or not a.is_contiguous() or a.element_size() != 2:
+                raise ValueError(f"k_out / v_out must be contiguous 16-bit {shape}")
+        if slots.element_size() != 4 or not slots.is_contiguous():
+            raise ValueError("slots must be contiguous int32")
+        _lib.check(lib().arckv_kv_gather_mx4(self.kv_pool.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+                                             slots.data_ptr(), shape[0], self.num_blocks, self.hkv, self.d,
+                                             self._stream(stream)), "arckv_kv_gather_mx4")
 
     def project(self, db: DeviceBatch, x, w_qkv, q, k_new, v_new, rope_theta: float, stream=None):
         """Q/K/V of the batch's computed tokens from their hidden states x [n_tokens, H]
@@ -224,6 +255,8 @@ class PrefillEngine:
         """project() with the KV scatter fused in (arckv_qkv_rope_to_pool): Q into q, the batch's
         K and V straight into the engine's pools at the plan's slots; no scatter() follows."""
         import torch
+        if self.kv_format != "bf16":
+            raise ValueError("project_to_pool writes bf16 pools: a 4-bit pool takes project() and scatter()")
         t, h = db.n_tokens, int(x.shape[1])
         n_out = (self.hq + 2 * self.hkv) * self.d
         if tuple(x.shape) != (t, h) or tuple(w_qkv.shape) != (n_out, h) or x.element_size() != 2 or \
@@ -238,27 +271,49 @@ class PrefillEngine:
         _lib.check(lib().arckv_qkv_rope_to_pool(
             x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d, db.cu_q.data_ptr(),
             db.seq_lens.data_ptr(), db.plan.n_reqs, float(rope_theta), self._y.data_ptr(), self._y.numel(),
-            q.data_ptr(), self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.num_phys,
+            q.data_ptr(), self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.num_blocks,
             db.slot_mapping.data_ptr(), self._stream(stream)), "arckv_qkv_rope_to_pool")
 
-    def attention(self, db: DeviceBatch, q, out, stream=None, events=None):
-        """Prefill attention of the batch.  `events`: optional (begin, mid, end) torch.cuda.Event
-        triple (already recorded once, so that each has its HIP handle), recorded by the library
-        right before the attention kernel, between it and the split-KV combine, and after it."""
+    def attention(self, db: DeviceBatch, q, out, stream=None, events=None, lse=None):
+        """Attention of the batch over the engine's pools.  `events` (bf16 pools): optional (begin,
+        mid, end) torch.cuda.Event triple (already recorded once, so that each has its HIP handle),
+        recorded by the library right before the attention kernel, between it and the split-KV
+        combine, and after it.  `lse`: optional fp32 [n_tokens, Hq] that receives
+        log sum_j exp(scale q . K[j]) of every row and head (for attention_weights)."""
         shape = (db.n_tokens, self.hq, self.d)
         if tuple(q.shape) != shape or tuple(out.shape) != shape or not (
                 q.is_contiguous() and out.is_contiguous()) or q.element_size() != 2:
             raise ValueError(f"q / out must be contiguous 16-bit {shape}")
-        args = (self.k_pool.data_ptr(), self.v_pool.data_ptr(), q.data_ptr(), out.data_ptr(),
-                db.block_tables.data_ptr(), int(db.block_tables.shape[1]), db.cu_q.data_ptr(),
-                db.seq_lens.data_ptr(), db.plan.n_reqs, db.n_tokens, self.num_phys, db.work_ptr,
-                db.n_work, db.n_combine, db.tile_cols, self.hq, self.hkv, self.d, self.scale,
-                self._ws.data_ptr() if db.ws_bytes else None, db.ws_bytes, self._stream(stream))
-        if events is None:
-            _lib.check(lib().arckv_prefill_attention(*args), "arckv_prefill_attention")
-        else:
-            _lib.check(lib().arckv_prefill_attention_timed(*args, *(e.cuda_event for e in events)),
+        if lse is not None:
+            self._check_lse(db, lse)
+        args = (db.block_tables.data_ptr(), int(db.block_tables.shape[1]), db.cu_q.data_ptr(), db.seq_lens.data_ptr(),
+                db.plan.n_reqs, db.n_tokens, self.num_blocks, db.work_ptr, db.n_work, db.n_combine, db.tile_cols,
+                self.hq, self.hkv, self.d, self.scale, self._ws.data_ptr() if db.ws_bytes else None, db.ws_bytes,
+                self._stream(stream))
+        qo = (q.data_ptr(), out.data_ptr())
+        if self.kv_format == "mx4":
+            if events is not None:
+                raise ValueError("events are recorded around the bf16 kernels only")
+            _lib.check(lib().arckv_prefill_attention_mx4(self.kv_pool.data_ptr(), *qo,
+                                                         None if lse is None else lse.data_ptr(), *args),
+                       "arckv_prefill_attention_mx4")
+            return
+        pools = (self.k_pool.data_ptr(), self.v_pool.data_ptr())
+        if events is not None:
+            if lse is not None:
+                raise ValueError("the timed call writes no lse")
+            _lib.check(lib().arckv_prefill_attention_timed(*pools, *qo, *args, *(e.cuda_event for e in events)),
                        "arckv_prefill_attention_timed")
+        elif lse is not None:
+            _lib.check(lib().arckv_prefill_attention_lse(*pools, *qo, lse.data_ptr(), *args),
+                       "arckv_prefill_attention_lse")
+        else:
+            _lib.check(lib().arckv_prefill_attention(*pools, *qo, *args), "arckv_prefill_attention")
+
+    def _check_lse(self, db: DeviceBatch, lse):
+        if tuple(lse.shape) != (db.n_tokens, self.hq) or not lse.is_contiguous() or lse.element_size() != 4 \
+                or not lse.is_floating_point():
+            raise ValueError(f"lse must be contiguous fp32 {(db.n_tokens, self.hq)}")
 
     def step(self, token_lists, qkv_for_plan, stream=None, release: bool = True):
         """One batch: plan, upload, scatter, attend, release (release=False: the caller calls
