@@ -541,6 +541,63 @@ int32_t arckv_prefill_attention_mx4(const void* kv_pool, const void* q, void* ou
                                     int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
                                     float scale, void* workspace, int64_t ws_bytes, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Device: eviction inside a request by accumulated attention weight.  A long session keeps, for
+ * every KV head, the tokens that its queries attended to most, and goes on with fewer.  Four steps:
+ * attention with lse; attention_weights adds what every cached token received; evict_select
+ * chooses; kv_compact moves the chosen tokens into blocks of the caller's own (the source blocks
+ * may be shared with other requests and are only read).  The session then attends with the
+ * destination blocks as its block table and the kept number of tokens as its length: the causal
+ * rule needs only that its new tokens come last (rotated keys keep the position they were rotated
+ * for, so a producer goes on with the true positions).
+ * ------------------------------------------------------------------------------------- */
+
+/* weights[r][h][j] += (accumulate 0: =) sum over the new tokens of request r and the query heads of
+ * KV head h that see key j of exp(scale * q . K[j] - lse), j < min(L_r, 16 bt_stride, w_stride); later
+ * entries are left as they are.  k_pool: device, the K pool of layout ARCKV_LAYOUT_V1 or the pool
+ * of layout ARCKV_LAYOUT_MX4, as `layout` says (16-byte aligned).  q, lse: device, bf16 [n_q]
+ * [num_q_heads][head_dim] and fp32 [n_q][num_q_heads] (any bf16 / fp32 address; lse as the attention
+ * call wrote it).  weights: device fp32 [n_reqs][num_kv_heads][w_stride].  Tables, lengths and what
+ * out-of-range entries of a table do as for arckv_prefill_attention; no plan and no workspace.
+ * Every weight is summed in one order: the same call gives the same bits.  EINVAL on bad sizes
+ * (also n_reqs over 65535), NULL or misaligned pointers, EUNSUPPORTED as for the attention. */
+int32_t arckv_attention_weights(const void* k_pool, int32_t layout, const void* q, const float* lse,
+                                const int32_t* block_tables, int32_t bt_stride, const int32_t* cu_q,
+                                const int32_t* seq_lens, int32_t n_reqs, int64_t n_q,
+                                int64_t num_blocks, int32_t num_q_heads, int32_t num_kv_heads,
+                                int32_t head_dim, float scale, float* weights, int64_t w_stride,
+                                int32_t accumulate, void* stream);
+
+/* kept[r][h][0..keep): the positions of request r that stay for KV head h, ascending: the first
+ * n_first, the last n_recent, and of the others those of the greatest weights[r][h][.] (the lower
+ * position among equals; NaN counts as the least); all of them where L_r <= keep, then -1.
+ * weights: device fp32 [n_reqs][num_kv_heads][w_stride]; seq_lens: device [n_reqs] (a request of
+ * more than w_stride tokens is taken as its first w_stride).  kept: device int32 [n_reqs]
+ * [num_kv_heads][keep].  kept_weights (may be NULL): device fp32 [n_reqs][num_kv_heads][kw_stride],
+ * receives the kept positions' weights, then zeros, up to keep; it must not overlap weights.
+ * EINVAL unless 0 <= n_first + n_recent <= keep <= kw_stride, and on other bad sizes or NULL. */
+int32_t arckv_evict_select(const float* weights, int64_t w_stride, const int32_t* seq_lens,
+                           int32_t n_reqs, int32_t num_kv_heads, int32_t keep, int32_t n_first,
+                           int32_t n_recent, int32_t* kept, float* kept_weights, int64_t kw_stride,
+                           void* stream);
+
+/* Token i of dst_tables[r], head h <- token kept[r][h][i] of block_tables[r], K and V, an exact copy;
+ * a negative kept entry, one past the table, or one whose block is outside the pool moves nothing,
+ * and slots that nothing moves to keep what they hold.  block_tables: device [n_reqs][bt_stride];
+ * dst_tables: device [n_reqs][dst_stride], dst_stride >= ceil(keep / 16) (else EINVAL); rows of a
+ * destination block outside the pool are skipped.  A destination block must be in no source
+ * table of the call and only once in dst_tables.  Pools and other errors as for arckv_kv_scatter;
+ * n_reqs at most 65535, num_blocks at most 2^27. */
+int32_t arckv_kv_compact(void* k_pool, void* v_pool, const int32_t* block_tables, int32_t bt_stride,
+                         const int32_t* kept, int32_t keep, const int32_t* dst_tables,
+                         int32_t dst_stride, int32_t n_reqs, int64_t num_blocks,
+                         int32_t num_kv_heads, int32_t head_dim, void* stream);
+/* The same in a pool of layout MX4: codes and scales move as they are. */
+int32_t arckv_kv_compact_mx4(void* kv_pool, const int32_t* block_tables, int32_t bt_stride,
+                             const int32_t* kept, int32_t keep, const int32_t* dst_tables,
+                             int32_t dst_stride, int32_t n_reqs, int64_t num_blocks,
+                             int32_t num_kv_heads, int32_t head_dim, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

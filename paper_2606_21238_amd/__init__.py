@@ -569,3 +569,84 @@ def prefill_attention_noalloc(k_pool, v_pool, q, out, block_tables, cu_q, seq_le
                            tile_cols, scale)
     _lib.check(lib().arckv_prefill_attention_noalloc(*args, int(ws_bytes), C.c_void_p(_stream(stream))),
                "arckv_prefill_attention_noalloc")
+
+
+# ------------------------------------------------------------------------------------------
+# device: eviction by accumulated attention weight
+# ------------------------------------------------------------------------------------------
+
+def _f32(t, name: str):
+    if not t.is_floating_point():
+        raise ValueError(f"{name} must be fp32")
+    return _dev(t, 32, name)
+
+
+def attention_weights(k_pool, q, lse, weights, block_tables, cu_q, seq_lens, scale: float,
+                      accumulate: bool = True, stream=None):
+    """weights[r, h, j] += (accumulate False: =) the attention weight that key j of request r receives
+    from the batch's rows through KV head h.  k_pool: the K pool [blocks, Hkv, 16, D] of layout V1 or
+    the 4-bit pool uint8 [blocks, Hkv, 17 D]; q [n_q, Hq, D] bf16; lse fp32 [n_q, Hq] from the
+    attention call; weights fp32 [n, Hkv, stride]."""
+    n_q, hq, d = (int(x) for x in q.shape)
+    nb, hkv, n = int(k_pool.shape[0]), int(k_pool.shape[1]), int(seq_lens.shape[0])
+    if tuple(k_pool.shape) == (nb, hkv, 16, d):
+        pool, layout = _dev(k_pool, 16, "k_pool"), _lib.LAYOUT_V1
+    elif tuple(k_pool.shape) == (nb, hkv, 17 * d):
+        pool, layout = _dev(k_pool, 8, "k_pool"), _lib.LAYOUT_MX4
+    else:
+        raise ValueError("k_pool must be [blocks, Hkv, 16, D] (bf16) or [blocks, Hkv, 17 D] (4-bit)")
+    if weights.dim() != 3 or tuple(weights.shape[:2]) != (n, hkv):
+        raise ValueError("weights must be [n_reqs, Hkv, stride]")
+    if block_tables.dim() != 2 or int(block_tables.shape[0]) != n or cu_q.numel() != n + 1:
+        raise ValueError("block_tables must be [n_reqs, stride] and cu_q [n_reqs + 1]")
+    if lse is None:
+        raise ValueError("lse must be what the attention call wrote")
+    _lib.check(lib().arckv_attention_weights(
+        pool, layout, _dev(q, 16, "q"), _lse(lse, q), _dev(block_tables, 32, "block_tables"),
+        int(block_tables.shape[1]), _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), n, n_q, nb, hq, hkv, d,
+        float(scale), _f32(weights, "weights"), int(weights.shape[2]), 1 if accumulate else 0,
+        C.c_void_p(_stream(stream))), "arckv_attention_weights")
+
+
+def evict_select(weights, seq_lens, kept, n_first: int = 0, n_recent: int = 0, kept_weights=None, stream=None):
+    """kept [n, Hkv, keep] int32 <- for every request and KV head the positions that stay, ascending
+    (-1 behind them): the first n_first, the last n_recent, and the heaviest others.  weights fp32
+    [n, Hkv, stride], seq_lens int32 [n]; kept_weights (optional) fp32 [n, Hkv, >= keep]."""
+    n, hkv, stride = (int(x) for x in weights.shape)
+    if kept.dim() != 3 or tuple(kept.shape[:2]) != (n, hkv) or seq_lens.numel() != n:
+        raise ValueError("kept must be [n_reqs, Hkv, keep] and seq_lens [n_reqs]")
+    if kept_weights is not None and (kept_weights.dim() != 3 or tuple(kept_weights.shape[:2]) != (n, hkv)):
+        raise ValueError("kept_weights must be [n_reqs, Hkv, >= keep]")
+    _lib.check(lib().arckv_evict_select(
+        _f32(weights, "weights"), stride, _dev(seq_lens, 32, "seq_lens"), n, hkv, int(kept.shape[2]), int(n_first),
+        int(n_recent), _dev(kept, 32, "kept"), C.c_void_p(0) if kept_weights is None else _f32(kept_weights, "kept_weights"),
+        0 if kept_weights is None else int(kept_weights.shape[2]), C.c_void_p(_stream(stream))), "arckv_evict_select")
+
+
+def _compact_args(block_tables, kept, dst_tables, nb, hkv, d):
+    n = int(block_tables.shape[0])
+    if kept.dim() != 3 or tuple(kept.shape[:2]) != (n, hkv) or dst_tables.dim() != 2 or int(dst_tables.shape[0]) != n:
+        raise ValueError("kept must be [n_reqs, Hkv, keep], block_tables and dst_tables [n_reqs, stride]")
+    return (_dev(block_tables, 32, "block_tables"), int(block_tables.shape[1]), _dev(kept, 32, "kept"),
+            int(kept.shape[2]), _dev(dst_tables, 32, "dst_tables"), int(dst_tables.shape[1]), n, nb, hkv, d)
+
+
+def kv_compact(k_pool, v_pool, block_tables, kept, dst_tables, stream=None):
+    """Moves the kept tokens' K and V (layout V1): token i of dst_tables[r], head h <- token kept[r, h, i]
+    of block_tables[r].  No destination block may be in a source table."""
+    nb, hkv, d = int(k_pool.shape[0]), int(k_pool.shape[1]), int(k_pool.shape[3])
+    if tuple(k_pool.shape) != (nb, hkv, 16, d) or tuple(v_pool.shape) != (nb, hkv, d, 16):
+        raise ValueError("pools must be [blocks, Hkv, 16, D] (K) and [blocks, Hkv, D, 16] (V)")
+    _lib.check(lib().arckv_kv_compact(_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"),
+                                      *_compact_args(block_tables, kept, dst_tables, nb, hkv, d),
+                                      C.c_void_p(_stream(stream))), "arckv_kv_compact")
+
+
+def kv_compact_mx4(kv_pool, block_tables, kept, dst_tables, stream=None):
+    """kv_compact in a 4-bit pool uint8 [blocks, Hkv, 17 D]."""
+    nb, hkv, row = (int(x) for x in kv_pool.shape)
+    if row % 17 != 0:
+        raise ValueError("kv_pool must be [blocks, Hkv, 17 D] bytes")
+    _lib.check(lib().arckv_kv_compact_mx4(_dev(kv_pool, 8, "kv_pool"),
+                                          *_compact_args(block_tables, kept, dst_tables, nb, hkv, row // 17),
+                                          C.c_void_p(_stream(stream))), "arckv_kv_compact_mx4")

@@ -43,6 +43,7 @@
 //    fp32 partials plus a base-2 log-sum-exp that attn_combine merges.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <mutex>
 #include <type_traits>
@@ -1556,3 +1557,4 @@ extern "C" int32_t arckv_prefill_attention_noalloc(
 }
 
 #include "attn_mx4.hpp"
+#include "attn_weights.hpp"

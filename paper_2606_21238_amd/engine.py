@@ -315,6 +315,74 @@ class PrefillEngine:
                 or not lse.is_floating_point():
             raise ValueError(f"lse must be contiguous fp32 {(db.n_tokens, self.hq)}")
 
+    def attention_weights(self, db: DeviceBatch, q, lse, weights, accumulate: bool = True, stream=None):
+        """weights[r, h, j] += (accumulate False: =) the attention weight that token j of request r
+        receives from the batch's rows through KV head h; lse from attention(lse=).  weights: fp32
+        [n_reqs, Hkv, stride]; tokens past the stride are left out."""
+        shape = (db.n_tokens, self.hq, self.d)
+        if tuple(q.shape) != shape or not q.is_contiguous() or q.element_size() != 2:
+            raise ValueError(f"q must be contiguous 16-bit {shape}")
+        self._check_lse(db, lse)
+        n = db.plan.n_reqs
+        self._check_weights(n, weights)
+        mx4 = self.kv_format == "mx4"
+        _lib.check(lib().arckv_attention_weights(
+            (self.kv_pool if mx4 else self.k_pool).data_ptr(), _lib.LAYOUT_MX4 if mx4 else _lib.LAYOUT_V1, q.data_ptr(),
+            lse.data_ptr(), db.block_tables.data_ptr(), int(db.block_tables.shape[1]), db.cu_q.data_ptr(),
+            db.seq_lens.data_ptr(), n, db.n_tokens, self.num_blocks, self.hq, self.hkv, self.d, self.scale,
+            weights.data_ptr(), int(weights.shape[2]), 1 if accumulate else 0, self._stream(stream)),
+            "arckv_attention_weights")
+
+    def _check_weights(self, n: int, weights):
+        if weights.dim() != 3 or tuple(weights.shape[:2]) != (n, self.hkv) or not weights.is_contiguous() \
+                or weights.element_size() != 4 or not weights.is_floating_point():
+            raise ValueError(f"weights must be contiguous fp32 [{n}, {self.hkv}, stride]")
+
+    def evict(self, db: DeviceBatch, weights, keep: int, dst_tables, n_first: int = 0, n_recent: int = 0, stream=None):
+        """Cuts every request of the batch down to at most `keep` tokens for each KV head: the first
+        n_first, the last n_recent, and the heaviest others by `weights` (fp32 [n_reqs, Hkv, stride >= the
+        longest request]).  Their K and V move into the blocks of dst_tables (host int32 [n_reqs, >=
+        ceil(keep / 16)]: the caller's own, none of them a block of the batch, none twice; see
+        private_blocks).  Returns (kept positions int32 [n_reqs, Hkv, keep], -1 behind a shorter request's;
+        their weights, fp32).  The batch must not have been released.  Afterwards request r holds min(L_r, keep) tokens in dst_tables[r]."""
+        import torch
+        plan, n = db.plan, db.plan.n_reqs
+        self._check_weights(n, weights)
+        if n and int(weights.shape[2]) < int(plan.seq_lens.max()):
+            raise ValueError("weights must have an entry for every token of the longest request")
+        dst = np.ascontiguousarray(dst_tables, dtype=np.int32)
+        nb = -(-keep // 16)
+        if dst.ndim != 2 or dst.shape[0] != n or dst.shape[1] < nb:
+            raise ValueError(f"dst_tables must be [{n}, >= {nb}]")
+        own = dst[:, :nb].ravel()
+        if own.size:
+            lo, hi = int(own.min()), int(own.max())
+            if lo < 0 or hi >= self.num_blocks:
+                raise ValueError("dst_tables names blocks outside the pool")
+            uses = np.bincount(own, minlength=self.num_blocks + 1)
+            if uses.max() > 1:
+                raise ValueError("dst_tables names a block twice")
+            # (entries of -1 look at the spare last place)
+            if plan.block_tables.size and plan.block_tables.max() >= lo and uses[plan.block_tables].any():
+                raise ValueError("dst_tables names a block of the batch")
+        ts = self._torch_stream(stream)
+        with torch.cuda.stream(ts):
+            dev = torch.from_numpy(dst).to(self.device)
+            kept = torch.empty((n, self.hkv, keep), dtype=torch.int32, device=self.device)
+            kept_weights = torch.empty((n, self.hkv, keep), dtype=torch.float32, device=self.device)
+        raw = self._stream(stream)
+        _lib.check(lib().arckv_evict_select(weights.data_ptr(), int(weights.shape[2]), db.seq_lens.data_ptr(), n,
+                                            self.hkv, keep, n_first, n_recent, kept.data_ptr(),
+                                            kept_weights.data_ptr(), keep, raw), "arckv_evict_select")
+        args = (db.block_tables.data_ptr(), int(db.block_tables.shape[1]), kept.data_ptr(), keep, dev.data_ptr(),
+                int(dst.shape[1]), n, self.num_blocks, self.hkv, self.d, raw)
+        if self.kv_format == "mx4":
+            _lib.check(lib().arckv_kv_compact_mx4(self.kv_pool.data_ptr(), *args), "arckv_kv_compact_mx4")
+        else:
+            _lib.check(lib().arckv_kv_compact(self.k_pool.data_ptr(), self.v_pool.data_ptr(), *args),
+                       "arckv_kv_compact")
+        return kept, kept_weights
+
     def step(self, token_lists, qkv_for_plan, stream=None, release: bool = True):
         """One batch: plan, upload, scatter, attend, release (release=False: the caller calls
         release()).  qkv_for_plan(plan) returns the computed tokens' (q, k_new, v_new) device
