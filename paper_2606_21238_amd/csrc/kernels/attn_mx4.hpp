@@ -14,6 +14,7 @@
 #pragma once
 
 #include "mx4.hpp"
+#include "attn_mx4_wide.hpp"
 
 namespace {
 
@@ -221,8 +222,8 @@ __device__ __forceinline__ void mx4_chunk(Mx4State<D, NT>& st, Mx4Raw<D>& raw, i
   }
 }
 
-// COLS = 256: one item per work-group; 128: the list of kListItems items of the work-group.
-template <int D, int COLS>
+// Narrow tiles (128 columns): a work-group takes the list of kListItems items, a wave 16 columns.
+template <int D>
 __global__ __launch_bounds__(512) void mx4_attn_kernel(
     const uint8_t* __restrict__ pool, const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
     float* __restrict__ lse_out, const int32_t* __restrict__ block_tables, int bt_stride,
@@ -232,17 +233,16 @@ __global__ __launch_bounds__(512) void mx4_attn_kernel(
   using S = Mx4State<D, 1>;
   const int lane = threadIdx.x & 63, m16 = lane & 15, q4 = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  constexpr int kItems = COLS == arckv::kNarrowCols ? arckv::kListItems : 1;
+  constexpr int kItems = arckv::kListItems, COLS = arckv::kNarrowCols;
   for (int i = 0; i < kItems; ++i) {
     const Work w = work[static_cast<int64_t>(blockIdx.x) * kItems + i];
-    if (w.req < 0) return;                         // the end of a list, or an idle item
+    if (w.req < 0) return;                         // the end of the list
     const bool bad = w.req >= n_reqs || w.kvh < 0 || w.kvh >= hkv || w.col_start < 0;
     ARCKV_CHECK_WAVE(bad, ARCKV_CHECK_WORK);
     if (bad) continue;
     const int q0 = cu_q[w.req], qlen = cu_q[w.req + 1] - q0, len = seq_lens[w.req], ncols = qlen * G;
-    for (int local = wave * 16; local < COLS; local += 128) {      // a wave's columns
-    const int c0 = w.col_start + local;
-    if (c0 >= ncols) break;
+    const int local = wave * 16, c0 = w.col_start + local;
+    if (c0 >= ncols) continue;
     const int col = c0 + m16, tok = col / G;
     const bool cval = col < ncols && q0 + tok < n_q;
     const int64_t row = cval ? static_cast<int64_t>(q0 + tok) * hq + w.kvh * G + col % G : 0;
@@ -290,7 +290,6 @@ __global__ __launch_bounds__(512) void mx4_attn_kernel(
       if (w.slot >= 0) ws_lse[prow] = lse;
       else if (lse_out != nullptr) lse_out[row] = lse * kLn2;
     }
-    }
   }
 }
 
@@ -327,16 +326,24 @@ extern "C" int32_t arckv_prefill_attention_mx4(const void* kv_pool, const void* 
   auto* wk = reinterpret_cast<const Work*>(work);
   const float scale_log2 = scale * 1.4426950408889634f;
   if (n_work > 0) {
-    const bool wide = tile_cols == arckv::kWideCols;
-    const dim3 grid(static_cast<unsigned>(wide ? n_work : n_work / arckv::kListItems));
-#define ARCKV_MX4(DD, CC)                                                                                        \
-  hipLaunchKernelGGL((mx4_attn_kernel<DD, CC>), grid, dim3(512), 0, st, pool, qp, op, lse, block_tables,      \
-                     bt_stride, cu_q, seq_lens, n_reqs, wk, n_q, num_blocks, num_q_heads, num_kv_heads, G,       \
-                     scale_log2, ws_o, ws_lse, ws_slots)
-    if (head_dim == 64) {
-      if (wide) ARCKV_MX4(64, 256); else ARCKV_MX4(64, 128);
+    const bool any = (reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) % 16 != 0;
+    // head_dim 64: two work-groups share a unit where the plan asks for it (an odd number of entries);
+    // where it does not, LDS that nobody uses keeps each on a unit of its own
+    const unsigned lds = head_dim == 64 && n_work % 2 == 0 ? 32 << 10 : 0;
+    const GroupDiv gd{static_cast<uint32_t>(G), G == 1 ? 0 : static_cast<uint32_t>(((1ull << 32) + G - 1) / G)};
+#define ARCKV_MX4(KERNEL, GRID, GG, LDS)                                                                           \
+  hipLaunchKernelGGL((KERNEL), dim3(static_cast<unsigned>(GRID)), dim3(512), LDS, st, pool, qp, op, lse,        \
+                     block_tables, bt_stride, cu_q, seq_lens, n_reqs, wk, n_q, num_blocks, num_q_heads,         \
+                     num_kv_heads, GG, scale_log2, ws_o, ws_lse, ws_slots)
+    if (tile_cols == arckv::kNarrowCols) {
+      if (head_dim == 64) ARCKV_MX4(mx4_attn_kernel<64>, n_work / arckv::kListItems, G, 0);
+      else ARCKV_MX4(mx4_attn_kernel<128>, n_work / arckv::kListItems, G, 0);
+    } else if (head_dim == 64) {
+      if (any) ARCKV_MX4((mx4_attn_wide_kernel<64, true>), n_work, gd, lds);
+      else ARCKV_MX4((mx4_attn_wide_kernel<64, false>), n_work, gd, lds);
     } else {
-      if (wide) ARCKV_MX4(128, 256); else ARCKV_MX4(128, 128);
+      if (any) ARCKV_MX4((mx4_attn_wide_kernel<128, true>), n_work, gd, lds);
+      else ARCKV_MX4((mx4_attn_wide_kernel<128, false>), n_work, gd, lds);
     }
 #undef ARCKV_MX4
     const hipError_t e = hipGetLastError();
