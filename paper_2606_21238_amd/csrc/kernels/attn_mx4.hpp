@@ -28,30 +28,13 @@ struct Mx4Raw {
   uint32_t ks[2];
 };
 
-// Where a request's K and V are.
-struct Mx4Keys {
-  const uint8_t* pool;      // of the item's KV head: block 0
-  int64_t blk_stride;       // bytes per physical block
-  const cint32* bt;         // the request's block table
-  int nblk;                 // entries of it that may be used
-  uint32_t num_blocks;
-};
-
+// The raw bytes of the chunk whose two blocks are at bytes at[0], at[1] of `pool` (block 0 of the KV head).
 template <int D>
-__device__ __forceinline__ void mx4_load(const Mx4Keys& keys, int chunk, int lane, Mx4Raw<D>& raw) {
+__device__ __forceinline__ void mx4_load(const uint8_t* pool, const int64_t (&at)[2], int lane, Mx4Raw<D>& raw) {
   using L = mx4::Layout<D>;
   const int m = lane & 15, q4 = lane >> 4;
-  int64_t at[2];
-#pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int e = 2 * chunk + b;
-    const int32_t ph = e < keys.nblk ? keys.bt[e] : 0;
-    ARCKV_CHECK_WAVE(e < keys.nblk && static_cast<uint32_t>(ph) >= keys.num_blocks, ARCKV_CHECK_BLOCK);
-    // an entry out of range reads block 0
-    at[b] = static_cast<int64_t>(static_cast<uint32_t>(ph) >= keys.num_blocks ? 0 : ph) * keys.blk_stride;
-  }
-  const uint8_t* kb = keys.pool + (m >> 3 ? at[1] : at[0]);
-  const uint8_t* vb = keys.pool + (q4 >> 1 ? at[1] : at[0]);
+  const uint8_t* kb = pool + (m >> 3 ? at[1] : at[0]);
+  const uint8_t* vb = pool + (q4 >> 1 ? at[1] : at[0]);
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
     const int tt = 8 * ((m >> 2) & 1) + 4 * t + (m & 3);
@@ -68,7 +51,7 @@ __device__ __forceinline__ void mx4_load(const Mx4Keys& keys, int chunk, int lan
 // Online softmax state of a wave: NT tiles of 16 columns.
 template <int D, int NT>
 struct Mx4State {
-  static constexpr int NJ = D / 64, DT = D / 16, KS = D / 32;
+  static constexpr int NJ = D / 64, DT = D / 16, KS = D / 32, kTiles = NT;
   bf16x8_t q[NT][KS];
   f32x4_t o[NT][DT];
   float m[NT], l[NT];
@@ -117,9 +100,9 @@ __device__ __forceinline__ void mx4_mask_v(Mx4State<D, NT>& st, Mx4Raw<D>& raw, 
 }
 
 // One chunk (keys key0 .. key0 + 31): S, softmax, O.
-template <int D, int NT, bool MASKED>
+template <int D, int NT>
 __device__ __forceinline__ void mx4_chunk(Mx4State<D, NT>& st, Mx4Raw<D>& raw, int key0, int lane, int len,
-                                          float scale_log2, bool first) {
+                                          float scale_log2, bool first, bool masked) {
   using S = Mx4State<D, NT>;
   const int q4 = lane >> 4;
   f32x4_t s[NT][2];
@@ -139,7 +122,7 @@ __device__ __forceinline__ void mx4_chunk(Mx4State<D, NT>& st, Mx4Raw<D>& raw, i
   bf16x8_t p[NT];
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
-    if constexpr (MASKED) {
+    if (masked) {                                      // wave-uniform
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
@@ -188,7 +171,7 @@ __device__ __forceinline__ void mx4_chunk(Mx4State<D, NT>& st, Mx4Raw<D>& raw, i
     }
     st.l[n] += sum;
   }
-  if constexpr (MASKED) mx4_mask_v<D, NT>(st, raw, key0, lane, len);
+  if (masked) mx4_mask_v<D, NT>(st, raw, key0, lane, len);
 #pragma unroll
   for (int j = 0; j < S::NJ; ++j) {
     float vs[8];
@@ -222,74 +205,288 @@ __device__ __forceinline__ void mx4_chunk(Mx4State<D, NT>& st, Mx4Raw<D>& raw, i
   }
 }
 
-// Narrow tiles (128 columns): a work-group takes the list of kListItems items, a wave 16 columns.
+// Narrow tiles: a work-group of 8 waves takes the list of kListItems items that the plan gave it.
+//
+// Lists whose items have at most 16 columns (decode): the items' chunks, one after the other, are cut
+// into 8 equal runs, one for each wave, wherever the items end.  A wave keeps the bytes of three
+// chunks in flight, across items too, and nothing waits for another wave until all are done: a
+// wave's part of an item (at most 15 parts on a list) goes to LDS as (m, l, O), and one barrier later
+// all threads join the parts.
+// Other lists: item after item, 32 columns for a wave, 8, 4 or 2 waves to the same columns, each with
+// its run of the item's chunks, joined the same way.
+struct Mx4Item {
+  int req, kvh, col, slot, q0, ncols, P, len, kv_lo, n_chunks, first_chunk, min_pos;
+};
+
 template <int D>
-__global__ __launch_bounds__(512) void mx4_attn_kernel(
+__global__ __launch_bounds__(512) void mx4_attn_list_kernel(
     const uint8_t* __restrict__ pool, const uint16_t* __restrict__ q, uint16_t* __restrict__ out,
     float* __restrict__ lse_out, const int32_t* __restrict__ block_tables, int bt_stride,
     const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, int n_reqs,
-    const Work* __restrict__ work, int64_t n_q, int64_t num_blocks, int hq, int hkv, int G, float scale_log2,
+    const Work* __restrict__ work, int64_t n_q, int64_t num_blocks, int hq, int hkv, GroupDiv gd, float scale_log2,
     float* __restrict__ ws_o, float* __restrict__ ws_lse, int64_t ws_slots) {
-  using S = Mx4State<D, 1>;
-  const int lane = threadIdx.x & 63, m16 = lane & 15, q4 = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  constexpr int kItems = arckv::kListItems, COLS = arckv::kNarrowCols;
-  for (int i = 0; i < kItems; ++i) {
-    const Work w = work[static_cast<int64_t>(blockIdx.x) * kItems + i];
-    if (w.req < 0) return;                         // the end of the list
+  constexpr int kCols = arckv::kNarrowCols, kItems = arckv::kListItems, kWaves = 8;
+  constexpr int kPitch = D + 4;                      // floats of a row of parts: 16 columns, 16 bank groups
+  __shared__ __attribute__((aligned(16))) float part_o[256 * kPitch];
+  __shared__ float part_m[256], part_l[256];
+  __shared__ Mx4Item items[kItems];
+  const int tid = threadIdx.x, lane = tid & 63, m16 = lane & 15, q4 = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int G = static_cast<int>(gd.g);
+
+  // ---- the list: entries up to the first idle one; an entry naming nothing of the batch has no columns ------
+  {
+    const Work w = work[static_cast<int64_t>(blockIdx.x) * kItems + (lane & 7)];
+    const uint64_t idle = __builtin_amdgcn_ballot_w64(lane < kItems && w.req < 0);
+    const bool live = (idle & ((2ull << (lane & 7)) - 1)) == 0;
     const bool bad = w.req >= n_reqs || w.kvh < 0 || w.kvh >= hkv || w.col_start < 0;
-    ARCKV_CHECK_WAVE(bad, ARCKV_CHECK_WORK);
-    if (bad) continue;
-    const int q0 = cu_q[w.req], qlen = cu_q[w.req + 1] - q0, len = seq_lens[w.req], ncols = qlen * G;
-    const int local = wave * 16, c0 = w.col_start + local;
-    if (c0 >= ncols) continue;
-    const int col = c0 + m16, tok = col / G;
-    const bool cval = col < ncols && q0 + tok < n_q;
-    const int64_t row = cval ? static_cast<int64_t>(q0 + tok) * hq + w.kvh * G + col % G : 0;
-    S st;
+    ARCKV_CHECK_LANE(wave == 0 && lane < kItems && live && bad, ARCKV_CHECK_WORK);
+    const bool ok = live && !bad;
+    Mx4Item it{};
+    if (ok) {
+      it.req = w.req;
+      it.kvh = w.kvh;
+      it.col = w.col_start;
+      it.slot = w.slot;
+      it.q0 = cu_q[w.req];
+      const int S = cu_q[w.req + 1] - it.q0;
+      it.len = seq_lens[w.req];
+      it.P = it.len - S;
+      it.ncols = S * G;
+      it.kv_lo = max(w.kv_start, 0);
+      const int last = min(w.col_start + kCols, it.ncols) - 1;
+      const int kv_hi = min(w.kv_end, it.P + gd.tok(max(last, 0)) + 1);
+      it.n_chunks = last >= w.col_start && kv_hi > it.kv_lo ? (kv_hi - it.kv_lo + kMx4Chunk - 1) / kMx4Chunk : 0;
+      it.min_pos = it.P + gd.tok(it.col);
+    }
+    int upto = it.n_chunks;
+#pragma unroll
+    for (int s = 1; s < kItems; s <<= 1) {
+      const int x = __shfl_up(upto, s);
+      if ((lane & 7) >= s) upto += x;
+    }
+    it.first_chunk = upto - it.n_chunks;
+    if (tid < kItems) items[tid] = it;
+  }
+  __syncthreads();
+  const int total = items[kItems - 1].first_chunk + items[kItems - 1].n_chunks;
+  int most = 0;                                      // columns of the widest item
+#pragma unroll
+  for (int i = 0; i < kItems; ++i) most = max(most, min(items[i].ncols - items[i].col, kCols));
+  if (most <= 0) return;
+  const uint32_t nb32 = static_cast<uint32_t>(num_blocks);
+  const int64_t blk_stride = static_cast<int64_t>(hkv) * mx4::Layout<D>::kBytes;
+
+  // ---- a wave's run of chunks: its item, its place, and the two blocks of the chunk to load next ------------
+  struct Cursor {
+    int item, chunk, left, nblk;                     // chunk: of the item's key range; left: of the run
+    const cint32* bt;
+    const uint8_t* head;
+    int32_t ph[2];
+  };
+  auto open = [&](Cursor& c, int i) {                // uniform: an item of the list
+    c.item = i;
+    const int req = __builtin_amdgcn_readfirstlane(items[i].req), len = __builtin_amdgcn_readfirstlane(items[i].len);
+    c.bt = (const cint32*)(block_tables) + static_cast<int64_t>(req) * bt_stride +
+           __builtin_amdgcn_readfirstlane(items[i].kv_lo) / 16;
+    c.nblk = min((len + 15) >> 4, bt_stride) - __builtin_amdgcn_readfirstlane(items[i].kv_lo) / 16;
+    c.head = pool + static_cast<int64_t>(__builtin_amdgcn_readfirstlane(items[i].kvh)) * mx4::Layout<D>::kBytes;
+  };
+  auto blocks = [&](Cursor& c) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int e = 2 * c.chunk + b;
+      c.ph[b] = c.left > 0 && e < c.nblk ? c.bt[e] : 0;
+    }
+  };
+  auto chunks_of = [&](int i) { return __builtin_amdgcn_readfirstlane(items[i].n_chunks); };
+  auto step = [&](Cursor& c) {                       // on to the next chunk of the run
+    --c.left;
+    ++c.chunk;
+    if (c.left > 0 && c.chunk == chunks_of(c.item)) {
+      int i = c.item + 1;
+      while (chunks_of(i) == 0) ++i;                 // the run has chunks left: an item follows
+      c.chunk = 0;
+      open(c, i);
+    }
+  };
+  auto load = [&](Cursor& c, Mx4Raw<D>& raw) {       // the chunk at the cursor, then the cursor moves on
+    int64_t at[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      ARCKV_CHECK_WAVE(c.left > 0 && static_cast<uint32_t>(c.ph[b]) >= nb32, ARCKV_CHECK_BLOCK);
+      // an entry out of range reads block 0
+      at[b] = static_cast<int64_t>(static_cast<uint32_t>(c.ph[b]) >= nb32 ? 0 : c.ph[b]) * blk_stride;
+    }
+    if (c.left > 0) mx4_load<D>(c.head, at, lane, raw);
+    step(c);
+    blocks(c);
+  };
+  auto begin = [&](int from, int to, int i, int chunk) {   // `to - from` chunks from chunk `chunk` of item i
+    Cursor c{};
+    c.left = to - from;
+    c.chunk = chunk;
+    open(c, i);
+    blocks(c);
+    return c;
+  };
+  // this lane's columns of an item: queries and positions
+  auto take = [&](auto& st, int i, int col0) {
+    using S = std::remove_reference_t<decltype(st)>;
     st.reset();
-    st.pos[0] = cval ? len - qlen + tok : -1;
 #pragma unroll
-    for (int s = 0; s < S::KS; ++s) {
-      bf16x8_t x{};
-      if (cval) __builtin_memcpy(&x, q + row * D + q4 * (D / 4) + 8 * s, 16);
-      st.q[0][s] = x;
-    }
-    const int min_pos = len - qlen + c0 / G, max_pos = len - qlen + (min(c0 + 16, ncols) - 1) / G;
-    const int kv_lo = max(w.kv_start, 0), kv_hi = min(w.kv_end, max_pos + 1);
-    const Mx4Keys keys{pool + static_cast<int64_t>(w.kvh) * mx4::Layout<D>::kBytes,
-                       static_cast<int64_t>(hkv) * mx4::Layout<D>::kBytes,
-                       (const cint32*)(block_tables) + static_cast<int64_t>(w.req) * bt_stride,
-                       min((len + 15) >> 4, bt_stride), static_cast<uint32_t>(num_blocks)};
-    for (int k = kv_lo; k < kv_hi; k += kMx4Chunk) {
-      Mx4Raw<D> raw;
-      mx4_load<D>(keys, k / kMx4Chunk, lane, raw);
-      if (k + kMx4Chunk - 1 > min_pos) mx4_chunk<D, 1, true>(st, raw, k, lane, len, scale_log2, k == kv_lo);
-      else mx4_chunk<D, 1, false>(st, raw, k, lane, len, scale_log2, k == kv_lo);
-    }
-    float l = st.l[0] + __shfl_xor(st.l[0], 16);
-    l = sum_halves(l);
-    const float inv = l > 0.f ? 1.f / l : 0.f;          // a NaN sum stays NaN in O
-    const float lse = l > 0.f ? st.m[0] + __log2f(l) : l == 0.f ? -INFINITY : l;
-    if (!cval || (w.slot >= 0 && w.slot >= ws_slots)) continue;
-    const int64_t prow = w.slot < 0 ? 0 : static_cast<int64_t>(w.slot) * COLS + local + m16;
+    for (int n = 0; n < S::kTiles; ++n) {
+      const int col = items[i].col + col0 + 16 * n + m16, tok = gd.tok(col);
+      const bool cval = col < items[i].ncols && items[i].q0 + tok < n_q;
+      const int64_t row = cval ? static_cast<int64_t>(items[i].q0 + tok) * hq + items[i].kvh * G + (col - tok * G) : 0;
+      st.pos[n] = cval ? items[i].P + tok : -1;
 #pragma unroll
-    for (int j = 0; j < S::NJ; ++j) {
-      const float by = st.nan_key[j] <= st.pos[0] ? __builtin_nanf("") : inv;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        f32x4_t v;
-#pragma unroll
-        for (int t = 0; t < 4; ++t) v[t] = st.o[0][4 * j + t][r] * by;
-        const int d = 64 * j + 16 * q4 + 4 * r;
-        if (w.slot < 0) store_out<true>(out + row * D + d, __builtin_convertvector(v, bf16x4_t));
-        else *reinterpret_cast<f32x4_t*>(ws_o + prow * D + d) = v;
+      for (int s = 0; s < S::KS; ++s) {
+        bf16x8_t x{};
+        if (cval) __builtin_memcpy(&x, q + row * D + q4 * (D / 4) + 8 * s, 16);
+        st.q[n][s] = x;
       }
     }
-    if (q4 == 0) {
-      if (w.slot >= 0) ws_lse[prow] = lse;
-      else if (lse_out != nullptr) lse_out[row] = lse * kLn2;
+  };
+  // a wave's part of an item into rows row .. of the parts
+  auto leave = [&](auto& st, int row) {
+    using S = std::remove_reference_t<decltype(st)>;
+#pragma unroll
+    for (int n = 0; n < S::kTiles; ++n) {
+      const int r0 = row + 16 * n + m16;
+      const float l = sum_halves(st.l[n] + __shfl_xor(st.l[n], 16));
+#pragma unroll
+      for (int j = 0; j < S::NJ; ++j)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          f32x4_t v;
+#pragma unroll
+          for (int t = 0; t < 4; ++t) v[t] = st.nan_key[j] <= st.pos[n] ? __builtin_nanf("") : st.o[n][4 * j + t][r];
+          *reinterpret_cast<f32x4_t*>(part_o + r0 * kPitch + 64 * j + 16 * q4 + 4 * r) = v;
+        }
+      if (q4 == 0) {
+        part_m[r0] = st.m[n];
+        part_l[r0] = l;
+      }
     }
+  };
+  // joins the parts of column c of item i, four dimensions a thread: parts k in [k0, k1) are at rows
+  // row + step * k, and is(k) says which of them there are
+  auto join = [&](int i, int c, int d, int row, int step_rows, int k0, int k1, auto is) {
+    const Mx4Item& it = items[i];
+    const int col = it.col + c, tok = gd.tok(col);
+    if (col >= it.ncols || it.q0 + tok >= n_q) return;
+    float m = -INFINITY;
+    for (int k = k0; k < k1; ++k)
+      if (is(k)) m = fmaxf(m, part_m[row + step_rows * k]);
+    f32x4_t o{};
+    float l = 0.f;
+    for (int k = k0; k < k1; ++k) {
+      if (!is(k)) continue;
+      const int r = row + step_rows * k;
+      const float a = part_m[r] == -INFINITY ? 0.f : fast_exp2(part_m[r] - m);
+      // (a part without a visible key has l = 0 and O = 0, a NaN one stays)
+      l += a * part_l[r];
+      o += a * *reinterpret_cast<const f32x4_t*>(part_o + r * kPitch + d);
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    const float lse = l > 0.f ? m + __log2f(l) : l == 0.f ? -INFINITY : l;
+    o *= inv;
+    const int64_t orow = static_cast<int64_t>(it.q0 + tok) * hq + it.kvh * G + (col - tok * G);
+    if (it.slot < 0) {
+      store_out<true>(out + orow * D + d, __builtin_convertvector(o, bf16x4_t));
+      if (d == 0 && lse_out != nullptr) lse_out[orow] = lse * kLn2;
+    } else if (it.slot < ws_slots) {
+      const int64_t prow = static_cast<int64_t>(it.slot) * kCols + c;
+      *reinterpret_cast<f32x4_t*>(ws_o + prow * D + d) = o;
+      if (d == 0) ws_lse[prow] = lse;
+    }
+  };
+
+  if (most <= 16) {
+    // ---- decode: 8 equal runs over the whole list --------------------------------------------------------------
+    const int from = total * wave / kWaves, to = total * (wave + 1) / kWaves;
+    if (to > from) {
+      int i = 0;
+      while (items[i].first_chunk + items[i].n_chunks <= from) ++i;
+      i = __builtin_amdgcn_readfirstlane(i);
+      const int chunk0 = from - __builtin_amdgcn_readfirstlane(items[i].first_chunk);
+      Cursor ld = begin(from, to, i, chunk0);
+      Mx4Raw<D> raw[3];
+      load(ld, raw[0]);
+      load(ld, raw[1]);
+      load(ld, raw[2]);
+      Mx4State<D, 1> st;
+      take(st, i, 0);
+      int chunk = chunk0, n = chunks_of(i), left = to - from;
+      bool fresh = true;
+      int kv_lo = __builtin_amdgcn_readfirstlane(items[i].kv_lo), min_pos = __builtin_amdgcn_readfirstlane(items[i].min_pos);
+      auto one = [&](Mx4Raw<D>& x) {
+        const int key0 = kv_lo + chunk * kMx4Chunk;
+        mx4_chunk<D, 1>(st, x, key0, lane, items[i].len, scale_log2, fresh, key0 + kMx4Chunk - 1 > min_pos);
+        fresh = false;
+        load(ld, x);
+        ++chunk;
+        if (--left == 0) {
+          leave(st, (wave + i) * 16);
+          return false;
+        }
+        if (chunk == n) {                            // the item ends inside the run
+          leave(st, (wave + i) * 16);
+          do ++i; while (chunks_of(i) == 0);
+          take(st, i, 0);
+          chunk = 0;
+          n = chunks_of(i);
+          kv_lo = __builtin_amdgcn_readfirstlane(items[i].kv_lo);
+          min_pos = __builtin_amdgcn_readfirstlane(items[i].min_pos);
+          fresh = true;
+        }
+        return true;
+      };
+      while (one(raw[0]) && one(raw[1]) && one(raw[2])) {}
+    }
+    __syncthreads();
+    for (int e = tid; e < kItems * 16 * (D / 4); e += 512) {
+      const int i = e / (16 * (D / 4)), c = e / (D / 4) % 16, d = 4 * (e % (D / 4));
+      const int a = items[i].first_chunk, b = a + items[i].n_chunks;
+      join(i, c, d, i * 16 + c, 16, 0, kWaves, [&](int w) {
+        return max(total * w / kWaves, a) < min(total * (w + 1) / kWaves, b);
+      });
+    }
+    return;
+  }
+  // ---- item after item: CW x 32 columns, 8 / CW runs of the item's chunks -----------------------------------------
+  for (int i = 0; i < kItems; ++i) {
+    const int cols = __builtin_amdgcn_readfirstlane(min(items[i].ncols - items[i].col, kCols)), n = chunks_of(i);
+    if (cols <= 0) continue;
+    const int CW = cols <= 32 ? 1 : cols <= 64 ? 2 : 4, KG = kWaves / CW;
+    const int cw = wave % CW, kg = wave / CW;
+    const int from = n * kg / KG, to = n * (kg + 1) / KG;
+    Mx4State<D, 2> st;
+    Cursor ld = begin(from, to, i, from);
+    Mx4Raw<D> raw[2];
+    load(ld, raw[0]);
+    load(ld, raw[1]);
+    take(st, i, 32 * cw);
+    const int kv_lo = __builtin_amdgcn_readfirstlane(items[i].kv_lo), min_pos = __builtin_amdgcn_readfirstlane(items[i].min_pos);
+    auto one = [&](int chunk, Mx4Raw<D>& x) {
+      const int key0 = kv_lo + chunk * kMx4Chunk;
+      mx4_chunk<D, 2>(st, x, key0, lane, items[i].len, scale_log2, chunk == from, key0 + kMx4Chunk - 1 > min_pos);
+      load(ld, x);
+    };
+    int k = from;
+    for (; k + 1 < to; k += 2) {
+      one(k, raw[0]);
+      one(k + 1, raw[1]);
+    }
+    if (k < to) one(k, raw[0]);
+    leave(st, wave * 32);                            // rows (kg CW + cw) 32 ..: CW 32 rows for each run
+    __syncthreads();
+    for (int e = tid; e < cols * (D / 4); e += 512) {
+      const int c = e / (D / 4);
+      join(i, c, 4 * (e % (D / 4)), c, CW * 32, 0, KG, [&](int) { return true; });
+    }
+    __syncthreads();
   }
 }
 
@@ -336,8 +533,8 @@ extern "C" int32_t arckv_prefill_attention_mx4(const void* kv_pool, const void* 
                      block_tables, bt_stride, cu_q, seq_lens, n_reqs, wk, n_q, num_blocks, num_q_heads,         \
                      num_kv_heads, GG, scale_log2, ws_o, ws_lse, ws_slots)
     if (tile_cols == arckv::kNarrowCols) {
-      if (head_dim == 64) ARCKV_MX4(mx4_attn_kernel<64>, n_work / arckv::kListItems, G, 0);
-      else ARCKV_MX4(mx4_attn_kernel<128>, n_work / arckv::kListItems, G, 0);
+      if (head_dim == 64) ARCKV_MX4(mx4_attn_list_kernel<64>, n_work / arckv::kListItems, gd, 0);
+      else ARCKV_MX4(mx4_attn_list_kernel<128>, n_work / arckv::kListItems, gd, 0);
     } else if (head_dim == 64) {
       if (any) ARCKV_MX4((mx4_attn_wide_kernel<64, true>), n_work, gd, lds);
       else ARCKV_MX4((mx4_attn_wide_kernel<64, false>), n_work, gd, lds);
