@@ -15,82 +15,147 @@
 namespace {
 
 constexpr int kWtCols = 128;    // columns in LDS at a time: 4 tiles of 32
+constexpr float kLog2e = 1.4426950408889634f;
 
+// What a work-group needs of its request.
+struct WtReq {
+  int q0, P, ncols, bound;      // first row, cached tokens, columns, keys that get a weight
+  const int32_t* bt;
+};
+__device__ __forceinline__ WtReq wt_request(int r, const int32_t* block_tables, int bt_stride, const int32_t* cu_q,
+                                            const int32_t* seq_lens, int64_t n_q, int G, int64_t w_stride) {
+  WtReq x;
+  x.q0 = cu_q[r];
+  const int qlen = cu_q[r + 1] - x.q0, len = seq_lens[r];
+  x.P = len - qlen;
+  x.ncols = static_cast<int>(min(static_cast<int64_t>(qlen), max(n_q - x.q0, static_cast<int64_t>(0)))) * G;
+  x.bound = static_cast<int>(min(static_cast<int64_t>(min(len, bt_stride * 16)), w_stride));
+  x.bt = block_tables + static_cast<int64_t>(r) * bt_stride;
+  return x;
+}
+
+// One key's bytes as a lane holds them: lane l32 of a subtile of 32 keys has its key's dimensions of k-steps
+// 0 .. KS - 1 of its half hg: 16 i + 8 hg .. (bf16 rows), hg D / 2 + 8 i .. (codes: one piece of a row).
+template <int D, bool MX4>
+struct WtKey {
+  static constexpr int KS = D / 16;
+  uint32_t c[MX4 ? D / 16 : D / 4];
+  uint32_t sc[MX4 ? D / 64 : 1];
+
+  __device__ __forceinline__ void load(const uint8_t* pool, int32_t ph, int64_t num_blocks, int hkv, int kvh, int key,
+                                       int hg) {
+    const bool bad = ph < 0 || ph >= num_blocks;
+    ARCKV_CHECK_LANE(bad && (key & 15) == 0 && hg == 0, ARCKV_CHECK_BLOCK);
+    const int64_t blk = static_cast<int64_t>(bad ? 0 : ph) * hkv + kvh;      // an entry out of range reads block 0
+    if constexpr (MX4) {
+      using L = mx4::Layout<D>;
+      const uint8_t* b = pool + blk * L::kBytes;
+      __builtin_memcpy(c, __builtin_assume_aligned(b + (key & 15) * L::kRow + hg * (D / 4), 16), D / 4);
+#pragma unroll
+      for (int g = 0; g < D / 64; ++g) sc[g] = b[L::kKScale + (key & 15) * L::kGroups + hg * (D / 64) + g];
+    } else {
+      const uint8_t* b = pool + (blk * 16 + (key & 15)) * (2 * D) + 16 * hg;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) __builtin_memcpy(c + 4 * i, __builtin_assume_aligned(b + 32 * i, 16), 16);
+    }
+  }
+  __device__ __forceinline__ bf16x8_t step(int i) const {
+    if constexpr (MX4) {
+      const float s = mx4::scale_value(sc[i / 4]);
+      return __builtin_bit_cast(bf16x8_t, u32x4_t{mx4::decode2<0>(c[i], s), mx4::decode2<1>(c[i], s),
+                                                  mx4::decode2<2>(c[i], s), mx4::decode2<3>(c[i], s)});
+    } else {
+      return __builtin_bit_cast(bf16x8_t, u32x4_t{c[4 * i], c[4 * i + 1], c[4 * i + 2], c[4 * i + 3]});
+    }
+  }
+};
+// the 16-byte chunk of a row of q that goes with k-step i
+template <int D, bool MX4>
+__device__ __forceinline__ int wt_chunk(int i, int hg) { return MX4 ? hg * (D / 16) + i : 2 * i + hg; }
+
+// The weights of 32 columns for this lane's key, of S's 16 registers: register 4 g + j is column cb + 8 g + 4 hg + j.
+template <class Lse>
+__device__ __forceinline__ float wt_sum(const f32x16_t& s, float scale_log2, int cb, int hg, bool masked, int cmin,
+                                        int ncols, Lse lse) {
+  float sum[4];
+#pragma unroll
+  for (int g = 0; g < 4; ++g) {
+    const f32x4_t l4 = lse(g);
+    float p[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) p[j] = fast_exp2(fmaf(s[4 * g + j], scale_log2, -l4[j]));
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int c = cb + 8 * g + 4 * hg + j;
+        p[j] = c >= cmin && c < ncols ? p[j] : 0.f;
+      }
+    }
+    sum[g] = (p[0] + p[1]) + (p[2] + p[3]);
+  }
+  return (sum[0] + sum[1]) + (sum[2] + sum[3]);
+}
+
+// the first column that sees a key
+__device__ __forceinline__ int first_column(int64_t key, int P, int G) {
+  return static_cast<int>(min(max(key - P, static_cast<int64_t>(0)) * G, static_cast<int64_t>(INT32_MAX)));
+}
+
+// Many columns: keys stay, columns stream.  A work-group takes KW x 32 keys at a time, n_split work-groups
+// of a (request, KV head) in turn.
 template <int D, bool MX4, int KW>
-__global__ __launch_bounds__(512, 2) void attn_weights_kernel(
+__global__ __launch_bounds__(512, 4) void attn_weights_kernel(
     const uint8_t* __restrict__ pool, const uint16_t* __restrict__ q, const float* __restrict__ lse,
     const int32_t* __restrict__ block_tables, int bt_stride, const int32_t* __restrict__ cu_q,
-    const int32_t* __restrict__ seq_lens, int64_t n_q, int64_t num_blocks, int hq, int hkv, int G, float scale_log2,
-    float* __restrict__ weights, int64_t w_stride, int accumulate) {
+    const int32_t* __restrict__ seq_lens, int64_t n_q, int64_t num_blocks, int hq, int hkv, GroupDiv gd, float scale_log2,
+    float* __restrict__ weights, int64_t w_stride, int accumulate, int n_split) {
   constexpr int kThreads = 512, CS = 8 / KW, KS = D / 16, TILES = kWtCols / 32;
   constexpr int kRowBytes = D * 2, kChunkBytes = kWtCols * kRowBytes;
   constexpr int NLD = kChunkBytes / (kThreads * 16);      // 16-byte loads of a thread for a chunk
   constexpr int kRowThreads = kRowBytes / 16, kRowsPer = kThreads / kRowThreads;
   __shared__ __attribute__((aligned(1024))) char qs[2][kChunkBytes];
   __shared__ __attribute__((aligned(16))) float ls[2][kWtCols];
-  __shared__ float part[CS > 1 ? (CS - 1) * KW * 64 : 1];
+  __shared__ float part[CS > 1 ? (CS - 1) * KW * 32 : 1];
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave % KW, cs = wave / KW;
-  const int kvh = blockIdx.x % hkv, r = blockIdx.y;
-  const int q0 = cu_q[r], qlen = cu_q[r + 1] - q0, len = seq_lens[r], P = len - qlen;
-  const int64_t bound = min(static_cast<int64_t>(min(len, bt_stride * 16)), w_stride);
-  const int64_t wg_key = static_cast<int64_t>(blockIdx.x / hkv) * (KW * 64);
-  if (wg_key >= bound) return;
-  const int key0 = static_cast<int>(wg_key) + kw * 64;
-  const int ncols = min(static_cast<int64_t>(qlen), max(n_q - q0, static_cast<int64_t>(0))) * G;
-  // columns from the first that sees the work-group's first key
-  const int first = static_cast<int>(min(static_cast<int64_t>(max(0, static_cast<int>(wg_key) - P)) * G, static_cast<int64_t>(ncols)));
-  const int c_lo = first / kWtCols * kWtCols;
+  const int kvh = blockIdx.x % hkv, r = blockIdx.y, G = static_cast<int>(gd.g);
+  const WtReq rq = wt_request(r, block_tables, bt_stride, cu_q, seq_lens, n_q, G, w_stride);
+  float* const wrow = weights + (static_cast<int64_t>(r) * hkv + kvh) * w_stride;
 
-  // ---- the wave's keys: lane l32 of subtile s is key key0 + 32 s + l32 ---------------------------
-  bf16x8_t kf[2][KS];
-  const int32_t* bt = block_tables + static_cast<int64_t>(r) * bt_stride;
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int key = key0 + 32 * s + l32;
-    const int e = min(key, max(static_cast<int>(bound) - 1, 0)) >> 4;
-    int32_t ph = bt[e];
-    const bool bad = ph < 0 || ph >= num_blocks;
-    ARCKV_CHECK_LANE(key < bound && bad && (key & 15) == 0 && hg == 0, ARCKV_CHECK_BLOCK);
-    ph = bad ? 0 : ph;               // an entry out of range reads block 0
-    const int64_t blk = static_cast<int64_t>(ph) * hkv + kvh;
-    if constexpr (MX4) {
-      using L = mx4::Layout<D>;
-      const uint8_t* b = pool + blk * L::kBytes;
-      uint32_t c[D / 16];
-      __builtin_memcpy(c, __builtin_assume_aligned(b + (key & 15) * L::kRow + hg * (D / 4), 16), D / 4);
-#pragma unroll
-      for (int g = 0; g < D / 64; ++g) {
-        const float sc = mx4::scale_value(b[L::kKScale + (key & 15) * L::kGroups + hg * (D / 64) + g]);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const uint32_t w = c[4 * g + i];
-          kf[s][4 * g + i] = __builtin_bit_cast(bf16x8_t, u32x4_t{mx4::decode2<0>(w, sc), mx4::decode2<1>(w, sc),
-                                                                  mx4::decode2<2>(w, sc), mx4::decode2<3>(w, sc)});
-        }
-      }
-    } else {
-      const uint8_t* b = pool + (blk * 16 + (key & 15)) * kRowBytes;
-#pragma unroll
-      for (int i = 0; i < KS; ++i) kf[s][i] = *reinterpret_cast<const bf16x8_t*>(b + 32 * i + 16 * hg);
-    }
-  }
-
-  // ---- columns: rows of q and their sums, a chunk ahead in registers ---------------------------------
+  // columns: rows of q and their sums, a chunk ahead in registers
   u32x4_t qn[NLD];
   float ln = 0.f;
+  // (four columns from a multiple of four are rows behind each other where G is a multiple of four: their
+  // address is the wave's, not the lane's)
+  const bool by_four = G % 4 == 0;
   auto fetch = [&](int c0) {
+    if (by_four && c0 + kWtCols <= rq.ncols) {
+#pragma unroll
+      for (int i = 0; i < NLD; ++i) {
+        constexpr int kWaveRows = 64 / kRowThreads;       // 4 (D = 128) or 8 rows of a wave and load
+        const int c = c0 + i * kRowsPer + wave * kWaveRows;
+        const int t0 = gd.tok(c);
+        const uint16_t* b0 = q + (static_cast<int64_t>(rq.q0 + t0) * hq + kvh * G + (c - t0 * G)) * D;
+        uint32_t ofs = lane * 8;
+        if (kWaveRows == 8 && G == 4) ofs += lane >= 32 ? (hq - 4) * D : 0;      // the second four are the next token's
+        __builtin_memcpy(&qn[i], b0 + ofs, 16);
+      }
+      if (tid < kWtCols) {
+        const int c = c0 + tid, tok = gd.tok(c);
+        ln = lse[static_cast<int64_t>(rq.q0 + tok) * hq + kvh * G + (c - tok * G)] * kLog2e;
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < NLD; ++i) {
-      const int c = c0 + i * kRowsPer + tid / kRowThreads;
-      const int tok = c / G;
-      const int64_t row = static_cast<int64_t>(q0 + tok) * hq + kvh * G + (c - tok * G);
+      const int c = c0 + i * kRowsPer + tid / kRowThreads, tok = gd.tok(c);
+      const int64_t row = static_cast<int64_t>(rq.q0 + tok) * hq + kvh * G + (c - tok * G);
       qn[i] = u32x4_t{};
-      if (c < ncols) __builtin_memcpy(&qn[i], q + row * D + (tid % kRowThreads) * 8, 16);
+      if (c < rq.ncols) __builtin_memcpy(&qn[i], q + row * D + (tid % kRowThreads) * 8, 16);
     }
     if (tid < kWtCols) {
-      const int c = c0 + tid, tok = c / G;
-      ln = c < ncols ? lse[static_cast<int64_t>(q0 + tok) * hq + kvh * G + (c - tok * G)] * 1.4426950408889634f : 0.f;
+      const int c = c0 + tid, tok = gd.tok(c);
+      ln = c < rq.ncols ? lse[static_cast<int64_t>(rq.q0 + tok) * hq + kvh * G + (c - tok * G)] * kLog2e : 0.f;
     }
   };
   auto put = [&](int buf) {
@@ -101,77 +166,120 @@ __global__ __launch_bounds__(512, 2) void attn_weights_kernel(
     }
     if (tid < kWtCols) ls[buf][tid] = ln;
   };
-  float acc[2] = {0.f, 0.f};
-  int cmin[2];           // the first column that sees this lane's key
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    const int64_t c = static_cast<int64_t>(max(0, key0 + 32 * s + l32 - P)) * G;
-    cmin[s] = static_cast<int>(min(c, static_cast<int64_t>(INT32_MAX)));
-  }
-  const int64_t all_see = static_cast<int64_t>(max(0, key0 + 63 - P)) * G;   // columns from here on see every key of the wave
 
-  if (c_lo < ncols) {
-    fetch(c_lo);
-    put(0);
-  }
-  __syncthreads();
-  int buf = 0;
-  for (int c0 = c_lo; c0 < ncols; c0 += kWtCols, buf ^= 1) {
-    const bool more = c0 + kWtCols < ncols;
-    if (more) fetch(c0 + kWtCols);
-    for (int t = cs; t < TILES; t += CS) {
-      const int cb = c0 + 32 * t;
-      if (cb >= ncols) break;
-      const char* qb = qs[buf] + 32 * t * kRowBytes;
-      f32x16_t s[2];
+  for (int64_t wg_key = static_cast<int64_t>(blockIdx.x / hkv) * (KW * 32); wg_key < rq.bound;
+       wg_key += static_cast<int64_t>(n_split) * (KW * 32)) {
+    const int key = static_cast<int>(wg_key) + kw * 32 + l32;
+    bf16x8_t kf[KS];
+    {
+      WtKey<D, MX4> raw;
+      raw.load(pool, rq.bt[min(key, rq.bound - 1) >> 4], num_blocks, hkv, kvh, key, hg);
 #pragma unroll
-      for (int i = 0; i < KS; ++i) {
-        const int ch = MX4 ? hg * KS + i : 2 * i + hg;
-        const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(qb + l32 * kRowBytes + ((ch ^ fk<D>(l32)) * 16));
-#pragma unroll
-        for (int x = 0; x < 2; ++x)
-          s[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, kf[x][i], i == 0 ? f32x16_t{} : s[x], 0, 0, 0);
-      }
-      const bool masked = cb < all_see || cb + 32 > ncols;
-      float sum[2][4];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const f32x4_t l4 = *reinterpret_cast<const f32x4_t*>(&ls[buf][32 * t + 8 * g + 4 * hg]);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          float p[4];
-#pragma unroll
-          for (int j = 0; j < 4; ++j) p[j] = fast_exp2(fmaf(s[x][4 * g + j], scale_log2, -l4[j]));
-          if (masked) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const int c = cb + 8 * g + 4 * hg + j;
-              p[j] = c >= cmin[x] && c < ncols ? p[j] : 0.f;
-            }
-          }
-          sum[x][g] = (p[0] + p[1]) + (p[2] + p[3]);
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < 2; ++x) acc[x] += (sum[x][0] + sum[x][1]) + (sum[x][2] + sum[x][3]);
+      for (int i = 0; i < KS; ++i) kf[i] = raw.step(i);
     }
-    if (more) put(buf ^ 1);
+    const int c_lo = min(first_column(wg_key, rq.P, G), rq.ncols) / kWtCols * kWtCols;
+    const int cmin = first_column(key, rq.P, G);
+    const int all_see = first_column(wg_key + kw * 32 + 31, rq.P, G);   // columns from here on see every key of the wave
+    float acc = 0.f;
+    if (c_lo < rq.ncols) {
+      fetch(c_lo);
+      put(0);
+    }
     __syncthreads();
-  }
-  // ---- the two halves of a key's columns, then the waves that shared the columns --------------------
-  const float a0 = sum_halves(acc[0]), a1 = sum_halves(acc[1]);
-  float total = hg == 0 ? a0 : a1;     // lane = key key0 + lane
-  if constexpr (CS > 1) {
-    if (cs > 0) part[((cs - 1) * KW + kw) * 64 + lane] = total;
-    __syncthreads();
-    if (cs > 0) return;
+    int buf = 0;
+    for (int c0 = c_lo; c0 < rq.ncols; c0 += kWtCols, buf ^= 1) {
+      const bool more = c0 + kWtCols < rq.ncols;
+      if (more) fetch(c0 + kWtCols);
+      for (int t = cs; t < TILES; t += CS) {
+        const int cb = c0 + 32 * t;
+        if (cb >= rq.ncols) break;
+        const char* qb = qs[buf] + 32 * t * kRowBytes;
+        f32x16_t s;
 #pragma unroll
-    for (int c = 1; c < CS; ++c) total += part[((c - 1) * KW + kw) * 64 + lane];
+        for (int i = 0; i < KS; ++i) {
+          const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(qb + l32 * kRowBytes + ((wt_chunk<D, MX4>(i, hg) ^ fk<D>(l32)) * 16));
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, kf[i], i == 0 ? f32x16_t{} : s, 0, 0, 0);
+        }
+        acc += wt_sum(s, scale_log2, cb, hg, cb < all_see || cb + 32 > rq.ncols, cmin, rq.ncols,
+                      [&](int g) { return *reinterpret_cast<const f32x4_t*>(&ls[buf][32 * t + 8 * g + 4 * hg]); });
+      }
+      if (more) put(buf ^ 1);
+      __syncthreads();
+    }
+    // the two halves of a key's columns, then the waves that shared the columns
+    float total = sum_halves(acc);
+    if constexpr (CS > 1) {
+      if (cs > 0 && hg == 0) part[((cs - 1) * KW + kw) * 32 + l32] = total;
+      __syncthreads();
+      if (cs == 0) {
+#pragma unroll
+        for (int c = 1; c < CS; ++c) total += part[((c - 1) * KW + kw) * 32 + l32];
+      }
+    }
+    if (cs == 0 && hg == 0 && key < rq.bound) wrow[key] = accumulate ? wrow[key] + total : total;
   }
-  const int key = key0 + lane;
-  if (key >= bound) return;
-  float* w = weights + (static_cast<int64_t>(r) * hkv + kvh) * w_stride + key;
-  *w = accumulate ? *w + total : total;
+}
+
+// Few columns (decode): columns stay, 32 of them in registers, and keys stream, 32 at a time for a wave,
+// the next 32 on their way meanwhile.  Waves of n_split work-groups take a request's subtiles in turn.
+template <int D, bool MX4>
+__global__ __launch_bounds__(256, MX4 || D == 64 ? 4 : 3) void attn_weights_stream_kernel(
+    const uint8_t* __restrict__ pool, const uint16_t* __restrict__ q, const float* __restrict__ lse,
+    const int32_t* __restrict__ block_tables, int bt_stride, const int32_t* __restrict__ cu_q,
+    const int32_t* __restrict__ seq_lens, int64_t n_q, int64_t num_blocks, int hq, int hkv, GroupDiv gd, float scale_log2,
+    float* __restrict__ weights, int64_t w_stride, int accumulate, int n_split) {
+  constexpr int KS = D / 16;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hg = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = blockIdx.x % hkv, r = blockIdx.y, G = static_cast<int>(gd.g);
+  const WtReq rq = wt_request(r, block_tables, bt_stride, cu_q, seq_lens, n_q, G, w_stride);
+  float* const wrow = weights + (static_cast<int64_t>(r) * hkv + kvh) * w_stride;
+  const int first = blockIdx.x / hkv * 4 + wave, by = 4 * n_split, nsub = (rq.bound + 31) / 32;
+  if (first >= nsub) return;
+  const int tiles = max((rq.ncols + 31) / 32, accumulate ? 0 : 1);
+  for (int t = 0; t < tiles; ++t) {                  // more than 32 columns: pass after pass over the same keys
+    const int cb = 32 * t, c = cb + l32, tok = gd.tok(c);
+    const int64_t row = c < rq.ncols ? static_cast<int64_t>(rq.q0 + tok) * hq + kvh * G + (c - tok * G) : 0;
+    WtKey<D, MX4> raw;
+    float old = 0.f;
+    auto fetch = [&](int sub, int32_t ph) {
+      const int key = sub * 32 + l32;
+      raw.load(pool, ph, num_blocks, hkv, kvh, key, hg);
+      if ((accumulate || t > 0) && hg == 0) old = key < rq.bound ? wrow[key] : 0.f;
+    };
+    auto block = [&](int sub) { return rq.bt[min(sub * 32 + l32, rq.bound - 1) >> 4]; };
+    fetch(first, block(first));
+    int32_t ph = block(min(first + by, nsub - 1));
+    bf16x8_t a[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) {
+      a[i] = bf16x8_t{};
+      if (c < rq.ncols) __builtin_memcpy(&a[i], q + row * D + wt_chunk<D, MX4>(i, hg) * 8, 16);
+    }
+    // a column that is not there: q of zeros and a sum of infinity give a weight of zero
+    const float mine = c < rq.ncols ? lse[row] * kLog2e : INFINITY;
+    f32x4_t l4[4];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) l4[g][j] = __shfl(mine, 8 * g + 4 * hg + j);
+    const int last = cb + min(32, rq.ncols - cb) - 1, pos0 = rq.P + gd.tok(cb);
+    for (int sub = first; sub < nsub; sub += by) {
+      f32x16_t s;
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], raw.step(i), i == 0 ? f32x16_t{} : s, 0, 0, 0);
+      const float was = old;
+      if (sub + by < nsub) {
+        fetch(sub + by, ph);
+        ph = block(min(sub + 2 * by, nsub - 1));
+      }
+      const int key = sub * 32 + l32;
+      const float total = sum_halves(wt_sum(s, scale_log2, cb, hg, sub * 32 + 31 > pos0 || last < cb, first_column(key, rq.P, G),
+                                            last + 1, [&](int g) { return l4[g]; }));
+      if (hg == 0 && key < rq.bound) wrow[key] = was + total;
+    }
+  }
 }
 
 }  // namespace
@@ -198,21 +306,34 @@ extern "C" int32_t arckv_attention_weights(const void* k_pool, int32_t layout, c
   if (num_blocks == 0) return arckv::fail(ARCKV_EINVAL, "%s: num_blocks", fn);
   const int G = num_q_heads / num_kv_heads;
   const int64_t keys = std::min<int64_t>(w_stride, static_cast<int64_t>(bt_stride) * 16);
-  const int KW = 8;
-  const int64_t wgs = (keys + KW * 64 - 1) / (KW * 64) * num_kv_heads;
-  if (wgs > INT32_MAX) return arckv::fail(ARCKV_EINVAL, "%s: too many keys", fn);
-  const dim3 grid(static_cast<unsigned>(wgs), n_reqs);
+  const int64_t pairs = static_cast<int64_t>(n_reqs) * num_kv_heads;
   auto* st = static_cast<hipStream_t>(stream);
-#define ARCKV_WEIGHTS(DD, MM, KK)                                                                              \
-  hipLaunchKernelGGL((attn_weights_kernel<DD, MM, KK>), grid, dim3(512), 0, st, static_cast<const uint8_t*>(k_pool), \
-                     static_cast<const uint16_t*>(q), lse, block_tables, bt_stride, cu_q, seq_lens, n_q, num_blocks,  \
-                     num_q_heads, num_kv_heads, G, scale * 1.4426950408889634f, weights, w_stride, accumulate)
-  const bool mx = layout == ARCKV_LAYOUT_MX4;
+  const GroupDiv gd{static_cast<uint32_t>(G), G == 1 ? 0 : static_cast<uint32_t>(((1ull << 32) + G - 1) / G)};
+  // work-groups of `per` keys for each (request, KV head): about `want` in all, no more than its keys need
+  auto split = [&](int64_t per, int64_t want) {
+    return static_cast<int>(std::max<int64_t>(1, std::min((keys + per - 1) / per, (want + pairs - 1) / pairs)));
+  };
+#define ARCKV_WEIGHTS(KERNEL, THREADS, PER, WANT)                                                              \
+  do {                                                                                                         \
+    const int ns = split(PER, WANT);                                                                           \
+    hipLaunchKernelGGL((KERNEL), dim3(static_cast<unsigned>(ns) * num_kv_heads, n_reqs), dim3(THREADS), 0, st, \
+                       static_cast<const uint8_t*>(k_pool), static_cast<const uint16_t*>(q), lse, block_tables, \
+                       bt_stride, cu_q, seq_lens, n_q, num_blocks, num_q_heads, num_kv_heads, gd,              \
+                       scale * 1.4426950408889634f, weights, w_stride, accumulate, ns);                        \
+  } while (0)
+#define ARCKV_WEIGHTS_DM(DD, MM)                                                                     \
+  do {                                                                                               \
+    if (few) ARCKV_WEIGHTS((attn_weights_stream_kernel<DD, MM>), 256, 128, 4096);                    \
+    else if (pairs * ((keys + 255) / 256) >= 500) ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, 8>), 512, 256, 4096); \
+    else ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, 4>), 512, 128, 4096);                            \
+  } while (0)
+  const bool few = n_q * G <= static_cast<int64_t>(n_reqs) * 32;
   if (head_dim == 64) {
-    if (mx) ARCKV_WEIGHTS(64, true, 8); else ARCKV_WEIGHTS(64, false, 8);
+    if (layout == ARCKV_LAYOUT_MX4) ARCKV_WEIGHTS_DM(64, true); else ARCKV_WEIGHTS_DM(64, false);
   } else {
-    if (mx) ARCKV_WEIGHTS(128, true, 8); else ARCKV_WEIGHTS(128, false, 8);
+    if (layout == ARCKV_LAYOUT_MX4) ARCKV_WEIGHTS_DM(128, true); else ARCKV_WEIGHTS_DM(128, false);
   }
+#undef ARCKV_WEIGHTS_DM
 #undef ARCKV_WEIGHTS
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return arckv::fail(ARCKV_EDEVICE, "%s: %s", fn, hipGetErrorString(e));
