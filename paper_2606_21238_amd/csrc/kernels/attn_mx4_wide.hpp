@@ -115,15 +115,25 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     ARCKV_CHECK_WAVE(ph < 0 || static_cast<uint32_t>(ph) >= nb32, ARCKV_CHECK_BLOCK);
     // wave-uniform; an entry out of range reads block 0
     const int32_t pb = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(ph) >= nb32 ? 0 : ph);
-    const uint8_t* base = pool + (static_cast<int64_t>(pb) * blk_stride + head);
+    uint8_t* base = const_cast<uint8_t*>(pool) + (static_cast<int64_t>(pb) * blk_stride + head);
+    // one block of one head as a buffer: its address stays in scalar registers
+    const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(base, 0, L4::kBytes, 0x00027000);
     const Place p = place();
     const uint32_t c_ofs = p.piece * (4 * NB);           // of the codes of either
     const uint32_t ks_ofs = L4::kKScale + (p.piece / 8) * L4::kGroups + (p.piece % 8) * NB / 4;
     const uint32_t vs_ofs = L4::kVScale + (p.vpair / 16) * 16 + p.vhalf * 8 + p.vquad * 4;
-    __builtin_memcpy(x.k, __builtin_assume_aligned(base + c_ofs, 4 * NB), 4 * NB);
-    __builtin_memcpy(x.v, __builtin_assume_aligned(base + L4::kV + c_ofs, 4 * NB), 4 * NB);
-    __builtin_memcpy(x.vs, __builtin_assume_aligned(base + vs_ofs, 4 * NB), 4 * NB);
-    x.ks = base[ks_ofs];
+    if constexpr (NB == 2) {
+      const auto k = __builtin_amdgcn_raw_buffer_load_b64(buf, c_ofs, 0, 0);
+      const auto v = __builtin_amdgcn_raw_buffer_load_b64(buf, L4::kV + c_ofs, 0, 0);
+      const auto vs = __builtin_amdgcn_raw_buffer_load_b64(buf, vs_ofs, 0, 0);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) { x.k[i] = k[i]; x.v[i] = v[i]; x.vs[i] = vs[i]; }
+    } else {
+      x.k[0] = __builtin_amdgcn_raw_buffer_load_b32(buf, c_ofs, 0, 0);
+      x.v[0] = __builtin_amdgcn_raw_buffer_load_b32(buf, L4::kV + c_ofs, 0, 0);
+      x.vs[0] = __builtin_amdgcn_raw_buffer_load_b32(buf, vs_ofs, 0, 0);
+    }
+    x.ks = __builtin_amdgcn_raw_buffer_load_b8(buf, ks_ofs, 0, 0);
   };
   // Before a masked tile is converted: V of the keys past the prompt's end may be anything, and V of a
   // key that only later columns see may be NaN.  Neither may meet a weight of zero, so their scales
@@ -144,8 +154,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
   // conversions, in parts: NB 16-byte chunks of a K row, then 4 NB tokens of two dimensions of V
   constexpr int PARTS = 2 * NB + 2;
   uint32_t vx[4 * NB];
-  auto convert = [&](const Raw& x, int tile, int part) {
-    const int st = (tile % kSt) * 2 * TILE;
+  auto convert = [&](const Raw& x, int st, int part) {          // st: byte offset of the tile's stage
     if (part < NB) {
       const float ks = mx4::scale_value(x.ks);
       const uint32_t c = x.k[part];
@@ -236,22 +245,28 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
   };
 
   // ---- M phase: V^T P, then K Q^T of the next tile, with the conversion of tile j + 2 between ----------
-  Raw raw;                          // bytes of tile j + 2, then of tile j + 3
-  auto m_phase = [&](int j) {
-    const char* vb = smem + (j % kSt) * 2 * TILE + TILE;
-    const char* kb = smem + ((j + 1) % kSt) * 2 * TILE;
-    const int vlane = l32 * 32 + ((hg ^ sv(l32)) * 16);
+  // Bytes of tile j + 2, and of tile j + 3 on their way.  D = 64 has registers for one of them: its load
+  // goes out once the conversion is through.
+  constexpr bool kAhead = D == 128;
+  Raw raw, next;
+  // Byte offsets of the stages of tiles j, j + 1 and j + 2 of the step being run.
+  int st0 = 0, st1 = 2 * TILE, st2 = 4 * TILE;
+  auto m_phase = [&]() {
+    // The lane's operand of V: rows l32 + 32 md of block sp, its half.  Of K: row pi(l32) + 32 mb, chunk 2 ks + hg
+    // swizzled: stages and rows start at multiples of 256 (D = 64: 128) bytes, so chunks 2 ks on are an
+    // exclusive or away.
+    const char* const va = smem + (st0 + TILE + l32 * 32 + ((hg ^ sv(l32)) * 16));
+    const uint32_t kr = pi_row(l32), ka = st1 + kr * (2 * D) + ((hg ^ fk<D>(kr)) * 16);
     auto op_at = [&](int n) -> bf16x8_t {
       if (n < 4 * DM) {
         const int sp = n / DM, md = n % DM;
-        return *reinterpret_cast<const bf16x8_t*>(vb + sp * BLK_BYTES + md * 1024 + vlane);
+        return *reinterpret_cast<const bf16x8_t*>(va + sp * BLK_BYTES + md * 1024);
       }
       const int ks = (n - 4 * DM) / 2, mb = (n - 4 * DM) % 2;
-      const int r = mb * 32 + pi_row(l32);
-      const int c = 2 * ks + hg;
-      return *reinterpret_cast<const bf16x8_t*>(kb + r * 2 * D + ((c ^ fk<D>(r)) * 16));
+      return *reinterpret_cast<const bf16x8_t*>(smem + (ka ^ (ks * 32)) + mb * (64 * D));
     };
     constexpr int EVERY = NOP / (PARTS + 2);
+    if constexpr (kAhead) load(__builtin_amdgcn_readfirstlane(next_v), next);
     bf16x8_t opv[NOP];
 #pragma unroll
     for (int n = 0; n < PD; ++n) opv[n] = op_at(n);
@@ -267,10 +282,18 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
         sacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opv[n], qf[ks], ks == 0 ? f32x16_t{} : sacc[mb], 0, 0, 0);
       }
       if (n % EVERY == EVERY / 2) {
-        if (n / EVERY < PARTS) convert(raw, j + 2, n / EVERY);
-        else if (n / EVERY == PARTS) load(__builtin_amdgcn_readfirstlane(next_v), raw);
+        if (n / EVERY < PARTS) convert(raw, st2, n / EVERY);
+        else if (n / EVERY == PARTS && !kAhead) load(__builtin_amdgcn_readfirstlane(next_v), raw);
       }
     }
+    // keep the operand reads PD ahead: DS reads, then one MFMA and one read at a time
+    __builtin_amdgcn_sched_group_barrier(0x100, PD, 0);
+#pragma unroll
+    for (int n = 0; n < NOP - PD; ++n) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_group_barrier(0x008, PD, 0);
   };
   auto s_first = [&]() {
     const char* kb = smem;
@@ -337,11 +360,11 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     if (tile_masked(0)) mask_v(raw, 0);
     if (tile_masked(1)) mask_v(raw1, 1);
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) convert(raw, 0, p);
+    for (int p = 0; p < PARTS; ++p) convert(raw, st0, p);
     fetch_next(2);
     barrier();                                           // every wave has its queries
 #pragma unroll
-    for (int p = 0; p < PARTS; ++p) convert(raw1, 1, p);
+    for (int p = 0; p < PARTS; ++p) convert(raw1, st1, p);
     load(__builtin_amdgcn_readfirstlane(next_v), raw);
     fetch_next(3);
     barrier();                                           // tiles 0 and 1 are there
@@ -355,7 +378,12 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
       barrier();
       // past the key range the table gives block 0 and the conversion writes a stage nobody reads
       if (tile_masked(j + 2)) mask_v(raw, j + 2);
-      m_phase(j);
+      m_phase();
+      if constexpr (kAhead) raw = next;
+      const int st3 = st0;
+      st0 = st1;
+      st1 = st2;
+      st2 = st3;
       fetch_next(j + 4);
       pin_m();
       if (grp == 0 || j + 1 < ntiles) barrier();
