@@ -91,9 +91,9 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
   struct Place {
     int piece, krow, kch, vpair, vhalf, vquad;
   };
-  auto place = [&]() {
+  auto place = [&](bool fresh) {
     Place p;
-    p.piece = (wave & 1) * 64 + (D == 64 ? lane_now() : lane);
+    p.piece = (wave & 1) * 64 + (fresh ? lane_now() : lane);
     p.krow = wblk * 16 + p.piece / 8;                    // row of the tile, and 16-byte chunk of it
     p.kch = NB * (p.piece % 8);
     p.vpair = NB == 2 ? p.piece % 64 : (p.piece % 64) / 2;
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     uint8_t* base = const_cast<uint8_t*>(pool) + (static_cast<int64_t>(pb) * blk_stride + head);
     // one block of one head as a buffer: its address stays in scalar registers
     const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(base, 0, L4::kBytes, 0x00027000);
-    const Place p = place();
+    const Place p = place(D == 64);
     const uint32_t c_ofs = p.piece * (4 * NB);           // of the codes of either
     const uint32_t ks_ofs = L4::kKScale + (p.piece / 8) * L4::kGroups + (p.piece % 8) * NB / 4;
     const uint32_t vs_ofs = L4::kVScale + (p.vpair / 16) * 16 + p.vhalf * 8 + p.vquad * 4;
@@ -139,7 +139,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
   // key that only later columns see may be NaN.  Neither may meet a weight of zero, so their scales
   // are replaced; NaN comes back at the end for the columns that see the first such key.
   auto mask_v = [&](Raw& x, int tile) {
-    const Place p = place();
+    const Place p = place(D == 64);
     int first = INT32_MAX;
 #pragma unroll
     for (int k = 4 * NB - 1; k >= 0; --k) {
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
       const float ks = mx4::scale_value(x.ks);
       const uint32_t c = x.k[part];
       const u32x4_t v = {mx4::decode2<0>(c, ks), mx4::decode2<1>(c, ks), mx4::decode2<2>(c, ks), mx4::decode2<3>(c, ks)};
-      const Place p = place();
+      const Place p = place(D == 64);
       *reinterpret_cast<u32x4_t*>(smem + st + p.krow * 2 * D + (((p.kch + part) ^ fk<D>(p.krow)) * 16)) = v;
     } else if (part < 2 * NB) {
       const int i = part - NB;
@@ -173,7 +173,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
       uint32_t v[2 * NB];
 #pragma unroll
       for (int k = 0; k < 2 * NB; ++k) v[k] = __builtin_amdgcn_perm(vx[2 * k + 1], vx[2 * k], d == 0 ? 0x05040100u : 0x07060302u);
-      const Place p = place();
+      const Place p = place(false);
       char* to = smem + st + TILE + wblk * BLK_BYTES + (2 * p.vpair + d) * 32 + ((p.vhalf ^ sv(2 * p.vpair)) * 16) + p.vquad * 8;
       __builtin_memcpy(__builtin_assume_aligned(to, 8 * NB), v, 8 * NB);
     }
