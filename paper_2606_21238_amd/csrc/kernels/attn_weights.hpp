@@ -74,9 +74,9 @@ template <int D, bool MX4>
 __device__ __forceinline__ int wt_chunk(int i, int hg) { return MX4 ? hg * (D / 16) + i : 2 * i + hg; }
 
 // The weights of 32 columns for this lane's key, of S's 16 registers: register 4 g + j is column cb + 8 g + 4 hg + j.
-template <class Lse>
-__device__ __forceinline__ float wt_sum(const f32x16_t& s, float scale_log2, int cb, int hg, bool masked, int cmin,
-                                        int ncols, Lse lse) {
+template <bool MASKED, class Lse>
+__device__ __forceinline__ float wt_sum(const f32x16_t& s, Lse lse, float scale_log2, int cb, int hg,
+                                        int cmin, int ncols) {
   float sum[4];
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
@@ -84,7 +84,7 @@ __device__ __forceinline__ float wt_sum(const f32x16_t& s, float scale_log2, int
     float p[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) p[j] = fast_exp2(fmaf(s[4 * g + j], scale_log2, -l4[j]));
-    if (masked) {
+    if constexpr (MASKED) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         const int c = cb + 8 * g + 4 * hg + j;
@@ -101,75 +101,62 @@ __device__ __forceinline__ int first_column(int64_t key, int P, int G) {
   return static_cast<int>(min(max(key - P, static_cast<int64_t>(0)) * G, static_cast<int64_t>(INT32_MAX)));
 }
 
-// Many columns: keys stay, columns stream.  A work-group takes KW x 32 keys at a time, n_split work-groups
-// of a (request, KV head) in turn.
-template <int D, bool MX4, int KW>
+// Many columns: keys stay, columns stream.  n_split work-groups share a (request, KV head) in equal runs of
+// subtiles of 32 keys; a work-group takes 8 of its subtiles at a time, one for each wave, and where fewer
+// are left, 2 or 4 waves share a subtile's columns.
+template <int D, bool MX4, bool ANY>
 __global__ __launch_bounds__(512, 4) void attn_weights_kernel(
     const uint8_t* __restrict__ pool, const uint16_t* __restrict__ q, const float* __restrict__ lse,
     const int32_t* __restrict__ block_tables, int bt_stride, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ seq_lens, int64_t n_q, int64_t num_blocks, int hq, int hkv, GroupDiv gd, float scale_log2,
     float* __restrict__ weights, int64_t w_stride, int accumulate, int n_split) {
-  constexpr int kThreads = 512, CS = 8 / KW, KS = D / 16, TILES = kWtCols / 32;
+  constexpr int kThreads = 512, KS = D / 16, TILES = kWtCols / 32;
   constexpr int kRowBytes = D * 2, kChunkBytes = kWtCols * kRowBytes;
   constexpr int NLD = kChunkBytes / (kThreads * 16);      // 16-byte loads of a thread for a chunk
-  constexpr int kRowThreads = kRowBytes / 16, kRowsPer = kThreads / kRowThreads;
+  constexpr int kRowThreads = kRowBytes / 16, kWaveRows = 64 / kRowThreads;
   __shared__ __attribute__((aligned(1024))) char qs[2][kChunkBytes];
   __shared__ __attribute__((aligned(16))) float ls[2][kWtCols];
-  __shared__ float part[CS > 1 ? (CS - 1) * KW * 32 : 1];
+  __shared__ float part[6][2][64];                        // of the waves that only help
   const int tid = threadIdx.x, lane = tid & 63, l32 = lane & 31, hg = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), kw = wave % KW, cs = wave / KW;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % hkv, r = blockIdx.y, G = static_cast<int>(gd.g);
   const WtReq rq = wt_request(r, block_tables, bt_stride, cu_q, seq_lens, n_q, G, w_stride);
   float* const wrow = weights + (static_cast<int64_t>(r) * hkv + kvh) * w_stride;
 
-  // columns: rows of q and their sums, a chunk ahead in registers
-  u32x4_t qn[NLD];
+  // Rows of q straight into LDS, chunk x of row c at x ^ fk(c); columns past the last load row 0, never used.
+  // ANY: q at an address that is not a multiple of 16 goes through registers.
   float ln = 0.f;
-  // (four columns from a multiple of four are rows behind each other where G is a multiple of four: their
-  // address is the wave's, not the lane's)
-  const bool by_four = G % 4 == 0;
-  auto fetch = [&](int c0) {
-    if (by_four && c0 + kWtCols <= rq.ncols) {
-#pragma unroll
-      for (int i = 0; i < NLD; ++i) {
-        constexpr int kWaveRows = 64 / kRowThreads;       // 4 (D = 128) or 8 rows of a wave and load
-        const int c = c0 + i * kRowsPer + wave * kWaveRows;
-        const int t0 = gd.tok(c);
-        const uint16_t* b0 = q + (static_cast<int64_t>(rq.q0 + t0) * hq + kvh * G + (c - t0 * G)) * D;
-        uint32_t ofs = lane * 8;
-        if (kWaveRows == 8 && G == 4) ofs += lane >= 32 ? (hq - 4) * D : 0;      // the second four are the next token's
-        __builtin_memcpy(&qn[i], b0 + ofs, 16);
-      }
-      if (tid < kWtCols) {
-        const int c = c0 + tid, tok = gd.tok(c);
-        ln = lse[static_cast<int64_t>(rq.q0 + tok) * hq + kvh * G + (c - tok * G)] * kLog2e;
-      }
-      return;
-    }
+  auto fetch = [&](int c0, int buf) {
 #pragma unroll
     for (int i = 0; i < NLD; ++i) {
-      const int c = c0 + i * kRowsPer + tid / kRowThreads, tok = gd.tok(c);
-      const int64_t row = static_cast<int64_t>(rq.q0 + tok) * hq + kvh * G + (c - tok * G);
-      qn[i] = u32x4_t{};
-      if (c < rq.ncols) __builtin_memcpy(&qn[i], q + row * D + (tid % kRowThreads) * 8, 16);
+      const int at = i * (kThreads * 16) + wave * 1024;   // of the wave's 64 pieces of 16 bytes
+      const int cl = at / kRowBytes + lane / kRowThreads, c = c0 + cl, tok = gd.tok(c);
+      const int64_t row = c < rq.ncols ? static_cast<int64_t>(rq.q0 + tok) * hq + kvh * G + (c - tok * G) : 0;
+      const uint16_t* src = q + row * D + (((lane % kRowThreads) ^ fk<D>(cl)) * 8);
+      if constexpr (ANY) load_any16(src, qs[buf] + at + lane * 16);
+      else load_lds16(src, (lds_void*)(qs[buf] + at));
     }
     if (tid < kWtCols) {
       const int c = c0 + tid, tok = gd.tok(c);
       ln = c < rq.ncols ? lse[static_cast<int64_t>(rq.q0 + tok) * hq + kvh * G + (c - tok * G)] * kLog2e : 0.f;
     }
   };
-  auto put = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < NLD; ++i) {
-      const int c = i * kRowsPer + tid / kRowThreads, ch = tid % kRowThreads;
-      *reinterpret_cast<u32x4_t*>(qs[buf] + c * kRowBytes + ((ch ^ fk<D>(c)) * 16)) = qn[i];
-    }
+  auto landed = [&](int buf) {                            // this wave's part of a chunk is in LDS
     if (tid < kWtCols) ls[buf][tid] = ln;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   };
+  static_assert(kWaveRows * kRowBytes == 1024, "a wave's load is whole rows");
 
-  for (int64_t wg_key = static_cast<int64_t>(blockIdx.x / hkv) * (KW * 32); wg_key < rq.bound;
-       wg_key += static_cast<int64_t>(n_split) * (KW * 32)) {
-    const int key = static_cast<int>(wg_key) + kw * 32 + l32;
+  const int nsub = (rq.bound + 31) / 32;
+  const int64_t share = blockIdx.x / hkv;
+  const int sub1 = static_cast<int>((share + 1) * nsub / n_split);
+  for (int sub = static_cast<int>(share * nsub / n_split), step; sub < sub1; sub += step) {
+    step = min(sub1 - sub, 8);
+    const int KW = step > 4 ? 8 : step > 2 ? 4 : 2, CS = 8 / KW;             // uniform
+    const int kw = wave % KW, cs = wave / KW;
+    const int64_t wg_key = static_cast<int64_t>(sub) * 32;
+    const int key = sub * 32 + kw * 32 + l32;
+    const bool mine = kw < step;                                             // a subtile of its own
     bf16x8_t kf[KS];
     {
       WtKey<D, MX4> raw;
@@ -180,43 +167,63 @@ __global__ __launch_bounds__(512, 4) void attn_weights_kernel(
     const int c_lo = min(first_column(wg_key, rq.P, G), rq.ncols) / kWtCols * kWtCols;
     const int cmin = first_column(key, rq.P, G);
     const int all_see = first_column(wg_key + kw * 32 + 31, rq.P, G);   // columns from here on see every key of the wave
-    float acc = 0.f;
+    // sums of the tiles 0, 1, 2, 3 modulo 4 (of which a wave has every CS-th), added up in one order whoever has them
+    float acc[TILES] = {};
     if (c_lo < rq.ncols) {
-      fetch(c_lo);
-      put(0);
+      fetch(c_lo, 0);
+      landed(0);
     }
     __syncthreads();
     int buf = 0;
     for (int c0 = c_lo; c0 < rq.ncols; c0 += kWtCols, buf ^= 1) {
       const bool more = c0 + kWtCols < rq.ncols;
-      if (more) fetch(c0 + kWtCols);
-      for (int t = cs; t < TILES; t += CS) {
-        const int cb = c0 + 32 * t;
-        if (cb >= rq.ncols) break;
-        const char* qb = qs[buf] + 32 * t * kRowBytes;
+      if (more) fetch(c0 + kWtCols, buf ^ 1);
+      const int nt = mine ? min(TILES, (rq.ncols - c0 + 31) / 32) : 0;
+      // rows start at multiples of 256 (D = 64: 128) bytes: the swizzled chunks are an exclusive or away
+      const uint32_t a0 = l32 * kRowBytes + ((wt_chunk<D, MX4>(0, hg) ^ fk<D>(l32)) * 16);
+      auto at = [&](int t, int i) {
+        const char* qb = qs[buf] + t * (32 * kRowBytes);
+        return *reinterpret_cast<const bf16x8_t*>(qb + (a0 ^ (wt_chunk<D, MX4>(i, 0) * 16)));
+      };
+      // a tile's first operands are read beside the exponentials of the tile before (as many as 128 registers hold)
+      constexpr int kAhead = KS / 2 - (MX4 && D == 128 ? 1 : 0);
+      bf16x8_t a[KS];
+      auto read_first = [&](int t) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) a[i] = at(t, i);
+      };
+      if (cs < nt) read_first(cs);
+#pragma unroll
+      for (int k = 0; k < TILES; ++k) {
+        const int t = cs + CS * k, cb = c0 + 32 * t;
+        if (t >= nt) break;
+#pragma unroll
+        for (int i = kAhead; i < KS; ++i) a[i] = at(t, i);
         f32x16_t s;
 #pragma unroll
-        for (int i = 0; i < KS; ++i) {
-          const bf16x8_t a = *reinterpret_cast<const bf16x8_t*>(qb + l32 * kRowBytes + ((wt_chunk<D, MX4>(i, hg) ^ fk<D>(l32)) * 16));
-          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, kf[i], i == 0 ? f32x16_t{} : s, 0, 0, 0);
-        }
-        acc += wt_sum(s, scale_log2, cb, hg, cb < all_see || cb + 32 > rq.ncols, cmin, rq.ncols,
-                      [&](int g) { return *reinterpret_cast<const f32x4_t*>(&ls[buf][32 * t + 8 * g + 4 * hg]); });
+        for (int i = 0; i < KS; ++i)
+          s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], kf[i], i == 0 ? f32x16_t{} : s, 0, 0, 0);
+        if (t + CS < nt) read_first(t + CS);
+        const float* lt = &ls[buf][32 * t + 4 * hg];
+        auto l4 = [&](int g) { return *reinterpret_cast<const f32x4_t*>(lt + 8 * g); };
+        if (cb < all_see || cb + 32 > rq.ncols) acc[k] += wt_sum<true>(s, l4, scale_log2, cb, hg, cmin, rq.ncols);
+        else acc[k] += wt_sum<false>(s, l4, scale_log2, cb, hg, cmin, rq.ncols);
       }
-      if (more) put(buf ^ 1);
+      if (more) landed(buf ^ 1);
       __syncthreads();
     }
-    // the two halves of a key's columns, then the waves that shared the columns
-    float total = sum_halves(acc);
-    if constexpr (CS > 1) {
-      if (cs > 0 && hg == 0) part[((cs - 1) * KW + kw) * 32 + l32] = total;
-      __syncthreads();
-      if (cs == 0) {
-#pragma unroll
-        for (int c = 1; c < CS; ++c) total += part[((c - 1) * KW + kw) * 32 + l32];
+    float total = (acc[0] + acc[1]) + (acc[2] + acc[3]);
+    if (CS > 1) {
+      if (cs > 0) {
+        part[wave - KW][0][lane] = acc[0];
+        part[wave - KW][1][lane] = acc[1];
       }
+      __syncthreads();
+      if (CS == 2) total = (acc[0] + part[kw][0][lane]) + (acc[1] + part[kw][1][lane]);
+      else total = (acc[0] + part[kw][0][lane]) + (part[kw + KW][0][lane] + part[kw + 2 * KW][0][lane]);
     }
-    if (cs == 0 && hg == 0 && key < rq.bound) wrow[key] = accumulate ? wrow[key] + total : total;
+    total = sum_halves(total);             // the other columns of the key
+    if (cs == 0 && mine && hg == 0 && key < rq.bound) wrow[key] = accumulate ? wrow[key] + total : total;
   }
 }
 
@@ -263,7 +270,7 @@ __global__ __launch_bounds__(256, MX4 || D == 64 ? 4 : 3) void attn_weights_stre
     for (int g = 0; g < 4; ++g)
 #pragma unroll
       for (int j = 0; j < 4; ++j) l4[g][j] = __shfl(mine, 8 * g + 4 * hg + j);
-    const int last = cb + min(32, rq.ncols - cb) - 1, pos0 = rq.P + gd.tok(cb);
+    const int pos0 = rq.P + gd.tok(cb);
     for (int sub = first; sub < nsub; sub += by) {
       f32x16_t s;
 #pragma unroll
@@ -275,8 +282,11 @@ __global__ __launch_bounds__(256, MX4 || D == 64 ? 4 : 3) void attn_weights_stre
         ph = block(min(sub + 2 * by, nsub - 1));
       }
       const int key = sub * 32 + l32;
-      const float total = sum_halves(wt_sum(s, scale_log2, cb, hg, sub * 32 + 31 > pos0 || last < cb, first_column(key, rq.P, G),
-                                            last + 1, [&](int g) { return l4[g]; }));
+      const bool masked = sub * 32 + 31 > pos0 || rq.ncols <= cb;
+      auto sums = [&](int g) { return l4[g]; };
+      const float mine32 = masked ? wt_sum<true>(s, sums, scale_log2, cb, hg, first_column(key, rq.P, G), rq.ncols)
+                                  : wt_sum<false>(s, sums, scale_log2, cb, hg, 0, rq.ncols);
+      const float total = sum_halves(mine32);
       if (hg == 0 && key < rq.bound) wrow[key] = was + total;
     }
   }
@@ -324,9 +334,10 @@ extern "C" int32_t arckv_attention_weights(const void* k_pool, int32_t layout, c
 #define ARCKV_WEIGHTS_DM(DD, MM)                                                                     \
   do {                                                                                               \
     if (few) ARCKV_WEIGHTS((attn_weights_stream_kernel<DD, MM>), 256, 128, 4096);                    \
-    else if (pairs * ((keys + 255) / 256) >= 500) ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, 8>), 512, 256, 4096); \
-    else ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, 4>), 512, 128, 4096);                            \
+    else if (any) ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, true>), 512, 64, 512);                  \
+    else ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, false>), 512, 64, 512);                          \
   } while (0)
+  const bool any = reinterpret_cast<uintptr_t>(q) % 16 != 0;
   const bool few = n_q * G <= static_cast<int64_t>(n_reqs) * 32;
   if (head_dim == 64) {
     if (layout == ARCKV_LAYOUT_MX4) ARCKV_WEIGHTS_DM(64, true); else ARCKV_WEIGHTS_DM(64, false);
