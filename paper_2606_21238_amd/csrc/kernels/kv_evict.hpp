@@ -2,8 +2,10 @@
 //
 // evict_select: for every (request, KV head), which `keep` of L positions stay: the first n_first,
 // the last n_recent, and of the others those of the greatest weight, the lower position first
-// among equals.  One work-group finds the weight of the last one to stay by its bits, eight at a
-// time from the top (a histogram of each eight in LDS), then writes the kept positions in order.
+// among equals.  One work-group finds the weight of the last one to stay by its digits from the
+// top, 12, 10 and 10 bits, each from a histogram in LDS (of the keys that share the digits before; 12
+// bits first, because 8, the sign and most of the exponent, put most of the keys into a few bins, where
+// additions wait for each other: 74 us for 32 rows of 32768, and XXX), then writes the kept positions in order.
 // kv_compact: the kept tokens' K and V into other blocks, position i of the result from position
 // kept[i]; a head's tokens move on their own, so the same slot may hold another token for another
 // head.  A work-group writes one block of one head.
@@ -21,14 +23,22 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
   if (w != w) return 0;
   return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
+__device__ __forceinline__ float key_weight(uint32_t k) {
+  return __builtin_bit_cast(float, k & 0x80000000u ? k ^ 0x80000000u : ~k);
+}
 
-__global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
+constexpr int kSelWaves = kSelThreads / 64;
+
+// KEYS: how many keys a thread holds, so rows of up to 1024 KEYS are read once.
+template <int KEYS>
+__global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_kernel(
     const float* __restrict__ weights, int64_t w_stride, const int32_t* __restrict__ seq_lens, int hkv, int keep,
     int n_first, int n_recent, int32_t* __restrict__ kept, float* __restrict__ kept_weights, int64_t kw_stride) {
-  __shared__ int hist[256];
-  __shared__ int wave_take[kSelThreads / 64], wave_equal[kSelThreads / 64];
+  __shared__ int hist[4096];
+  __shared__ int wave_sum[kSelWaves], wave_take[kSelWaves], wave_equal[kSelWaves];
   __shared__ int pick, above;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, h = blockIdx.x, r = blockIdx.y;
+  const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.x, r = blockIdx.y;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int64_t seg = static_cast<int64_t>(r) * hkv + h;
   const float* w = weights + seg * w_stride;
   int32_t* out = kept + seg * keep;
@@ -38,74 +48,151 @@ __global__ __launch_bounds__(kSelThreads) void evict_select_kernel(
   const int lo = len <= keep ? 0 : n_first, hi = len <= keep ? 0 : len - n_recent;   // positions that compete
   int need = len <= keep ? 0 : keep - n_first - n_recent;                            // how many of them stay
 
-  // the key of the last one to stay, and how many with that very key
-  uint32_t prefix = 0;
-  if (need > 0) {
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      if (tid < 256) hist[tid] = 0;
-      __syncthreads();
-      for (int i = lo + tid; i < hi; i += kSelThreads) {
-        const uint32_t k = weight_key(w[i]);
-        if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&hist[(k >> shift) & 255u], 1);
+  // A wave has a run of positions, in tiles of KEYS x 64; the tile in its registers is read again only where
+  // a run has several.  Positions past the run have the key 0.
+  const int run = (len + kSelWaves * 64 - 1) / (kSelWaves * 64) * 64;
+  const int from = min(wave * run, len), to = min(from + run, len);
+  constexpr int kTile = KEYS * 64;
+  const int tiles = (run + kTile - 1) / kTile;
+  uint32_t key[KEYS];
+  int have = -1;
+  // f(u, i, key) for every position of the wave in order, four at a time past which there is nothing to do
+  auto each = [&](auto f) {
+    for (int t = 0; t < tiles; ++t) {
+      const int i0 = from + t * kTile, n = min(run - t * kTile, kTile);
+      if (have != t) {
+#pragma unroll
+        for (int u = 0; u < KEYS; u += 4) {
+          if (64 * u >= n) break;
+          float x[4];
+#pragma unroll
+          for (int v = 0; v < 4; ++v) {
+            const int i = i0 + 64 * (u + v) + lane;
+            x[v] = i < to ? w[i] : 0.f;
+          }
+#pragma unroll
+          for (int v = 0; v < 4; ++v) key[u + v] = i0 + 64 * (u + v) + lane < to ? weight_key(x[v]) : 0;
+        }
+        have = t;
       }
+#pragma unroll
+      for (int u = 0; u < KEYS; u += 4) {
+        if (64 * u >= n) break;
+#pragma unroll
+        for (int v = 0; v < 4; ++v) f(i0 + 64 * (u + v) + lane, key[u + v]);
+      }
+    }
+  };
+
+  // Most waves have a run of competing positions only, and need no look at a position.
+  const bool inner = from >= lo && from + run <= hi;
+  // the key of the last one to stay (its digits from the top), and how many with that very key
+  uint32_t prefix = 0xffffffffu;           // nobody competes: no key is greater
+  if (need > 0) {
+    prefix = 0;
+    constexpr int kShift[3] = {20, 10, 0}, kBits[3] = {12, 10, 10};
+#pragma unroll
+    for (int pass = 0; pass < 3; ++pass) {
+      const int shift = kShift[pass];
+      constexpr int kPer = 4096 / kSelThreads;
+      const int bins = 1 << kBits[pass];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (i * kSelThreads < bins) hist[i * kSelThreads + tid] = 0;
       __syncthreads();
-      if (wave == 0) {       // the highest digit with at least `need` keys from it up
-        int c[4], sum = 0;
+      auto count = [&](uint32_t k) {
+        if (pass == 0 || (k >> (shift + kBits[pass])) == (prefix >> (shift + kBits[pass])))
+          atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
+      };
+      // (the key 0 of positions behind an inner run only adds to the lowest digit, where it decides nothing)
+      if (inner) each([&](int, uint32_t k) { count(k); });
+      else each([&](int i, uint32_t k) { if (i >= lo && i < min(hi, to)) count(k); });
+      __syncthreads();
+      // the highest digit with at least `need` keys from it up: a thread has `per` of them, thread 0 the highest
+      const int per = bins / kSelThreads;    // 4, then 1
+      int c[kPer], sum = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { c[i] = hist[255 - (4 * lane + i)]; sum += c[i]; }
-        int upto = sum;
+      for (int i = 0; i < kPer; ++i) {
+        c[i] = i < per ? hist[bins - 1 - (per * tid + i)] : 0;
+        sum += c[i];
+      }
+      int upto = sum;
 #pragma unroll
-        for (int s = 1; s < 64; s <<= 1) {
-          const int x = __shfl_up(upto, s);
-          if (lane >= s) upto += x;
+      for (int s = 1; s < 64; s <<= 1) {
+        const int x = __shfl_up(upto, s);
+        if (lane >= s) upto += x;
+      }
+      if (lane == 63) wave_sum[wave] = upto;
+      __syncthreads();
+      int before = upto - sum;
+      for (int v = 0; v < wave; ++v) before += wave_sum[v];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        if (before < need && before + c[i] >= need) {
+          pick = bins - 1 - (per * tid + i);
+          above = before;
         }
-        int before = upto - sum;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (before < need && before + c[i] >= need) { pick = 255 - (4 * lane + i); above = before; }
-          before += c[i];
-        }
+        before += c[i];
       }
       __syncthreads();
       prefix |= static_cast<uint32_t>(pick) << shift;
       need -= above;
-      __syncthreads();
     }
-  } else {
-    prefix = 0xffffffffu;    // no key is greater
   }
 
-  // positions in order: greater keys, and the first `need` equal ones
-  int at = 0, equal = 0;
-  for (int i0 = 0; i0 < len; i0 += kSelThreads) {
-    const int i = i0 + tid;
-    const float x = i < len ? w[i] : 0.f;
-    const bool held = i < len && (i < lo || i >= hi);
-    const uint32_t k = weight_key(x);
-    const bool eq = i < len && !held && need > 0 && k == prefix;
-    const uint64_t eqs = __builtin_amdgcn_ballot_w64(eq);
-    if (lane == 0) wave_equal[wave] = __builtin_popcountll(eqs);
-    __syncthreads();
-    int rank = equal + __builtin_popcountll(eqs & ((1ull << lane) - 1)), all = equal;
-    for (int v = 0; v < kSelThreads / 64; ++v) {
-      if (v < wave) rank += wave_equal[v];
-      all += wave_equal[v];
-    }
-    const bool take = held || (i < len && !held && k > prefix) || (eq && rank < need);
-    const uint64_t takes = __builtin_amdgcn_ballot_w64(take);
-    if (lane == 0) wave_take[wave] = __builtin_popcountll(takes);
-    __syncthreads();
-    int dst = at + __builtin_popcountll(takes & ((1ull << lane) - 1)), next = at;
-    for (int v = 0; v < kSelThreads / 64; ++v) {
-      if (v < wave) dst += wave_take[v];
-      next += wave_take[v];
-    }
+  // Positions in order: greater keys, and the first `need` equal ones.  A wave counts its own, learns what the
+  // waves before it have, and writes.
+  auto classify = [&](int i, uint32_t k, bool& take, bool& eq) {
+    const bool held = i < lo || i >= hi;
+    take = i < to && (held || k > prefix);
+    eq = i < to && !held && need > 0 && k == prefix;
+  };
+  const bool plain = inner && prefix != 0;   // (prefix 0, a NaN: the key of what is not there)
+  int takes = 0, equals = 0;
+  if (plain) {
+    each([&](int, uint32_t k) {
+      takes += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k > prefix));
+      equals += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k == prefix));
+    });
+  } else {
+    each([&](int i, uint32_t k) {
+      bool take, eq;
+      classify(i, k, take, eq);
+      takes += __builtin_popcountll(__builtin_amdgcn_ballot_w64(take));
+      equals += __builtin_popcountll(__builtin_amdgcn_ballot_w64(eq));
+    });
+  }
+  if (lane == 0) {
+    wave_take[wave] = takes;
+    wave_equal[wave] = equals;
+  }
+  __syncthreads();
+  int at = 0, equal = 0;                   // of the waves before
+  for (int v = 0; v < wave; ++v) {
+    at += wave_take[v] + min(wave_equal[v], max(need - equal, 0));
+    equal += wave_equal[v];
+  }
+  auto put = [&](int i, uint32_t k, bool take) {
+    const uint64_t all = __builtin_amdgcn_ballot_w64(take);
     if (take) {
+      const int dst = at + __builtin_amdgcn_mbcnt_hi(static_cast<uint32_t>(all >> 32),
+                                                     __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(all), 0));
       out[dst] = i;
-      if (kw != nullptr) kw[dst] = x;
+      if (kw != nullptr) kw[dst] = key_weight(k);
     }
-    at = next;
-    equal = all;
+    at += __builtin_popcountll(all);
+  };
+  if (plain && equals == 0) {
+    each([&](int i, uint32_t k) { put(i, k, k > prefix); });
+  } else {
+    each([&](int i, uint32_t k) {
+      bool take, eq;
+      classify(i, k, take, eq);
+      const uint64_t eqs = __builtin_amdgcn_ballot_w64(eq);
+      take |= eq && equal + __builtin_popcountll(eqs & ((1ull << lane) - 1)) < need;
+      equal += __builtin_popcountll(eqs);
+      put(i, k, take);
+    });
   }
   for (int i = n_kept + tid; i < keep; i += kSelThreads) {
     out[i] = -1;
@@ -256,9 +343,14 @@ extern "C" int32_t arckv_evict_select(const float* weights, int64_t w_stride, co
   if (n_reqs == 0 || keep == 0) return ARCKV_OK;
   if ((weights == nullptr && w_stride > 0) || seq_lens == nullptr || kept == nullptr)
     return arckv::fail(ARCKV_EINVAL, "%s: NULL pointer", fn);
-  hipLaunchKernelGGL(evict_select_kernel, dim3(num_kv_heads, n_reqs), dim3(kSelThreads), 0,
-                     static_cast<hipStream_t>(stream), weights, w_stride, seq_lens, num_kv_heads, keep, n_first,
-                     n_recent, kept, kept_weights, kw_stride);
+  // rows for one work-group to a unit or fewer: 32 keys a thread; more: 16, and two work-groups to a unit
+  const bool one = static_cast<int64_t>(n_reqs) * num_kv_heads <= 256;
+#define ARCKV_SELECT(KEYS)                                                                                    \
+  hipLaunchKernelGGL(evict_select_kernel<KEYS>, dim3(num_kv_heads, n_reqs), dim3(kSelThreads), 0,             \
+                     static_cast<hipStream_t>(stream), weights, w_stride, seq_lens, num_kv_heads, keep,       \
+                     n_first, n_recent, kept, kept_weights, kw_stride)
+  if (one) ARCKV_SELECT(32); else ARCKV_SELECT(16);
+#undef ARCKV_SELECT
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return arckv::fail(ARCKV_EDEVICE, "%s: %s", fn, hipGetErrorString(e));
   return ARCKV_OK;
