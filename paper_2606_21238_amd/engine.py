@@ -367,7 +367,9 @@ class PrefillEngine:
                 raise ValueError("dst_tables names a block of the batch")
         ts = self._torch_stream(stream)
         with torch.cuda.stream(ts):
-            dev = torch.from_numpy(dst).to(self.device)
+            host = torch.empty(dst.shape, dtype=torch.int32, pin_memory=True)
+            host.numpy()[:] = dst
+            dev = host.to(self.device, non_blocking=True)
             kept = torch.empty((n, self.hkv, keep), dtype=torch.int32, device=self.device)
             kept_weights = torch.empty((n, self.hkv, keep), dtype=torch.float32, device=self.device)
         raw = self._stream(stream)

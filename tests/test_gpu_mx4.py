@@ -81,7 +81,8 @@ def test_scatter_and_gather(d, hkv, n, kind):
         assert np.array_equal(bf16_to_f64(bits(got)), w, equal_nan=True)
 
 
-@pytest.mark.parametrize("d,hkv,n,start", [(128, 8, 1000, 5), (64, 2, 300, 0), (128, 2, 2049, 8)])
+@pytest.mark.parametrize("d,hkv,n,start", [(128, 8, 1000, 5), (64, 2, 300, 0), (128, 2, 2049, 8), (64, 3, 1500, 3),
+                                           (128, 1, 1025, 15), (64, 2, 3001, 0)])
 def test_scatter_of_whole_requests(d, hkv, n, start):
     """Prefill-shaped slots: consecutive slots of scattered blocks."""
     print_case(f"mx4 store in runs d={d} hkv={hkv} n={n} start={start}")
@@ -97,6 +98,32 @@ def test_scatter_of_whole_requests(d, hkv, n, start):
     want = omx.new_pool(nblk, hkv, d)
     omx.scatter(want, k[keep], v[keep], slots[keep])
     assert np.array_equal(pool.cpu().numpy(), want)
+    ko, vo = (torch.empty((n, hkv, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ak.kv_gather_mx4(pool, torch.from_numpy(slots).to(DEV), ko, vo)
+    torch.cuda.synchronize()
+    for got, rows in ((ko, k), (vo, v)):
+        assert np.array_equal(bf16_to_f64(bits(got)), np.where(keep[:, None, None], omx.stored(rows), 0.0))
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_unrelated_slots_in_bulk(d):
+    """More tokens than a small batch has, none beside another, and some in pairs."""
+    print_case(f"mx4 store of unrelated slots d={d}")
+    rng = np.random.default_rng(d)
+    n, hkv = 1300, 2
+    slots = rng.permutation(90 * 16)[:n].astype(np.int32)
+    slots[100:108] = np.arange(8) + 90 * 16                 # one whole half block among them
+    slots[201:217] = np.arange(16) + 91 * 16                # a block
+    k, v = random_rows(n, hkv, d, rng, "any"), random_rows(n, hkv, d, rng, "normal")
+    pool = store(k, v, slots, 92)
+    want = omx.new_pool(92, hkv, d)
+    omx.scatter(want, k, v, slots)
+    finite_bytes_equal(pool, want, k, v, slots)
+    ko, vo = (torch.empty((n, hkv, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ak.kv_gather_mx4(pool, torch.from_numpy(slots).to(DEV), ko, vo)
+    torch.cuda.synchronize()
+    for got, rows in ((ko, k), (vo, v)):
+        assert np.array_equal(bf16_to_f64(bits(got)), omx.stored(rows), equal_nan=True)
 
 
 def test_every_code_rounds_as_defined():
