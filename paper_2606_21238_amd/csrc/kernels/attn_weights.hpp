@@ -76,10 +76,11 @@ __device__ __forceinline__ int wt_chunk(int i, int hg) { return MX4 ? hg * (D / 
 // The weights of 32 columns for this lane's key, of S's 16 registers: register 4 g + j is column cb + 8 g + 4 hg + j.
 template <bool MASKED, class Lse>
 __device__ __forceinline__ float wt_sum(const f32x16_t& s, Lse lse, float scale_log2, int cb, int hg,
-                                        int cmin, int ncols) {
-  float sum[4];
+                                        int cmin, int ncols, int groups = 4) {
+  float sum[4] = {};
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
+    if (g >= groups) break;                          // (uniform) the columns from 8 g on are not there
     const f32x4_t l4 = lse(g);
     float p[4];
 #pragma unroll
@@ -270,7 +271,7 @@ __global__ __launch_bounds__(256, MX4 || D == 64 ? 4 : 3) void attn_weights_stre
     for (int g = 0; g < 4; ++g)
 #pragma unroll
       for (int j = 0; j < 4; ++j) l4[g][j] = __shfl(mine, 8 * g + 4 * hg + j);
-    const int pos0 = rq.P + gd.tok(cb);
+    const int pos0 = rq.P + gd.tok(cb), groups = (min(32, rq.ncols - cb) + 7) / 8;
     for (int sub = first; sub < nsub; sub += by) {
       f32x16_t s;
 #pragma unroll
@@ -284,8 +285,8 @@ __global__ __launch_bounds__(256, MX4 || D == 64 ? 4 : 3) void attn_weights_stre
       const int key = sub * 32 + l32;
       const bool masked = sub * 32 + 31 > pos0 || rq.ncols <= cb;
       auto sums = [&](int g) { return l4[g]; };
-      const float mine32 = masked ? wt_sum<true>(s, sums, scale_log2, cb, hg, first_column(key, rq.P, G), rq.ncols)
-                                  : wt_sum<false>(s, sums, scale_log2, cb, hg, 0, rq.ncols);
+      const float mine32 = masked ? wt_sum<true>(s, sums, scale_log2, cb, hg, first_column(key, rq.P, G), rq.ncols, groups)
+                                  : wt_sum<false>(s, sums, scale_log2, cb, hg, 0, rq.ncols, groups);
       const float total = sum_halves(mine32);
       if (hg == 0 && key < rq.bound) wrow[key] = was + total;
     }
