@@ -324,11 +324,41 @@ def pool_bytes(num_blocks: int, num_kv_heads: int, head_dim: int) -> int:
     return int(lib().arckv_pool_bytes(num_blocks, num_kv_heads, head_dim))
 
 
-def _stream(stream):
-    if stream is not None:
-        return stream
+def _current_stream(index: int | None = None) -> int:
+    """The handle of torch's current stream on a device (None: the current one).  (torch's own way to the
+    handle alone takes 0.1 us, a Stream object 3.)"""
     import torch
-    return torch.cuda.current_stream().cuda_stream
+    index = torch.cuda.current_device() if index is None else index
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream(index).cuda_stream if raw is None else raw(index)
+
+
+def _stream(stream):
+    return _current_stream() if stream is None else stream
+
+
+class _on:
+    """Makes the device of the tensors the current one for a call (they must share it), and gives the call's
+    stream: `stream`, or that device's current one."""
+
+    def __init__(self, stream, *tensors):
+        import torch
+        index = tensors[0].device.index
+        for t in tensors:
+            if t is not None and t.device.index != index:
+                raise ValueError("the tensors of a call must be on one device")
+        self.guard = None if index == torch.cuda.current_device() else torch.cuda.device(index)
+        self.stream, self.index = stream, index
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+        return C.c_void_p(_current_stream(self.index) if self.stream is None else self.stream)
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+        return False
 
 
 def _dev(t, dtype_bits: int | None = None, name: str = "tensor"):
@@ -389,14 +419,16 @@ def _mx4_rows(kv_pool, k, v, slot_mapping):
 
 def kv_scatter_mx4(kv_pool, k_new, v_new, slot_mapping, stream=None):
     """pool[slot[t]] <- (k_new[t], v_new[t]) in 4 bits; kv_pool uint8 [blocks, Hkv, 17 D]."""
-    _lib.check(lib().arckv_kv_scatter_mx4(*_mx4_rows(kv_pool, k_new, v_new, slot_mapping),
-                                          C.c_void_p(_stream(stream))), "arckv_kv_scatter_mx4")
+    args = _mx4_rows(kv_pool, k_new, v_new, slot_mapping)
+    with _on(stream, kv_pool, k_new, v_new, slot_mapping) as st:
+        _lib.check(lib().arckv_kv_scatter_mx4(*args, st), "arckv_kv_scatter_mx4")
 
 
 def kv_gather_mx4(kv_pool, slot_mapping, k_out, v_out, stream=None):
     """(k_out[t], v_out[t]) [n, Hkv, D] <- the values that pool[slot[t]] stands for, bf16."""
-    _lib.check(lib().arckv_kv_gather_mx4(*_mx4_rows(kv_pool, k_out, v_out, slot_mapping),
-                                         C.c_void_p(_stream(stream))), "arckv_kv_gather_mx4")
+    args = _mx4_rows(kv_pool, k_out, v_out, slot_mapping)
+    with _on(stream, kv_pool, k_out, v_out, slot_mapping) as st:
+        _lib.check(lib().arckv_kv_gather_mx4(*args, st), "arckv_kv_gather_mx4")
 
 
 def qkv_rope(x, w_qkv, cu_q, seq_lens, num_q_heads: int, num_kv_heads: int, rope_theta: float,
@@ -539,11 +571,13 @@ def prefill_attention(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work
     lse (optional): fp32 [n_q, Hq], receives log sum_j exp(scale q . K[j]) of every row and head."""
     args = _attention_args(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work, n_work, n_combine,
                            tile_cols, scale)
-    tail = (_workspace(workspace, ws_bytes), int(ws_bytes), C.c_void_p(_stream(stream)))
+    ws = _workspace(workspace, ws_bytes)
     if lse is None:
-        _lib.check(lib().arckv_prefill_attention(*args, *tail), "arckv_prefill_attention")
-    else:
-        _lib.check(lib().arckv_prefill_attention_lse(*args[:4], _lse(lse, q), *args[4:], *tail),
+        _lib.check(lib().arckv_prefill_attention(*args, ws, int(ws_bytes), C.c_void_p(_stream(stream))),
+                   "arckv_prefill_attention")
+        return
+    with _on(stream, k_pool, v_pool, q, out, lse, block_tables, cu_q, seq_lens, work, workspace) as st:
+        _lib.check(lib().arckv_prefill_attention_lse(*args[:4], _lse(lse, q), *args[4:], ws, int(ws_bytes), st),
                    "arckv_prefill_attention_lse")
 
 
@@ -555,9 +589,10 @@ def prefill_attention_mx4(kv_pool, q, out, block_tables, cu_q, seq_lens, work, n
         raise ValueError("kv_pool must be [blocks, Hkv, 17 D] bytes")
     args = _batch_args(q, out, block_tables, cu_q, seq_lens, work, n_work, n_combine, tile_cols, scale,
                        int(kv_pool.shape[0]), hkv)
-    _lib.check(lib().arckv_prefill_attention_mx4(_dev(kv_pool, 8, "kv_pool"), *args[:2], _lse(lse, q), *args[2:],
-                                                 _workspace(workspace, ws_bytes), int(ws_bytes),
-                                                 C.c_void_p(_stream(stream))), "arckv_prefill_attention_mx4")
+    ws = _workspace(workspace, ws_bytes)
+    with _on(stream, kv_pool, q, out, lse, block_tables, cu_q, seq_lens, work, workspace) as st:
+        _lib.check(lib().arckv_prefill_attention_mx4(_dev(kv_pool, 8, "kv_pool"), *args[:2], _lse(lse, q), *args[2:],
+                                                     ws, int(ws_bytes), st), "arckv_prefill_attention_mx4")
 
 
 def prefill_attention_noalloc(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work, n_work: int,
@@ -601,11 +636,11 @@ def attention_weights(k_pool, q, lse, weights, block_tables, cu_q, seq_lens, sca
         raise ValueError("block_tables must be [n_reqs, stride] and cu_q [n_reqs + 1]")
     if lse is None:
         raise ValueError("lse must be what the attention call wrote")
-    _lib.check(lib().arckv_attention_weights(
-        pool, layout, _dev(q, 16, "q"), _lse(lse, q), _dev(block_tables, 32, "block_tables"),
-        int(block_tables.shape[1]), _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), n, n_q, nb, hq, hkv, d,
-        float(scale), _f32(weights, "weights"), int(weights.shape[2]), 1 if accumulate else 0,
-        C.c_void_p(_stream(stream))), "arckv_attention_weights")
+    args = (pool, layout, _dev(q, 16, "q"), _lse(lse, q), _dev(block_tables, 32, "block_tables"),
+            int(block_tables.shape[1]), _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), n, n_q, nb, hq, hkv, d,
+            float(scale), _f32(weights, "weights"), int(weights.shape[2]), 1 if accumulate else 0)
+    with _on(stream, k_pool, q, lse, weights, block_tables, cu_q, seq_lens) as st:
+        _lib.check(lib().arckv_attention_weights(*args, st), "arckv_attention_weights")
 
 
 def evict_select(weights, seq_lens, kept, n_first: int = 0, n_recent: int = 0, kept_weights=None, stream=None):
@@ -617,10 +652,12 @@ def evict_select(weights, seq_lens, kept, n_first: int = 0, n_recent: int = 0, k
         raise ValueError("kept must be [n_reqs, Hkv, keep] and seq_lens [n_reqs]")
     if kept_weights is not None and (kept_weights.dim() != 3 or tuple(kept_weights.shape[:2]) != (n, hkv)):
         raise ValueError("kept_weights must be [n_reqs, Hkv, >= keep]")
-    _lib.check(lib().arckv_evict_select(
-        _f32(weights, "weights"), stride, _dev(seq_lens, 32, "seq_lens"), n, hkv, int(kept.shape[2]), int(n_first),
-        int(n_recent), _dev(kept, 32, "kept"), C.c_void_p(0) if kept_weights is None else _f32(kept_weights, "kept_weights"),
-        0 if kept_weights is None else int(kept_weights.shape[2]), C.c_void_p(_stream(stream))), "arckv_evict_select")
+    args = (_f32(weights, "weights"), stride, _dev(seq_lens, 32, "seq_lens"), n, hkv, int(kept.shape[2]), int(n_first),
+            int(n_recent), _dev(kept, 32, "kept"),
+            C.c_void_p(0) if kept_weights is None else _f32(kept_weights, "kept_weights"),
+            0 if kept_weights is None else int(kept_weights.shape[2]))
+    with _on(stream, weights, seq_lens, kept, kept_weights) as st:
+        _lib.check(lib().arckv_evict_select(*args, st), "arckv_evict_select")
 
 
 def _compact_args(block_tables, kept, dst_tables, nb, hkv, d):
@@ -637,9 +674,10 @@ def kv_compact(k_pool, v_pool, block_tables, kept, dst_tables, stream=None):
     nb, hkv, d = int(k_pool.shape[0]), int(k_pool.shape[1]), int(k_pool.shape[3])
     if tuple(k_pool.shape) != (nb, hkv, 16, d) or tuple(v_pool.shape) != (nb, hkv, d, 16):
         raise ValueError("pools must be [blocks, Hkv, 16, D] (K) and [blocks, Hkv, D, 16] (V)")
-    _lib.check(lib().arckv_kv_compact(_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"),
-                                      *_compact_args(block_tables, kept, dst_tables, nb, hkv, d),
-                                      C.c_void_p(_stream(stream))), "arckv_kv_compact")
+    args = _compact_args(block_tables, kept, dst_tables, nb, hkv, d)
+    with _on(stream, k_pool, v_pool, block_tables, kept, dst_tables) as st:
+        _lib.check(lib().arckv_kv_compact(_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"), *args, st),
+                   "arckv_kv_compact")
 
 
 def kv_compact_mx4(kv_pool, block_tables, kept, dst_tables, stream=None):
@@ -647,6 +685,6 @@ def kv_compact_mx4(kv_pool, block_tables, kept, dst_tables, stream=None):
     nb, hkv, row = (int(x) for x in kv_pool.shape)
     if row % 17 != 0:
         raise ValueError("kv_pool must be [blocks, Hkv, 17 D] bytes")
-    _lib.check(lib().arckv_kv_compact_mx4(_dev(kv_pool, 8, "kv_pool"),
-                                          *_compact_args(block_tables, kept, dst_tables, nb, hkv, row // 17),
-                                          C.c_void_p(_stream(stream))), "arckv_kv_compact_mx4")
+    args = _compact_args(block_tables, kept, dst_tables, nb, hkv, row // 17)
+    with _on(stream, kv_pool, block_tables, kept, dst_tables) as st:
+        _lib.check(lib().arckv_kv_compact_mx4(_dev(kv_pool, 8, "kv_pool"), *args, st), "arckv_kv_compact_mx4")

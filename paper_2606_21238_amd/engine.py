@@ -10,11 +10,12 @@ steps as separate calls.
 
 from __future__ import annotations
 
+import contextlib
 from dataclasses import dataclass
 
 import numpy as np
 
-from . import (BlockCache, BatchPlan, attention_plan, hash_blocks_batch, lib, unpack_prepared)
+from . import (BlockCache, BatchPlan, _current_stream, attention_plan, hash_blocks_batch, lib, unpack_prepared)
 from . import _lib
 
 
@@ -174,9 +175,23 @@ class PrefillEngine:
 
     def _stream(self, stream):
         if stream is None:
-            import torch
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return _current_stream(self.device.index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+    def _call(self, name: str, stream, *args):
+        """A library call on the engine's device (made the current one if it is not) and `stream`."""
+        import torch
+        index = self.device.index
+        if index is None or index == torch.cuda.current_device():
+            _lib.check(getattr(lib(), name)(*args, self._stream(stream)), name)
+        else:
+            with torch.cuda.device(index):
+                _lib.check(getattr(lib(), name)(*args, self._stream(stream)), name)
+
+    @staticmethod
+    def _bad(t, shape, size: int = 2) -> bool:
+        """Whether t is not a contiguous device tensor of that shape and element size."""
+        return tuple(t.shape) != shape or not (t.is_cuda and t.is_contiguous()) or t.element_size() != size
 
     def _copy_meta(self, t: int, n_int: int, ts):
         """Staging buffer t -> its device buffer on stream ts; the event marks the copy done, so
@@ -203,30 +218,26 @@ class PrefillEngine:
 
     def scatter(self, db: DeviceBatch, k_new, v_new, stream=None):
         shape = (db.n_tokens, self.hkv, self.d)
-        if tuple(k_new.shape) != shape or tuple(v_new.shape) != shape or not (
-                k_new.is_contiguous() and v_new.is_contiguous()) or k_new.element_size() != 2:
+        if self._bad(k_new, shape) or self._bad(v_new, shape):
             raise ValueError(f"k_new / v_new must be contiguous 16-bit {shape}")
-        tail = (k_new.data_ptr(), v_new.data_ptr(), db.slot_mapping.data_ptr(), db.n_tokens, self.num_blocks,
-                self.hkv, self.d, self._stream(stream))
+        rows = (k_new.data_ptr(), v_new.data_ptr(), db.slot_mapping.data_ptr(), db.n_tokens, self.num_blocks,
+                self.hkv, self.d)
         if self.kv_format == "mx4":
-            _lib.check(lib().arckv_kv_scatter_mx4(self.kv_pool.data_ptr(), *tail), "arckv_kv_scatter_mx4")
+            self._call("arckv_kv_scatter_mx4", stream, self.kv_pool.data_ptr(), *rows)
         else:
-            _lib.check(lib().arckv_kv_scatter(self.k_pool.data_ptr(), self.v_pool.data_ptr(), *tail),
-                       "arckv_kv_scatter")
+            self._call("arckv_kv_scatter", stream, self.k_pool.data_ptr(), self.v_pool.data_ptr(), *rows)
 
     def gather(self, slots, k_out, v_out, stream=None):
         """The K and V rows [n, Hkv, D] that a 4-bit pool holds for `slots` (device int32 [n]), as bf16."""
         if self.kv_format != "mx4":
             raise ValueError("gather reads a 4-bit pool (kv_format mx4)")
         shape = (int(slots.numel()), self.hkv, self.d)
-        for a in (k_out, v_out):
-            if tuple(a.shape) != shape or not a.is_contiguous() or a.element_size() != 2:
-                raise ValueError(f"k_out / v_out must be contiguous 16-bit {shape}")
-        if slots.element_size() != 4 or not slots.is_contiguous():
-            raise ValueError("slots must be contiguous int32")
-        _lib.check(lib().arckv_kv_gather_mx4(self.kv_pool.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
-                                             slots.data_ptr(), shape[0], self.num_blocks, self.hkv, self.d,
-                                             self._stream(stream)), "arckv_kv_gather_mx4")
+        if self._bad(k_out, shape) or self._bad(v_out, shape):
+            raise ValueError(f"k_out / v_out must be contiguous 16-bit {shape}")
+        if self._bad(slots, tuple(slots.shape), 4):
+            raise ValueError("slots must be contiguous int32 on the device")
+        self._call("arckv_kv_gather_mx4", stream, self.kv_pool.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
+                   slots.data_ptr(), shape[0], self.num_blocks, self.hkv, self.d)
 
     def project(self, db: DeviceBatch, x, w_qkv, q, k_new, v_new, rope_theta: float, stream=None):
         """Q/K/V of the batch's computed tokens from their hidden states x [n_tokens, H]
@@ -281,38 +292,34 @@ class PrefillEngine:
         combine, and after it.  `lse`: optional fp32 [n_tokens, Hq] that receives
         log sum_j exp(scale q . K[j]) of every row and head (for attention_weights)."""
         shape = (db.n_tokens, self.hq, self.d)
-        if tuple(q.shape) != shape or tuple(out.shape) != shape or not (
-                q.is_contiguous() and out.is_contiguous()) or q.element_size() != 2:
+        if self._bad(q, shape) or self._bad(out, shape):
             raise ValueError(f"q / out must be contiguous 16-bit {shape}")
         if lse is not None:
             self._check_lse(db, lse)
         args = (db.block_tables.data_ptr(), int(db.block_tables.shape[1]), db.cu_q.data_ptr(), db.seq_lens.data_ptr(),
                 db.plan.n_reqs, db.n_tokens, self.num_blocks, db.work_ptr, db.n_work, db.n_combine, db.tile_cols,
-                self.hq, self.hkv, self.d, self.scale, self._ws.data_ptr() if db.ws_bytes else None, db.ws_bytes,
-                self._stream(stream))
+                self.hq, self.hkv, self.d, self.scale, self._ws.data_ptr() if db.ws_bytes else None, db.ws_bytes)
         qo = (q.data_ptr(), out.data_ptr())
         if self.kv_format == "mx4":
             if events is not None:
                 raise ValueError("events are recorded around the bf16 kernels only")
-            _lib.check(lib().arckv_prefill_attention_mx4(self.kv_pool.data_ptr(), *qo,
-                                                         None if lse is None else lse.data_ptr(), *args),
-                       "arckv_prefill_attention_mx4")
+            self._call("arckv_prefill_attention_mx4", stream, self.kv_pool.data_ptr(), *qo,
+                       None if lse is None else lse.data_ptr(), *args)
             return
         pools = (self.k_pool.data_ptr(), self.v_pool.data_ptr())
         if events is not None:
             if lse is not None:
                 raise ValueError("the timed call writes no lse")
-            _lib.check(lib().arckv_prefill_attention_timed(*pools, *qo, *args, *(e.cuda_event for e in events)),
+            _lib.check(lib().arckv_prefill_attention_timed(*pools, *qo, *args, self._stream(stream),
+                                                           *(e.cuda_event for e in events)),
                        "arckv_prefill_attention_timed")
         elif lse is not None:
-            _lib.check(lib().arckv_prefill_attention_lse(*pools, *qo, lse.data_ptr(), *args),
-                       "arckv_prefill_attention_lse")
+            self._call("arckv_prefill_attention_lse", stream, *pools, *qo, lse.data_ptr(), *args)
         else:
-            _lib.check(lib().arckv_prefill_attention(*pools, *qo, *args), "arckv_prefill_attention")
+            self._call("arckv_prefill_attention", stream, *pools, *qo, *args)
 
     def _check_lse(self, db: DeviceBatch, lse):
-        if tuple(lse.shape) != (db.n_tokens, self.hq) or not lse.is_contiguous() or lse.element_size() != 4 \
-                or not lse.is_floating_point():
+        if self._bad(lse, (db.n_tokens, self.hq), 4) or not lse.is_floating_point():
             raise ValueError(f"lse must be contiguous fp32 {(db.n_tokens, self.hq)}")
 
     def attention_weights(self, db: DeviceBatch, q, lse, weights, accumulate: bool = True, stream=None):
@@ -320,22 +327,21 @@ class PrefillEngine:
         receives from the batch's rows through KV head h; lse from attention(lse=).  weights: fp32
         [n_reqs, Hkv, stride]; tokens past the stride are left out."""
         shape = (db.n_tokens, self.hq, self.d)
-        if tuple(q.shape) != shape or not q.is_contiguous() or q.element_size() != 2:
+        if self._bad(q, shape):
             raise ValueError(f"q must be contiguous 16-bit {shape}")
         self._check_lse(db, lse)
         n = db.plan.n_reqs
         self._check_weights(n, weights)
         mx4 = self.kv_format == "mx4"
-        _lib.check(lib().arckv_attention_weights(
-            (self.kv_pool if mx4 else self.k_pool).data_ptr(), _lib.LAYOUT_MX4 if mx4 else _lib.LAYOUT_V1, q.data_ptr(),
-            lse.data_ptr(), db.block_tables.data_ptr(), int(db.block_tables.shape[1]), db.cu_q.data_ptr(),
-            db.seq_lens.data_ptr(), n, db.n_tokens, self.num_blocks, self.hq, self.hkv, self.d, self.scale,
-            weights.data_ptr(), int(weights.shape[2]), 1 if accumulate else 0, self._stream(stream)),
-            "arckv_attention_weights")
+        self._call("arckv_attention_weights", stream, (self.kv_pool if mx4 else self.k_pool).data_ptr(),
+                   _lib.LAYOUT_MX4 if mx4 else _lib.LAYOUT_V1, q.data_ptr(), lse.data_ptr(), db.block_tables.data_ptr(),
+                   int(db.block_tables.shape[1]), db.cu_q.data_ptr(), db.seq_lens.data_ptr(), n, db.n_tokens,
+                   self.num_blocks, self.hq, self.hkv, self.d, self.scale, weights.data_ptr(), int(weights.shape[2]),
+                   1 if accumulate else 0)
 
     def _check_weights(self, n: int, weights):
-        if weights.dim() != 3 or tuple(weights.shape[:2]) != (n, self.hkv) or not weights.is_contiguous() \
-                or weights.element_size() != 4 or not weights.is_floating_point():
+        if weights.dim() != 3 or self._bad(weights, (n, self.hkv, int(weights.shape[2])), 4) or \
+                not weights.is_floating_point():
             raise ValueError(f"weights must be contiguous fp32 [{n}, {self.hkv}, stride]")
 
     def evict(self, db: DeviceBatch, weights, keep: int, dst_tables, n_first: int = 0, n_recent: int = 0, stream=None):
@@ -365,24 +371,20 @@ class PrefillEngine:
             # (entries of -1 look at the spare last place)
             if plan.block_tables.size and plan.block_tables.max() >= lo and uses[plan.block_tables].any():
                 raise ValueError("dst_tables names a block of the batch")
-        ts = self._torch_stream(stream)
-        with torch.cuda.stream(ts):
-            host = torch.empty(dst.shape, dtype=torch.int32, pin_memory=True)
-            host.numpy()[:] = dst
+        host = torch.empty(dst.shape, dtype=torch.int32, pin_memory=True)
+        host.numpy()[:] = dst
+        with contextlib.nullcontext() if stream is None else torch.cuda.stream(self._torch_stream(stream)):
             dev = host.to(self.device, non_blocking=True)
             kept = torch.empty((n, self.hkv, keep), dtype=torch.int32, device=self.device)
             kept_weights = torch.empty((n, self.hkv, keep), dtype=torch.float32, device=self.device)
-        raw = self._stream(stream)
-        _lib.check(lib().arckv_evict_select(weights.data_ptr(), int(weights.shape[2]), db.seq_lens.data_ptr(), n,
-                                            self.hkv, keep, n_first, n_recent, kept.data_ptr(),
-                                            kept_weights.data_ptr(), keep, raw), "arckv_evict_select")
+        self._call("arckv_evict_select", stream, weights.data_ptr(), int(weights.shape[2]), db.seq_lens.data_ptr(), n,
+                   self.hkv, keep, n_first, n_recent, kept.data_ptr(), kept_weights.data_ptr(), keep)
         args = (db.block_tables.data_ptr(), int(db.block_tables.shape[1]), kept.data_ptr(), keep, dev.data_ptr(),
-                int(dst.shape[1]), n, self.num_blocks, self.hkv, self.d, raw)
+                int(dst.shape[1]), n, self.num_blocks, self.hkv, self.d)
         if self.kv_format == "mx4":
-            _lib.check(lib().arckv_kv_compact_mx4(self.kv_pool.data_ptr(), *args), "arckv_kv_compact_mx4")
+            self._call("arckv_kv_compact_mx4", stream, self.kv_pool.data_ptr(), *args)
         else:
-            _lib.check(lib().arckv_kv_compact(self.k_pool.data_ptr(), self.v_pool.data_ptr(), *args),
-                       "arckv_kv_compact")
+            self._call("arckv_kv_compact", stream, self.k_pool.data_ptr(), self.v_pool.data_ptr(), *args)
         return kept, kept_weights
 
     def step(self, token_lists, qkv_for_plan, stream=None, release: bool = True):
