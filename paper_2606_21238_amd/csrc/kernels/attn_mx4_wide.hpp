@@ -247,11 +247,12 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
   // ---- M phase: V^T P, then K Q^T of the next tile, with the conversion of tile j + 2 between ----------
   // Bytes of tile j + 2, and of tile j + 3 on their way.  D = 64 has registers for one of them: its load
   // goes out once the conversion is through.
+  // (Two sets that change places, in steps of two: a copy from one to the other would wait for the load.)
   constexpr bool kAhead = D == 128;
   Raw raw, next;
   // Byte offsets of the stages of tiles j, j + 1 and j + 2 of the step being run.
   int st0 = 0, st1 = 2 * TILE, st2 = 4 * TILE;
-  auto m_phase = [&]() {
+  auto m_phase = [&](Raw& cur, Raw& nxt) {
     // The lane's operand of V: rows l32 + 32 md of block sp, its half.  Of K: row pi(l32) + 32 mb, chunk 2 ks + hg
     // swizzled: stages and rows start at multiples of 256 (D = 64: 128) bytes, so chunks 2 ks on are an
     // exclusive or away.
@@ -266,7 +267,10 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
       return *reinterpret_cast<const bf16x8_t*>(smem + (ka ^ (ks * 32)) + mb * (64 * D));
     };
     constexpr int EVERY = NOP / (PARTS + 2);
-    if constexpr (kAhead) load(__builtin_amdgcn_readfirstlane(next_v), next);
+    if constexpr (kAhead) {
+      load(__builtin_amdgcn_readfirstlane(next_v), nxt);
+      __builtin_amdgcn_sched_barrier(0);   // out before the MFMAs, not sunk behind them
+    }
     bf16x8_t opv[NOP];
 #pragma unroll
     for (int n = 0; n < PD; ++n) opv[n] = op_at(n);
@@ -282,8 +286,8 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
         sacc[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(opv[n], qf[ks], ks == 0 ? f32x16_t{} : sacc[mb], 0, 0, 0);
       }
       if (n % EVERY == EVERY / 2) {
-        if (n / EVERY < PARTS) convert(raw, st2, n / EVERY);
-        else if (n / EVERY == PARTS && !kAhead) load(__builtin_amdgcn_readfirstlane(next_v), raw);
+        if (n / EVERY < PARTS) convert(cur, st2, n / EVERY);
+        else if (n / EVERY == PARTS && !kAhead) load(__builtin_amdgcn_readfirstlane(next_v), cur);
       }
     }
     // keep the operand reads PD ahead: DS reads, then one MFMA and one read at a time
@@ -372,14 +376,13 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     s_first();                                           // M(-1)
     pin_m();
     barrier();
-    auto step = [&](int j, auto masked) {
+    auto step = [&](int j, auto masked, Raw& cur, Raw& nxt) {
       v_phase(j, masked);
       pin_v();
       barrier();
       // past the key range the table gives block 0 and the conversion writes a stage nobody reads
-      if (tile_masked(j + 2)) mask_v(raw, j + 2);
-      m_phase();
-      if constexpr (kAhead) raw = next;
+      if (tile_masked(j + 2)) mask_v(cur, j + 2);
+      m_phase(cur, nxt);
       const int st3 = st0;
       st0 = st1;
       st1 = st2;
@@ -399,8 +402,24 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     }
     int j = 0;
     if constexpr (D == 128) asm volatile(".p2align 5");
-    for (; j < n_plain; ++j) step(j, std::false_type{});
-    for (; j < ntiles; ++j) step(j, std::true_type{});
+    if constexpr (kAhead) {
+      for (; j + 1 < n_plain; j += 2) {
+        step(j, std::false_type{}, raw, next);
+        step(j + 1, std::false_type{}, next, raw);
+      }
+      if (j < n_plain) {
+        step(j, std::false_type{}, raw, next);
+        raw = next;
+        ++j;
+      }
+      for (; j < ntiles; ++j) {
+        step(j, std::true_type{}, raw, next);
+        raw = next;
+      }
+    } else {
+      for (; j < n_plain; ++j) step(j, std::false_type{}, raw, raw);
+      for (; j < ntiles; ++j) step(j, std::true_type{}, raw, raw);
+    }
   }
 
   // ---- epilogue: O^T register r of block md holds dim 32 md + 8 (r / 4) + 4 hg + r % 4 ------
