@@ -111,12 +111,14 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     const int b = tile * (kBK / 16) + wblk;                          // relative to b_lo
     next_v = b < n_tbl ? tbl[b] : 0;
   };
-  auto load = [&](int32_t ph, Raw& x) {
+  // one block of one head as a buffer: its address stays in scalar registers
+  auto block_at = [&](int32_t ph) {
     ARCKV_CHECK_WAVE(ph < 0 || static_cast<uint32_t>(ph) >= nb32, ARCKV_CHECK_BLOCK);
     // wave-uniform; an entry out of range reads block 0
     const int32_t pb = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(ph) >= nb32 ? 0 : ph);
-    uint8_t* base = const_cast<uint8_t*>(pool) + (static_cast<int64_t>(pb) * blk_stride + head);
-    // one block of one head as a buffer: its address stays in scalar registers
+    return const_cast<uint8_t*>(pool) + (static_cast<int64_t>(pb) * blk_stride + head);
+  };
+  auto load = [&](uint8_t* base, Raw& x) {
     const __amdgpu_buffer_rsrc_t buf = __builtin_amdgcn_make_buffer_rsrc(base, 0, L4::kBytes, 0x00027000);
     const Place p = place(D == 64);
     const uint32_t c_ofs = p.piece * (4 * NB);           // of the codes of either
@@ -252,7 +254,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
   Raw raw, next;
   // Byte offsets of the stages of tiles j, j + 1 and j + 2 of the step being run.
   int st0 = 0, st1 = 2 * TILE, st2 = 4 * TILE;
-  auto m_phase = [&](Raw& cur, Raw& nxt) {
+  auto m_phase = [&](Raw& cur, Raw& nxt, uint8_t* block) {
     // The lane's operand of V: rows l32 + 32 md of block sp, its half.  Of K: row pi(l32) + 32 mb, chunk 2 ks + hg
     // swizzled: stages and rows start at multiples of 256 (D = 64: 128) bytes, so chunks 2 ks on are an
     // exclusive or away.
@@ -267,10 +269,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
       return *reinterpret_cast<const bf16x8_t*>(smem + (ka ^ (ks * 32)) + mb * (64 * D));
     };
     constexpr int EVERY = NOP / (PARTS + 2);
-    if constexpr (kAhead) {
-      load(__builtin_amdgcn_readfirstlane(next_v), nxt);
-      __builtin_amdgcn_sched_barrier(0);   // out before the MFMAs, not sunk behind them
-    }
+    if constexpr (kAhead) load(block, nxt);
     bf16x8_t opv[NOP];
 #pragma unroll
     for (int n = 0; n < PD; ++n) opv[n] = op_at(n);
@@ -287,7 +286,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
       }
       if (n % EVERY == EVERY / 2) {
         if (n / EVERY < PARTS) convert(cur, st2, n / EVERY);
-        else if (n / EVERY == PARTS && !kAhead) load(__builtin_amdgcn_readfirstlane(next_v), cur);
+        else if (n / EVERY == PARTS && !kAhead) load(block_at(__builtin_amdgcn_readfirstlane(next_v)), cur);
       }
     }
     // keep the operand reads PD ahead: DS reads, then one MFMA and one read at a time
@@ -296,6 +295,8 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     for (int n = 0; n < NOP - PD; ++n) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      // the loads of tile j + 3 after the first MFMAs: at the end of the phase they would come late
+      if (kAhead && n < 4) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
     }
     __builtin_amdgcn_sched_group_barrier(0x008, PD, 0);
   };
@@ -351,8 +352,8 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
       else load_lds16(src, (lds_void*)(qst + i * 1024));
     }
     auto first = [&](int t) { return b_lo + t * (kBK / 16) + wblk < nblk ? first_ph[t] : 0; };
-    load(first(0), raw);
-    load(first(1), raw1);
+    load(block_at(first(0)), raw);
+    load(block_at(first(1)), raw1);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
   }
   __syncthreads();                  // nan_key is set, table and queries are here
@@ -369,7 +370,7 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     barrier();                                           // every wave has its queries
 #pragma unroll
     for (int p = 0; p < PARTS; ++p) convert(raw1, st1, p);
-    load(__builtin_amdgcn_readfirstlane(next_v), raw);
+    load(block_at(__builtin_amdgcn_readfirstlane(next_v)), raw);
     fetch_next(3);
     barrier();                                           // tiles 0 and 1 are there
     if (grp == 1) barrier();                             // half step 0: group 1 waits
@@ -377,12 +378,14 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     pin_m();
     barrier();
     auto step = [&](int j, auto masked, Raw& cur, Raw& nxt) {
+      uint8_t* block = nullptr;
+      if constexpr (kAhead) block = block_at(__builtin_amdgcn_readfirstlane(next_v));    // of tile j + 3
       v_phase(j, masked);
       pin_v();
       barrier();
       // past the key range the table gives block 0 and the conversion writes a stage nobody reads
       if (tile_masked(j + 2)) mask_v(cur, j + 2);
-      m_phase(cur, nxt);
+      m_phase(cur, nxt, block);
       const int st3 = st0;
       st0 = st1;
       st1 = st2;
