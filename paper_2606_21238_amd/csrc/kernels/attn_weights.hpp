@@ -158,22 +158,19 @@ __global__ __launch_bounds__(512, 4) void attn_weights_kernel(
     const int64_t wg_key = static_cast<int64_t>(sub) * 32;
     const int key = sub * 32 + kw * 32 + l32;
     const bool mine = kw < step;                                             // a subtile of its own
-    bf16x8_t kf[KS];
-    {
-      WtKey<D, MX4> raw;
-      raw.load(pool, rq.bt[min(key, rq.bound - 1) >> 4], num_blocks, hkv, kvh, key, hg);
-#pragma unroll
-      for (int i = 0; i < KS; ++i) kf[i] = raw.step(i);
-    }
+    // keys and the first columns are asked for together
+    WtKey<D, MX4> raw;
+    raw.load(pool, rq.bt[min(key, rq.bound - 1) >> 4], num_blocks, hkv, kvh, key, hg);
     const int c_lo = min(first_column(wg_key, rq.P, G), rq.ncols) / kWtCols * kWtCols;
     const int cmin = first_column(key, rq.P, G);
     const int all_see = first_column(wg_key + kw * 32 + 31, rq.P, G);   // columns from here on see every key of the wave
     // sums of the tiles 0, 1, 2, 3 modulo 4 (of which a wave has every CS-th), added up in one order whoever has them
     float acc[TILES] = {};
-    if (c_lo < rq.ncols) {
-      fetch(c_lo, 0);
-      landed(0);
-    }
+    if (c_lo < rq.ncols) fetch(c_lo, 0);
+    bf16x8_t kf[KS];
+#pragma unroll
+    for (int i = 0; i < KS; ++i) kf[i] = raw.step(i);
+    if (c_lo < rq.ncols) landed(0);
     __syncthreads();
     int buf = 0;
     for (int c0 = c_lo; c0 < rq.ncols; c0 += kWtCols, buf ^= 1) {

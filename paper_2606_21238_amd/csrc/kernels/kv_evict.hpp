@@ -34,7 +34,9 @@ template <int KEYS>
 __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_kernel(
     const float* __restrict__ weights, int64_t w_stride, const int32_t* __restrict__ seq_lens, int hkv, int keep,
     int n_first, int n_recent, int32_t* __restrict__ kept, float* __restrict__ kept_weights, int64_t kw_stride) {
-  __shared__ int hist[4096];
+  // one histogram for every kCopies-th lane: fewer lanes of a wave meet at an address
+  constexpr int kCopies = KEYS > 16 ? 4 : 2;
+  __shared__ int hist[kCopies][4096];
   __shared__ int wave_sum[kSelWaves], wave_take[kSelWaves], wave_equal[kSelWaves];
   __shared__ int pick, above;
   const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.x, r = blockIdx.y;
@@ -62,16 +64,16 @@ __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_k
       const int i0 = from + t * kTile, n = min(run - t * kTile, kTile);
       if (have != t) {
 #pragma unroll
-        for (int u = 0; u < KEYS; u += 4) {
+        for (int u = 0; u < KEYS; u += 16) {
           if (64 * u >= n) break;
-          float x[4];
+          float x[16];                     // 16 loads in flight
 #pragma unroll
-          for (int v = 0; v < 4; ++v) {
+          for (int v = 0; v < 16; ++v) {
             const int i = i0 + 64 * (u + v) + lane;
             x[v] = i < to ? w[i] : 0.f;
           }
 #pragma unroll
-          for (int v = 0; v < 4; ++v) key[u + v] = i0 + 64 * (u + v) + lane < to ? weight_key(x[v]) : 0;
+          for (int v = 0; v < 16; ++v) key[u + v] = i0 + 64 * (u + v) + lane < to ? weight_key(x[v]) : 0;
         }
         have = t;
       }
@@ -98,11 +100,13 @@ __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_k
       const int bins = 1 << kBits[pass];
 #pragma unroll
       for (int i = 0; i < kPer; ++i)
-        if (i * kSelThreads < bins) hist[i * kSelThreads + tid] = 0;
+        if (i * kSelThreads < bins)
+#pragma unroll
+          for (int v = 0; v < kCopies; ++v) hist[v][i * kSelThreads + tid] = 0;
       __syncthreads();
       auto count = [&](uint32_t k) {
         if (pass == 0 || (k >> (shift + kBits[pass])) == (prefix >> (shift + kBits[pass])))
-          atomicAdd(&hist[(k >> shift) & (bins - 1)], 1);
+          atomicAdd(&hist[lane % kCopies][(k >> shift) & (bins - 1)], 1);
       };
       // (the key 0 of positions behind an inner run only adds to the lowest digit, where it decides nothing)
       if (inner) each([&](int, uint32_t k) { count(k); });
@@ -113,7 +117,9 @@ __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_k
       int c[kPer], sum = 0;
 #pragma unroll
       for (int i = 0; i < kPer; ++i) {
-        c[i] = i < per ? hist[bins - 1 - (per * tid + i)] : 0;
+        c[i] = 0;
+#pragma unroll
+        for (int v = 0; v < kCopies; ++v) c[i] += i < per ? hist[v][bins - 1 - (per * tid + i)] : 0;
         sum += c[i];
       }
       int upto = sum;
