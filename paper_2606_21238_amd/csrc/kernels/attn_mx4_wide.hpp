@@ -137,9 +137,10 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     }
     x.ks = __builtin_amdgcn_raw_buffer_load_b8(buf, ks_ofs, 0, 0);
   };
-  // Before a masked tile is converted: V of the keys past the prompt's end may be anything, and V of a
-  // key that only later columns see may be NaN.  Neither may meet a weight of zero, so their scales
-  // are replaced; NaN comes back at the end for the columns that see the first such key.
+  // Before a masked tile is converted: V of the keys past the item's last (the prompt's end, or block 0 past
+  // the last tile) may be anything, and V of a key that only later columns see may be NaN.  Neither may
+  // meet a weight of zero, so their scales are replaced; NaN comes back at the end for the columns that
+  // see the first such key.
   auto mask_v = [&](Raw& x, int tile) {
     const Place p = place(D == 64);
     int first = INT32_MAX;
@@ -147,9 +148,9 @@ __global__ __launch_bounds__(512, D == 64 ? 4 : 1) void mx4_attn_wide_kernel(
     for (int k = 4 * NB - 1; k >= 0; --k) {
       const int key = kv_lo + tile * kBK + wblk * 16 + p.vhalf * 8 + p.vquad * 4 + k, sh = 8 * (k & 3);
       uint32_t& s = x.vs[k / 4];
-      const bool nan = ((s >> sh) & 255u) == mx4::kNanScale && key < L;
+      const bool nan = ((s >> sh) & 255u) == mx4::kNanScale && key < kv_hi;
       first = nan ? key : first;
-      if (nan || key >= L) s = (s & ~(255u << sh)) | (127u << sh);
+      if (nan || key >= kv_hi) s = (s & ~(255u << sh)) | (127u << sh);
     }
     if (first != INT32_MAX) atomicMin(&nan_key[p.vpair / 16], first);
   };

@@ -186,3 +186,18 @@ def test_outputs_of_idle_rows_stay():
     out, lse, _ = attend(b, q=q)
     n = len(b["q"])
     assert torch.isnan(out[n:]).all() and torch.isnan(lse[n:]).all() and torch.isfinite(out[:n]).all()
+
+
+@pytest.mark.parametrize("num_cus", [64, 256, 100000])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("reqs", [[(567, 88)], [(753, 69), (747, 283)], [(1918, 195)]])
+def test_block_0_of_nobody_reaches_nobody(reqs, d, num_cus):
+    """Tiles cut inside the keys that only some of their columns see, and a block 0 of NaN that no table names:
+    what is read of it past a cut must not count."""
+    for heads in (2, 8):
+        print_case(f"mx4 block 0 of NaN {reqs} heads={heads} d={d} num_cus={num_cus}")
+        b = make_batch(reqs, heads, heads, d, seed=110)
+        b["pool"] = (torch.cat([torch.full_like(b["pool"][0][:1], 0xFF), b["pool"][0]]),)
+        b["bt"] = np.where(b["bt"] >= 0, b["bt"] + 1, -1).astype(np.int32)
+        out, lse, _ = attend(b, num_cus)
+        check_out(b, out, lse, reference(b), f"heads {heads}")
