@@ -110,7 +110,7 @@ __global__ __launch_bounds__(512, 4) void attn_weights_kernel(
     const uint8_t* __restrict__ pool, const uint16_t* __restrict__ q, const float* __restrict__ lse,
     const int32_t* __restrict__ block_tables, int bt_stride, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ seq_lens, int64_t n_q, int64_t num_blocks, int hq, int hkv, GroupDiv gd, float scale_log2,
-    float* __restrict__ weights, int64_t w_stride, int accumulate, int n_split) {
+    float* __restrict__ weights, int64_t w_stride, int accumulate, int n_split, int cols_from, int cols_to) {
   constexpr int kThreads = 512, KS = D / 16, TILES = kWtCols / 32;
   constexpr int kRowBytes = D * 2, kChunkBytes = kWtCols * kRowBytes;
   constexpr int NLD = kChunkBytes / (kThreads * 16);      // 16-byte loads of a thread for a chunk
@@ -122,6 +122,7 @@ __global__ __launch_bounds__(512, 4) void attn_weights_kernel(
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int kvh = blockIdx.x % hkv, r = blockIdx.y, G = static_cast<int>(gd.g);
   const WtReq rq = wt_request(r, block_tables, bt_stride, cu_q, seq_lens, n_q, G, w_stride);
+  if (rq.ncols < cols_from || rq.ncols > cols_to) return;    // of the other kernel's
   float* const wrow = weights + (static_cast<int64_t>(r) * hkv + kvh) * w_stride;
 
   // Rows of q straight into LDS, chunk x of row c at x ^ fk(c); columns past the last load row 0, never used.
@@ -232,12 +233,13 @@ __global__ __launch_bounds__(256, MX4 || D == 64 ? 4 : 3) void attn_weights_stre
     const uint8_t* __restrict__ pool, const uint16_t* __restrict__ q, const float* __restrict__ lse,
     const int32_t* __restrict__ block_tables, int bt_stride, const int32_t* __restrict__ cu_q,
     const int32_t* __restrict__ seq_lens, int64_t n_q, int64_t num_blocks, int hq, int hkv, GroupDiv gd, float scale_log2,
-    float* __restrict__ weights, int64_t w_stride, int accumulate, int n_split) {
+    float* __restrict__ weights, int64_t w_stride, int accumulate, int n_split, int cols_from, int cols_to) {
   constexpr int KS = D / 16;
   const int lane = threadIdx.x & 63, l32 = lane & 31, hg = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = blockIdx.x % hkv, r = blockIdx.y, G = static_cast<int>(gd.g);
   const WtReq rq = wt_request(r, block_tables, bt_stride, cu_q, seq_lens, n_q, G, w_stride);
+  if (rq.ncols < cols_from || rq.ncols > cols_to) return;    // of the other kernel's
   float* const wrow = weights + (static_cast<int64_t>(r) * hkv + kvh) * w_stride;
   const int first = blockIdx.x / hkv * 4 + wave, by = 4 * n_split, nsub = (rq.bound + 31) / 32;
   if (first >= nsub) return;
@@ -317,26 +319,51 @@ extern "C" int32_t arckv_attention_weights(const void* k_pool, int32_t layout, c
   const int64_t pairs = static_cast<int64_t>(n_reqs) * num_kv_heads;
   auto* st = static_cast<hipStream_t>(stream);
   const GroupDiv gd{static_cast<uint32_t>(G), G == 1 ? 0 : static_cast<uint32_t>(((1ull << 32) + G - 1) / G)};
-  // work-groups of `per` keys for each (request, KV head): about `want` in all, no more than its keys need
-  auto split = [&](int64_t per, int64_t want) {
-    return static_cast<int>(std::max<int64_t>(1, std::min((keys + per - 1) / per, (want + pairs - 1) / pairs)));
+  // work-groups for each (request, KV head): about `want` in all, at least `least` to a pair, each with `per` keys
+  // or more
+  auto split = [&](int64_t per, int64_t want, int64_t least) {
+    return static_cast<int>(
+        std::max<int64_t>(1, std::min((keys + per - 1) / per, std::max(least, (want + pairs - 1) / pairs))));
   };
-#define ARCKV_WEIGHTS(KERNEL, THREADS, PER, WANT)                                                              \
+#define ARCKV_WEIGHTS(KERNEL, THREADS, PER, WANT, LEAST, FROM, TO)                                             \
   do {                                                                                                         \
-    const int ns = split(PER, WANT);                                                                           \
+    const int ns = split(PER, WANT, LEAST);                                                                    \
     hipLaunchKernelGGL((KERNEL), dim3(static_cast<unsigned>(ns) * num_kv_heads, n_reqs), dim3(THREADS), 0, st, \
                        static_cast<const uint8_t*>(k_pool), static_cast<const uint16_t*>(q), lse, block_tables, \
                        bt_stride, cu_q, seq_lens, n_q, num_blocks, num_q_heads, num_kv_heads, gd,              \
-                       scale * 1.4426950408889634f, weights, w_stride, accumulate, ns);                        \
+                       scale * 1.4426950408889634f, weights, w_stride, accumulate, ns, FROM, TO);              \
   } while (0)
-#define ARCKV_WEIGHTS_DM(DD, MM)                                                                     \
-  do {                                                                                               \
-    if (few) ARCKV_WEIGHTS((attn_weights_stream_kernel<DD, MM>), 256, 128, 4096);                    \
-    else if (any) ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, true>), 512, 64, 512);                  \
-    else ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, false>), 512, 64, 512);                          \
-  } while (0)
+  // Which kernel takes a request.  Up to 32 columns (bf16) or 64 (4 bits) its keys may stream past them: a second
+  // pass over bf16 keys costs more than what the other kernel's start does.  Streaming and stationary keys at 64
+  // requests of 2000, 32 / 8 heads: 4 columns 44 and 52 us (bf16), 17 and 34 (4 bits); 32: 45 and 50, 20 and 30;
+  // 48: 75 and 55, 31 and 38; 64: 76 and 55, 33 and 36; 128: 136 and 67, 59 and 51.  A batch of so few on average
+  // streams; requests over the limit, which there may be where some have several rows, are a second launch's.
+  const int limit = layout == ARCKV_LAYOUT_MX4 ? 64 : 32;
+  const bool few = n_q * G <= static_cast<int64_t>(n_reqs) * limit;
+  const bool mixed = few && n_q > n_reqs && n_q * G > limit;
   const bool any = reinterpret_cast<uintptr_t>(q) % 16 != 0;
-  const bool few = n_q * G <= static_cast<int64_t>(n_reqs) * 32;
+  const int stream_to = mixed ? limit : INT32_MAX, stay_from = mixed ? limit + 1 : INT32_MIN;
+  // Streaming: one round of the 1024 work-groups that fit at once, at least two to a pair and one for every 2048 keys
+  // that a request may have, which is what its longest request takes (64 requests of 2000 at 4 bits, about 1024, 2048
+  // and 4096 work-groups in all: 17, 19 and 21 us; of 8192: 65, 68 and 71; 256 ragged ones up to 3400, one and two to a
+  // pair: 84 and 75; 64 lognormal ones up to 12000, two and seven: 82 and 33); bf16, whose keys are the bound, two
+  // rounds (8 requests of 8000, 32 columns, 2048 and 4096: 28 and 34; 16 ragged ones up to 12000, 1024, 2048 and 4096:
+  // 57, 51 and 49).
+  // Stationary: about 512 (8 questions of 128 on 8192, 512, 1024 and 2048: 129, 141 and 146 us), but up to 4 to a pair
+  // where its keys are over 1024 each, for one request may have most of the rows (64 requests of 2600, one of
+  // them with 512 rows: 437 and 218 us, at the price of 73 and 79 us for 64 equal ones of 64 rows, 16 / 16 heads of
+  // 64); beside a streaming launch 8 (one of 128 rows among 63 of one: 44 us, and 134 where it streams too; the
+  // second launch costs 3 us where it finds no request).
+  const int64_t least = std::max<int64_t>(2, (keys + 2047) / 2048);
+  const int64_t least_stay = mixed ? 8 : std::min<int64_t>(4, (keys + 1023) / 1024);
+#define ARCKV_WEIGHTS_DM(DD, MM)                                                                              \
+  do {                                                                                                        \
+    if (few) ARCKV_WEIGHTS((attn_weights_stream_kernel<DD, MM>), 256, 128, MM ? 1024 : 2048, least, INT32_MIN, stream_to); \
+    if (!few || mixed) {                                                                                      \
+      if (any) ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, true>), 512, 64, 512, least_stay, stay_from, INT32_MAX);     \
+      else ARCKV_WEIGHTS((attn_weights_kernel<DD, MM, false>), 512, 64, 512, least_stay, stay_from, INT32_MAX);        \
+    }                                                                                                         \
+  } while (0)
   if (head_dim == 64) {
     if (layout == ARCKV_LAYOUT_MX4) ARCKV_WEIGHTS_DM(64, true); else ARCKV_WEIGHTS_DM(64, false);
   } else {

@@ -5,10 +5,15 @@
 // among equals.  One work-group finds the weight of the last one to stay by its digits from the
 // top, 12, 10 and 10 bits, each from a histogram in LDS (of the keys that share the digits before; 12
 // bits first, because 8, the sign and most of the exponent, put most of the keys into a few bins, where
-// additions wait for each other: 74 us for 32 rows of 32768, and XXX), then writes the kept positions in order.
+// additions wait for each other: 74 us for 32 rows of 32768, and 26), then writes the kept positions in order.
+// What bounds it is that one work-group has a row: its read (128 KB at 32768), three passes of LDS additions
+// and the barriers between, 24 to 26 us there; 512 ragged rows of up to 4096, two to a unit: 20 us.
 // kv_compact: the kept tokens' K and V into other blocks, position i of the result from position
 // kept[i]; a head's tokens move on their own, so the same slot may hold another token for another
-// head.  A work-group writes one block of one head.
+// head.  A work-group writes one block of one head.  The bound is the lines it reads, not the tokens: V has a token
+// every 32 bytes (4 bits: every 8), so of 1 token kept in 2 nearly every line of V comes in, and half of
+// K's.  64 requests of about 2600 down to 1024, 8 heads of 128: 93 us, 505 MB at 5.4 TB/s.  4 requests of 32768
+// down to 8192 at 4 bits: 27.5 us.
 #pragma once
 
 #include "mx4.hpp"
@@ -34,7 +39,8 @@ template <int KEYS>
 __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_kernel(
     const float* __restrict__ weights, int64_t w_stride, const int32_t* __restrict__ seq_lens, int hkv, int keep,
     int n_first, int n_recent, int32_t* __restrict__ kept, float* __restrict__ kept_weights, int64_t kw_stride) {
-  // one histogram for every kCopies-th lane: fewer lanes of a wave meet at an address
+  // one histogram for every kCopies-th lane: fewer lanes of a wave meet at an address (one for all of uniform
+  // weights, which meet least: 25.0 against 24.5 us for 32 rows of 32768, 26.2 against 25.2 for 1024 of 2600)
   constexpr int kCopies = KEYS > 16 ? 4 : 2;
   __shared__ int hist[kCopies][4096];
   __shared__ int wave_sum[kSelWaves], wave_take[kSelWaves], wave_equal[kSelWaves];
@@ -349,8 +355,10 @@ extern "C" int32_t arckv_evict_select(const float* weights, int64_t w_stride, co
   if (n_reqs == 0 || keep == 0) return ARCKV_OK;
   if ((weights == nullptr && w_stride > 0) || seq_lens == nullptr || kept == nullptr)
     return arckv::fail(ARCKV_EINVAL, "%s: NULL pointer", fn);
-  // rows for one work-group to a unit or fewer: 32 keys a thread; more: 16, and two work-groups to a unit
-  const bool one = static_cast<int64_t>(n_reqs) * num_kv_heads <= 256;
+  // Keys of a thread: 16, and two work-groups to a unit, which reads rows of more than 16384 again for every pass;
+  // 32 for such rows of a batch that leaves a unit to each.  32 and 16, us: 32 rows of 32768 24 and 34, 320 of them
+  // 51 and 53; 256 rows of 16384 17.6 and 17.2, 320 of 4096 20 and 14, 1024 of 2600 38 and 25.
+  const bool one = w_stride > 16384 && static_cast<int64_t>(n_reqs) * num_kv_heads <= 256;
 #define ARCKV_SELECT(KEYS)                                                                                    \
   hipLaunchKernelGGL(evict_select_kernel<KEYS>, dim3(num_kv_heads, n_reqs), dim3(kSelThreads), 0,             \
                      static_cast<hipStream_t>(stream), weights, w_stride, seq_lens, num_kv_heads, keep,       \

@@ -9,7 +9,8 @@
 // bytes.
 // kv_gather_mx4: the rows of `slots` as bf16.  A thread takes 8 tokens; where their slots follow each
 // other (through at most one end of half a block) it reads V as pieces of 32 bytes and transposes.
-// What bounds both is memory: 4 D bytes of rows per token and head against 17 / 16 D of codes.
+// What bounds both is memory: 4 D bytes of rows per token and head against 17 / 16 D of codes.  24576 tokens of 8
+// heads of 128, in runs: 25.6 and 25.7 us, 4.95 TB/s (a byte or a token at a time: 39.6 and 33.3).
 #pragma once
 
 #include "mx4.hpp"
@@ -255,6 +256,13 @@ __global__ __launch_bounds__(kMx4Threads) void kv_gather_mx4_kernel(
   }
 }
 
+// Whether there is enough to store or gather for the kernels that take runs of 8 tokens at a time: fewer work-groups,
+// each with a longer chain of waits.  Alone and in runs, us (store; gather), 8 heads of 128: 1024 tokens 3.4 and
+// 4.8; 3.9 and 5.6; 4096 6.6 and 6.6; 8.3 and 7.8; 8192 12.6 and 10.4; 14.0 and 10.8; 16384 22.0 and 16.2; 23.9 and
+// 17.3.  16 heads of 64: 4096 5.5 and 6.1; 6.4 and 7.7; 8192 9.4 and 8.5; 10.7 and 10.9.
+// (16384 tokens whose slots do not follow each other: 30.8 and 38.7; 25.6 and 30.3.)
+bool many_mx4_rows(int64_t n_tokens, int32_t hkv, int32_t head_dim) { return n_tokens * hkv * head_dim > 1 << 22; }
+
 // the checks that both calls make
 int32_t check_mx4_rows(const char* fn, const void* pool, const void* k, const void* v, const int32_t* slots,
                        int64_t n_tokens, int64_t num_blocks, int32_t hkv, int32_t head_dim) {
@@ -284,8 +292,7 @@ extern "C" int32_t arckv_kv_scatter_mx4(void* kv_pool, const void* k_new, const 
   const int32_t st = check_mx4_rows("kv_scatter_mx4", kv_pool, k_new, v_new, slot_mapping, n_tokens, num_blocks,
                                     num_kv_heads, head_dim);
   if (st != ARCKV_OK || n_tokens == 0) return st;
-  // few tokens spread over more work-groups, 16 (head_dim 64: 32) tokens each
-  const bool runs = n_tokens > 1024;
+  const bool runs = many_mx4_rows(n_tokens, num_kv_heads, head_dim);
   const int per = runs ? 64 : kMx4Threads / (head_dim / 8);
   const dim3 grid(static_cast<unsigned>((n_tokens + per - 1) / per), num_kv_heads);
   auto* s = static_cast<hipStream_t>(stream);
@@ -310,7 +317,7 @@ extern "C" int32_t arckv_kv_gather_mx4(const void* kv_pool, void* k_out, void* v
   const int32_t st = check_mx4_rows("kv_gather_mx4", kv_pool, k_out, v_out, slot_mapping, n_tokens, num_blocks,
                                     num_kv_heads, head_dim);
   if (st != ARCKV_OK || n_tokens == 0) return st;
-  const int tok = n_tokens > 1024 ? 8 : 1;      // tokens of a thread
+  const int tok = many_mx4_rows(n_tokens, num_kv_heads, head_dim) ? 8 : 1;      // tokens of a thread
   const int per = kMx4Threads / (head_dim / 8) * tok;
   const dim3 grid(static_cast<unsigned>((n_tokens + per - 1) / per), num_kv_heads);
   auto* s = static_cast<hipStream_t>(stream);

@@ -105,6 +105,35 @@ def test_attention_weights(case, fmt):
         assert torch.equal(run_weights(b, own, longest, False), w)
 
 
+MIXED = [
+    ([(400, 300)] + [(60 + 31 * i, 59 + 31 * i) for i in range(40)], 16, 4, 64),
+    ([(260, 228), (260, 227), (700, 699)] + [(33, 33)] * 3 + [(50 + i, 49 + i) for i in range(9)], 8, 4, 128),
+    ([(130, 66), (130, 65)] + [(40 + i, 39 + i) for i in range(20)], 3, 3, 128),
+    ([(1500, 0)] + [(20, 20 - i % 2) for i in range(60)], 2, 2, 64),
+]
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mx4"])
+@pytest.mark.parametrize("case", range(len(MIXED)))
+def test_weights_of_decode_and_prefill_in_one_batch(case, fmt):
+    """Requests with few columns, with many, with none and at the limits between: each gets its weights once."""
+    reqs, hq, hkv, d = MIXED[case]
+    print_case(f"weights of a mixed batch {reqs[:3]} hq={hq} hkv={hkv} d={d} {fmt}")
+    b = make_batch(reqs, hq, hkv, d, seed=2100 + case, fmt=fmt)
+    ref = reference(b)
+    lse = exact_lse(b, ref)
+    tol = weights_tolerance(b, ref, lse)
+    longest = max(L for L, _ in reqs)
+    for accumulate in (True, False):
+        w = run_weights(b, lse, longest + 3, accumulate)
+        for r, (L, _) in enumerate(reqs):
+            want = ref[r][4] + (1.0 if accumulate else 0.0)
+            err = (w[r, :, :L].double() - want).abs() - tol[r] - 2.0 ** -24 * want.abs() \
+                - ref[r][4] * 2.0 ** -24 * float(lse.abs().max())
+            assert float(err.max()) <= 0, f"request {r}: {float(err.max()):.3g} over its tolerance"
+            assert (w[r, :, L:] == 1).all()
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "mx4"])
 def test_weights_of_non_finite_keys_and_queries(fmt):
     """A NaN key is NaN where some column sees it and touches no other key; so does the NaN column of a query
@@ -184,6 +213,28 @@ def test_select(lens, hkv, keep, first, recent):
                 assert np.array_equal(gw[r, h, :keep], np.r_[w[r, h][want], np.zeros(keep - len(want), np.float32)],
                                       equal_nan=True)
         assert (gw[:, :, keep:] == 7).all() and torch.equal(only, kept)
+
+
+@pytest.mark.parametrize("lens,hkv", [([20000, 16385], 5), ([17000], 257), ([33000, 40], 129), ([16384], 3)])
+def test_select_of_long_rows(lens, hkv):
+    """Rows longer than what a work-group holds, few and many of them: the choice by a stable sort."""
+    print_case(f"select of long rows {lens} hkv={hkv}")
+    rng = np.random.default_rng(hkv)
+    keep, first, recent = 3001, 4, 100
+    w = (rng.integers(0, 9000, (len(lens), hkv, max(lens))) / 8).astype(np.float32)
+    kept = torch.empty(len(lens), hkv, keep, dtype=torch.int32, device=DEV)
+    kw = torch.empty(len(lens), hkv, keep, device=DEV)
+    ak.evict_select(torch.from_numpy(w).to(DEV), i32(lens), kept, first, recent, kept_weights=kw)
+    torch.cuda.synchronize()
+    got, gw = kept.cpu().numpy(), kw.cpu().numpy()
+    for r, L in enumerate(lens):
+        if L <= keep:
+            assert (got[r] == np.r_[np.arange(L), np.full(keep - L, -1)]).all()
+            continue
+        rest = np.argsort(-w[r, :, first:L - recent], axis=1, kind="stable")[:, : keep - first - recent] + first
+        held = np.tile(np.r_[np.arange(first), np.arange(L - recent, L)], (hkv, 1))
+        want = np.sort(np.concatenate([rest, held], axis=1), axis=1)
+        assert np.array_equal(got[r], want) and np.array_equal(gw[r], np.take_along_axis(w[r], want, axis=1))
 
 
 def test_select_takes_a_longer_request_as_its_first_tokens():

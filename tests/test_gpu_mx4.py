@@ -126,6 +126,43 @@ def test_unrelated_slots_in_bulk(d):
         assert np.array_equal(bf16_to_f64(bits(got)), omx.stored(rows), equal_nan=True)
 
 
+@pytest.mark.parametrize("d,hkv,n", [(128, 8, 4097), (128, 8, 4203), (64, 16, 4109), (64, 33, 2011), (128, 3, 10931)])
+def test_many_rows(d, hkv, n):
+    """Enough to be stored and read 8 tokens at a time: whole requests from any first slot, then unrelated slots with a
+    whole half block among them, some of each outside the pool."""
+    print_case(f"mx4 many rows d={d} hkv={hkv} n={n}")
+    rng = np.random.default_rng(n)
+    nblk = n // 16 + 30
+    table = rng.permutation(nblk)
+    m = n * 3 // 4
+    at, slots = 0, []
+    while sum(map(len, slots)) < m:                            # requests that start in a new block each
+        j = np.arange(int(rng.integers(1, 900)))
+        slots.append(table[at + j // 16] * 16 + j % 16)
+        at += len(j) // 16 + 1
+        if at > nblk - 60 - (n - m) // 16:
+            break
+    slots = np.concatenate(slots)[:m]
+    rest = rng.permutation(np.concatenate([table[at + 2:] * 16 + i for i in range(16)]))
+    slots = np.concatenate([slots, table[at + 1] * 16 + 8 + np.arange(8), rest])[:n].astype(np.int32)
+    n = len(slots)
+    assert n * hkv * d > 1 << 22 and len(set(slots.tolist())) == n
+    k, v = random_rows(n, hkv, d, rng, "normal"), random_rows(n, hkv, d, rng, "normal")
+    given = slots.copy()
+    given[rng.integers(0, n, n // 300)] = -1
+    given[rng.integers(0, n, n // 700)] = nblk * 16
+    pool = store(k, v, given, nblk)
+    keep = (given >= 0) & (given < nblk * 16)
+    want = omx.new_pool(nblk, hkv, d)
+    omx.scatter(want, k[keep], v[keep], given[keep])
+    assert np.array_equal(pool.cpu().numpy(), want)
+    ko, vo = (torch.full((n, hkv, d), float("nan"), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    ak.kv_gather_mx4(pool, torch.from_numpy(given).to(DEV), ko, vo)
+    torch.cuda.synchronize()
+    for got, rows in ((ko, k), (vo, v)):
+        assert np.array_equal(bf16_to_f64(bits(got)), np.where(keep[:, None, None], omx.stored(rows), 0.0))
+
+
 def test_every_code_rounds_as_defined():
     """Every bf16 magnitude under each of several scales, beside a value that sets the scale."""
     print_case("mx4 rounding, all magnitudes")
