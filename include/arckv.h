@@ -516,9 +516,9 @@ int32_t arckv_qkv_rope_to_pool(const void* x, const void* w_qkv, int64_t n_token
 int64_t arckv_mx4_pool_bytes(int64_t num_blocks, int32_t num_kv_heads, int32_t head_dim);
 
 /* pool[slot[t]] <- (k_new[t], v_new[t]) in 4 bits, t < n_tokens.  kv_pool: device, layout MX4.
- * Rows, slots, requirements, errors and what happens to slots outside the pool or given twice (one
- * token's K bytes and V bytes win, not always the same token's: callers give equal rows) as
- * for arckv_kv_scatter; num_blocks at most 2^27, n_tokens at most 2^31 - 1. */
+ * Rows, slots, requirements, errors and what happens to slots outside the pool as for
+ * arckv_kv_scatter; of tokens with the same slot any one's codes and any one's scales may stay, so
+ * callers give them equal rows; num_blocks at most 2^27, n_tokens at most 2^31 - 1. */
 int32_t arckv_kv_scatter_mx4(void* kv_pool, const void* k_new, const void* v_new,
                              const int32_t* slot_mapping, int64_t n_tokens, int64_t num_blocks,
                              int32_t num_kv_heads, int32_t head_dim, void* stream);

@@ -3,14 +3,19 @@
 //
 //   o = softmax(scale * q . K^T) V over keys 0..position, K and V as the 4-bit pool stands for
 //
-// A wave takes 16 query columns of an item and its keys in chunks of 32, straight from the pool
-// into registers: S^T = K . Q^T and O^T = V^T . P^T with v_mfma_f32_16x16x32_bf16, codes turned
+// Narrow tiles, here: a wave takes 16 or 32 query columns of an item and its keys in chunks of 32, straight
+// from the pool into registers: S^T = K . Q^T and O^T = V^T . P^T with v_mfma_f32_16x16x32_bf16, codes turned
 // into bf16 (exactly) as operands.  Which keys and dimensions feed which operand row is chosen so
 // that nothing is exchanged between lanes: lane (m, q4) = (lane % 16, lane / 16) holds
 //   K row i of tile t in {0, 1}: key 8 (i / 4) + 4 t + i % 4 of the chunk, dimensions [q4 D/4, (q4 + 1) D/4);
 //   S^T registers: keys 8 q4 + 4 t + r of column m, eight in a row, which is the B operand of P.V;
 //   V^T row m of tile 4 j + i: dimension 64 j + 4 m + i, keys [8 q4, 8 q4 + 8);
 //   O^T registers: dimensions 64 j + 16 q4 + 4 r + i of column m, 16 in a row.
+//
+// What bounds it is the pool's bytes, 17 / 64 of the bf16 kernel's: one new token of each of 64 requests of
+// 2000 (32 / 8 heads of 128) 33.8 us, 4.15 TB/s with the launch, of 8192 128.5 us, 4.45 TB/s, where a large copy
+// reaches 4.74; the bf16 kernel's decode takes 2.6 times as long at lognormal histories.  Small calls take the launch and a chain of
+// round trips (list, lengths, table, codes, join): 8 requests of 400 10 us.
 #pragma once
 
 #include "mx4.hpp"
@@ -211,7 +216,8 @@ __device__ __forceinline__ void mx4_chunk(Mx4State<D, NT>& st, Mx4Raw<D>& raw, i
 // into 8 equal runs, one for each wave, wherever the items end.  A wave keeps the bytes of three
 // chunks in flight, across items too, and nothing waits for another wave until all are done: a
 // wave's part of an item (at most 15 parts on a list) goes to LDS as (m, l, O), and one barrier later
-// all threads join the parts.
+// all threads join the parts.  (By item after item, as below: 41.3 instead of 33.8 us for 64 requests of
+// 2000, 56 instead of 43 at 16 / 16 heads of 64.)
 // Other lists: item after item, 32 columns for a wave, 8, 4 or 2 waves to the same columns, each with
 // its run of the item's chunks, joined the same way.
 struct Mx4Item {
@@ -525,7 +531,9 @@ extern "C" int32_t arckv_prefill_attention_mx4(const void* kv_pool, const void* 
   if (n_work > 0) {
     const bool any = (reinterpret_cast<uintptr_t>(q) | reinterpret_cast<uintptr_t>(out)) % 16 != 0;
     // head_dim 64: two work-groups share a unit where the plan asks for it (an odd number of entries);
-    // where it does not, LDS that nobody uses keeps each on a unit of its own
+    // where it does not, LDS that nobody uses keeps each on a unit of its own.  Alone and shared, us: 600 on
+    // 30000, 64 / 8 heads 483 and 500; 2 turns of 640 on 17008, 32 / 4, 299 and 314; 12 prompts of 1100,
+    // 16 / 16, 103 and 80; 2 turns of 2164 on 3920, 197 and 159.
     const unsigned lds = head_dim == 64 && n_work % 2 == 0 ? 32 << 10 : 0;
     const GroupDiv gd{static_cast<uint32_t>(G), G == 1 ? 0 : static_cast<uint32_t>(((1ull << 32) + G - 1) / G)};
 #define ARCKV_MX4(KERNEL, GRID, GG, LDS)                                                                           \

@@ -10,10 +10,10 @@
 // and the barriers between, 24 to 26 us there; 512 ragged rows of up to 4096, two to a unit: 20 us.
 // kv_compact: the kept tokens' K and V into other blocks, position i of the result from position
 // kept[i]; a head's tokens move on their own, so the same slot may hold another token for another
-// head.  A work-group writes one block of one head.  The bound is the lines it reads, not the tokens: V has a token
+// head.  A work-group writes one block (4 bits: four) of one head.  The bound is the lines it reads, not the tokens: V has a token
 // every 32 bytes (4 bits: every 8), so of 1 token kept in 2 nearly every line of V comes in, and half of
-// K's.  64 requests of about 2600 down to 1024, 8 heads of 128: 93 us, 505 MB at 5.4 TB/s.  4 requests of 32768
-// down to 8192 at 4 bits: 27.5 us.
+// K's.  64 requests of about 2600 down to 1024, 8 heads of 128: 92 us for 332 MB read and 132 written (5.05 TB/s).
+// 4 requests of 32768 down to 8192 at 4 bits: 24.8 us for 66 and 18 MB (3.4 TB/s), in pieces of lines.
 #pragma once
 
 #include "mx4.hpp"
@@ -212,11 +212,12 @@ __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_k
   }
 }
 
-// Where the 16 tokens of a destination block come from: slot of each, -1 for none.
-__device__ __forceinline__ void source_slots(int32_t* src, const int32_t* kept, int keep, const int32_t* bt,
+// Where the 16 N tokens of the destination blocks from b on come from: slot of each, -1 for none.
+template <int N>
+__device__ __forceinline__ void source_slots(int32_t (&src)[16 * N], const int32_t* kept, int keep, const int32_t* bt,
                                              int bt_stride, int64_t num_blocks, int b) {
   const int i = 16 * b + threadIdx.x;
-  if (threadIdx.x < 16) {
+  if (threadIdx.x < 16 * N) {
     int32_t s = -1;
     const int32_t p = i < keep ? kept[i] : -1;
     if (p >= 0 && (p >> 4) < bt_stride) {
@@ -237,8 +238,8 @@ __global__ __launch_bounds__(256) void kv_compact_kernel(
     int64_t num_blocks, int hkv) {
   __shared__ int32_t src[16];
   const int b = blockIdx.x / hkv, h = blockIdx.x % hkv, r = blockIdx.y, tid = threadIdx.x;
-  source_slots(src, kept + (static_cast<int64_t>(r) * hkv + h) * keep, keep,
-               block_tables + static_cast<int64_t>(r) * bt_stride, bt_stride, num_blocks, b);
+  source_slots<1>(src, kept + (static_cast<int64_t>(r) * hkv + h) * keep, keep,
+                  block_tables + static_cast<int64_t>(r) * bt_stride, bt_stride, num_blocks, b);
   const int32_t db = dst_tables[static_cast<int64_t>(r) * dst_stride + b];
   const bool bad = db < 0 || db >= num_blocks;
   ARCKV_CHECK_WAVE(bad && src[0] >= 0 && tid < 64, ARCKV_CHECK_BLOCK);
@@ -273,53 +274,79 @@ __global__ __launch_bounds__(256) void kv_compact_kernel(
   }
 }
 
+// A block has few bytes in 4 bits: a work-group takes 4, whose loads are in flight together (one block each:
+// 27.5 us for 4 requests of 32768 down to 8192).
+constexpr int kMoveBlocks = 4;
+
 template <int D>
 __global__ __launch_bounds__(256) void kv_compact_mx4_kernel(
     uint8_t* __restrict__ pool, const int32_t* __restrict__ block_tables, int bt_stride,
     const int32_t* __restrict__ kept, int keep, const int32_t* __restrict__ dst_tables, int dst_stride,
     int64_t num_blocks, int hkv) {
   using L = mx4::Layout<D>;
-  __shared__ int32_t src[16];
-  const int b = blockIdx.x / hkv, h = blockIdx.x % hkv, r = blockIdx.y, tid = threadIdx.x;
-  source_slots(src, kept + (static_cast<int64_t>(r) * hkv + h) * keep, keep,
-               block_tables + static_cast<int64_t>(r) * bt_stride, bt_stride, num_blocks, b);
-  const int32_t db = dst_tables[static_cast<int64_t>(r) * dst_stride + b];
-  const bool bad = db < 0 || db >= num_blocks;
-  ARCKV_CHECK_WAVE(bad && src[0] >= 0 && tid < 64, ARCKV_CHECK_BLOCK);
-  if (bad) return;
-  uint8_t* to = pool + (static_cast<int64_t>(db) * hkv + h) * L::kBytes;
-  auto from = [&](int t) { return pool + (static_cast<int64_t>(src[t] >> 4) * hkv + h) * L::kBytes; };
-  constexpr int WORDS = D / 8;
-  if (tid < 16 * WORDS) {
-    const int t = tid / WORDS, c = tid % WORDS;
-    if (src[t] >= 0)
-      *reinterpret_cast<uint32_t*>(to + t * L::kRow + 4 * c) =
-          *reinterpret_cast<const uint32_t*>(from(t) + (src[t] & 15) * L::kRow + 4 * c);
+  constexpr int N = kMoveBlocks, WORDS = D / 8, VN = N * D / 256;
+  __shared__ int32_t src[16 * N], dst[N];
+  const int b = blockIdx.x / hkv * N, h = blockIdx.x % hkv, r = blockIdx.y, tid = threadIdx.x;
+  if (tid >= 64 && tid < 64 + N) {
+    const int n = tid - 64;
+    const int32_t db = 16 * (b + n) < keep ? dst_tables[static_cast<int64_t>(r) * dst_stride + b + n] : -1;
+    dst[n] = db >= 0 && db < num_blocks ? db : -1;
   }
-  if (tid < 16 * L::kGroups) {
-    const int t = tid & 15, g = tid >> 4;
-    if (src[t] >= 0) {
-      to[L::kKScale + t * L::kGroups + g] = from(t)[L::kKScale + (src[t] & 15) * L::kGroups + g];
-      to[L::kVScale + g * 16 + t] = from(t)[L::kVScale + g * 16 + (src[t] & 15)];
-    }
+  source_slots<N>(src, kept + (static_cast<int64_t>(r) * hkv + h) * keep, keep,
+                  block_tables + static_cast<int64_t>(r) * bt_stride, bt_stride, num_blocks, b);
+  ARCKV_CHECK_LANE(tid < N && dst[tid % N] < 0 && src[16 * (tid % N)] >= 0, ARCKV_CHECK_BLOCK);
+  auto block = [&](int32_t ph) { return pool + (static_cast<int64_t>(ph) * hkv + h) * L::kBytes; };
+  auto from = [&](int32_t s) { return block(s >> 4); };
+  // loads: K codes, a word of a token; scales, one of a token and group; V codes, 8 tokens of a pair
+  const int kt = tid / WORDS, kc = tid % WORDS;
+  uint32_t kw[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    const int32_t s = tid < 16 * WORDS && dst[n] >= 0 ? src[16 * n + kt % 16] : -1;
+    kw[n] = s < 0 ? 0 : *reinterpret_cast<const uint32_t*>(from(s) + (s & 15) * L::kRow + 4 * kc);
   }
-  if (tid < D) {
-    const int half = tid / (D / 2), p = tid % (D / 2);
-    uint32_t x[8];
-    bool all = true;
+  const int sn = tid / (16 * L::kGroups), st = tid % 16, sg = tid / 16 % L::kGroups;
+  const int32_t ss = sn < N && dst[sn % N] >= 0 ? src[16 * (sn % N) + st] : -1;
+  uint8_t ks = 0, vs = 0;
+  if (ss >= 0) {
+    ks = from(ss)[L::kKScale + (ss & 15) * L::kGroups + sg];
+    vs = from(ss)[L::kVScale + sg * 16 + (ss & 15)];
+  }
+  uint32_t x[VN][8];
+  bool all[VN];
+#pragma unroll
+  for (int m = 0; m < VN; ++m) {
+    const int e = tid + 256 * m, n = e / D, half = e % D / (D / 2), p = e % (D / 2);
+    all[m] = true;
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const int t = 8 * half + j, s = src[t];
-      all &= s >= 0;
-      x[j] = s < 0 ? 0 : from(t)[L::kV + ((s & 15) >> 3) * L::kHalf + 8 * p + (s & 7)];
+      const int32_t s = dst[n] >= 0 ? src[16 * n + 8 * half + j] : -1;
+      all[m] &= s >= 0;
+      x[m][j] = s < 0 ? 0 : from(s)[L::kV + ((s & 15) >> 3) * L::kHalf + 8 * p + (s & 7)];
     }
-    uint8_t* at = to + L::kV + half * L::kHalf + 8 * p;
-    if (all) {
-      *reinterpret_cast<uint2*>(at) = uint2{x[0] | x[1] << 8 | x[2] << 16 | x[3] << 24, x[4] | x[5] << 8 | x[6] << 16 | x[7] << 24};
+  }
+  // stores; slots without a token keep what they hold
+#pragma unroll
+  for (int n = 0; n < N; ++n)
+    if (tid < 16 * WORDS && dst[n] >= 0 && src[16 * n + kt % 16] >= 0)
+      *reinterpret_cast<uint32_t*>(block(dst[n]) + kt * L::kRow + 4 * kc) = kw[n];
+  if (ss >= 0) {
+    uint8_t* to = block(dst[sn % N]);
+    to[L::kKScale + st * L::kGroups + sg] = ks;
+    to[L::kVScale + sg * 16 + st] = vs;
+  }
+#pragma unroll
+  for (int m = 0; m < VN; ++m) {
+    const int e = tid + 256 * m, n = e / D, half = e % D / (D / 2), p = e % (D / 2);
+    if (dst[n] < 0) continue;
+    uint8_t* at = block(dst[n]) + L::kV + half * L::kHalf + 8 * p;
+    if (all[m]) {
+      *reinterpret_cast<uint2*>(at) = uint2{x[m][0] | x[m][1] << 8 | x[m][2] << 16 | x[m][3] << 24,
+                                            x[m][4] | x[m][5] << 8 | x[m][6] << 16 | x[m][7] << 24};
     } else {
 #pragma unroll
       for (int j = 0; j < 8; ++j)
-        if (src[8 * half + j] >= 0) at[j] = static_cast<uint8_t>(x[j]);
+        if (src[16 * n + 8 * half + j] >= 0) at[j] = static_cast<uint8_t>(x[m][j]);
     }
   }
 }
@@ -377,7 +404,7 @@ extern "C" int32_t arckv_kv_compact(void* k_pool, void* v_pool, const int32_t* b
   const int32_t st = check_compact("kv_compact", k_pool, v_pool, block_tables, bt_stride, kept, keep, dst_tables,
                                    dst_stride, n_reqs, num_blocks, num_kv_heads, head_dim);
   if (st != ARCKV_OK || n_reqs == 0 || keep == 0) return st;
-  const dim3 grid(static_cast<unsigned>((keep + 15) / 16) * num_kv_heads, n_reqs);
+  const dim3 grid(static_cast<unsigned>((static_cast<int64_t>(keep) + 15) / 16) * num_kv_heads, n_reqs);
   auto* s = static_cast<hipStream_t>(stream);
   auto* k = static_cast<uint16_t*>(k_pool);
   auto* v = static_cast<uint16_t*>(v_pool);
@@ -399,7 +426,8 @@ extern "C" int32_t arckv_kv_compact_mx4(void* kv_pool, const int32_t* block_tabl
   const int32_t st = check_compact("kv_compact_mx4", kv_pool, kv_pool, block_tables, bt_stride, kept, keep,
                                    dst_tables, dst_stride, n_reqs, num_blocks, num_kv_heads, head_dim);
   if (st != ARCKV_OK || n_reqs == 0 || keep == 0) return st;
-  const dim3 grid(static_cast<unsigned>((keep + 15) / 16) * num_kv_heads, n_reqs);
+  const int nb = static_cast<int>((static_cast<int64_t>(keep) + 15) / 16);
+  const dim3 grid(static_cast<unsigned>((nb + kMoveBlocks - 1) / kMoveBlocks) * num_kv_heads, n_reqs);
   auto* s = static_cast<hipStream_t>(stream);
   auto* p = static_cast<uint8_t*>(kv_pool);
   if (head_dim == 64)

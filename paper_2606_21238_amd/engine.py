@@ -3,6 +3,9 @@
 prepare (hash blocks, plan the batch on the host cache, plan the attention work, pack the
 metadata: one native call) -> copy metadata to the device -> [project Q/K/V] -> scatter the
 computed tokens' K/V -> prefix-cached prefill attention -> release.
+kv_format="mx4" holds K and V in 4 bits and runs the same steps over them; gather() reads rows back.
+attention_weights() after attention(lse=) adds up what every cached token received, evict() moves
+the heaviest tokens into blocks that the caller owns.
 Every step is a libarckv call; this class owns the device buffers (PyTorch tensors used
 only as device memory) and the host cache handle.  plan() + upload() are the same first
 steps as separate calls.
