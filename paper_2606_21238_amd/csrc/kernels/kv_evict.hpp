@@ -39,10 +39,10 @@ template <int KEYS>
 __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_kernel(
     const float* __restrict__ weights, int64_t w_stride, const int32_t* __restrict__ seq_lens, int hkv, int keep,
     int n_first, int n_recent, int32_t* __restrict__ kept, float* __restrict__ kept_weights, int64_t kw_stride) {
-  // one histogram for every kCopies-th lane: fewer lanes of a wave meet at an address (one for all of uniform
-  // weights, which meet least: 25.0 against 24.5 us for 32 rows of 32768, 26.2 against 25.2 for 1024 of 2600)
+  // one histogram for every kCopies-th lane, side by side: fewer lanes of a wave meet at an address or a bank (one for
+  // all: 25.0 against 24.3 us for 32 rows of 32768 uniform weights, 26.2 against 25.1 for 1024 of 2600)
   constexpr int kCopies = KEYS > 16 ? 4 : 2;
-  __shared__ int hist[kCopies][4096];
+  __shared__ __attribute__((aligned(16))) int hist[4096][kCopies];
   __shared__ int wave_sum[kSelWaves], wave_take[kSelWaves], wave_equal[kSelWaves];
   __shared__ int pick, above;
   const int tid = threadIdx.x, lane = tid & 63, h = blockIdx.x, r = blockIdx.y;
@@ -108,11 +108,11 @@ __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_k
       for (int i = 0; i < kPer; ++i)
         if (i * kSelThreads < bins)
 #pragma unroll
-          for (int v = 0; v < kCopies; ++v) hist[v][i * kSelThreads + tid] = 0;
+          for (int v = 0; v < kCopies; ++v) hist[i * kSelThreads + tid][v] = 0;
       __syncthreads();
       auto count = [&](uint32_t k) {
         if (pass == 0 || (k >> (shift + kBits[pass])) == (prefix >> (shift + kBits[pass])))
-          atomicAdd(&hist[lane % kCopies][(k >> shift) & (bins - 1)], 1);
+          atomicAdd(&hist[(k >> shift) & (bins - 1)][lane % kCopies], 1);
       };
       // (the key 0 of positions behind an inner run only adds to the lowest digit, where it decides nothing)
       if (inner) each([&](int, uint32_t k) { count(k); });
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kSelThreads, KEYS > 16 ? 4 : 8) void evict_select_k
       for (int i = 0; i < kPer; ++i) {
         c[i] = 0;
 #pragma unroll
-        for (int v = 0; v < kCopies; ++v) c[i] += i < per ? hist[v][bins - 1 - (per * tid + i)] : 0;
+        for (int v = 0; v < kCopies; ++v) c[i] += i < per ? hist[bins - 1 - (per * tid + i)][v] : 0;
         sum += c[i];
       }
       int upto = sum;
