@@ -10,10 +10,10 @@
 // the same swizzled places.
 //
 // What bounds it is the matrix units with the conversions beside them: 2048 tokens on 32768, 64 / 8 heads of
-// 128, 1.91 to 1.98 ms (1.15 to 1.19 PFLOP/s; the bf16 kernel 1.80, a large matrix product's rate 1.71).
+// 128, 1.91 to 1.98 ms (1.15 to 1.19 PFLOP/s; the bf16 kernel 1.79, a large matrix product's rate 1.71).
 // Without the loads it would take 1.81 (against 1.95 on the same card), without the conversions 1.69, without
-// both 1.60.  8 questions of 128 on 8192: 216 us (bf16 227 to 237): 192 items on 256 units.  12 prompts of 1100,
-// 16 / 16 heads of 64: 73 us (bf16 68).  LDS operands 4 or 6 ahead and V writes without bank conflicts change
+// both 1.60.  8 questions of 128 on 8192, 40 / 8: 216 us (bf16 196): 192 items on 256 units.  12 prompts of 1100,
+// 16 / 16 heads of 64: 72 us (bf16 64).  LDS operands 4 or 6 ahead and V writes without bank conflicts change
 // nothing.
 #pragma once
 
