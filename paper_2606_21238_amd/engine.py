@@ -353,7 +353,9 @@ class PrefillEngine:
         longest request]).  Their K and V move into the blocks of dst_tables (host int32 [n_reqs, >=
         ceil(keep / 16)]: the caller's own, none of them a block of the batch, none twice; see
         private_blocks).  Returns (kept positions int32 [n_reqs, Hkv, keep], -1 behind a shorter request's;
-        their weights, fp32).  The batch must not have been released.  Afterwards request r holds min(L_r, keep) tokens in dst_tables[r]."""
+        their weights, fp32).  Afterwards request r holds min(L_r, keep) tokens in dst_tables[r].  The
+        batch must not have been released, and the stream must not be capturing (a graph takes
+        evict_select and kv_compact, with tables on the device)."""
         import torch
         plan, n = db.plan, db.plan.n_reqs
         self._check_weights(n, weights)
@@ -374,9 +376,11 @@ class PrefillEngine:
             # (entries of -1 look at the spare last place)
             if plan.block_tables.size and plan.block_tables.max() >= lo and uses[plan.block_tables].any():
                 raise ValueError("dst_tables names a block of the batch")
-        host = torch.empty(dst.shape, dtype=torch.int32, pin_memory=True)
-        host.numpy()[:] = dst
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(self._torch_stream(stream)):
+            if torch.cuda.is_current_stream_capturing():
+                raise ValueError("evict copies dst_tables from the host and cannot be captured")
+            host = torch.empty(dst.shape, dtype=torch.int32, pin_memory=True)
+            host.numpy()[:] = dst
             dev = host.to(self.device, non_blocking=True)
             kept = torch.empty((n, self.hkv, keep), dtype=torch.int32, device=self.device)
             kept_weights = torch.empty((n, self.hkv, keep), dtype=torch.float32, device=self.device)

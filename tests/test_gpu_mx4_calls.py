@@ -278,6 +278,22 @@ def test_refusals_of_the_binding():
         PrefillEngine(8, 2, 64, 4, 6, 2).gather(i32([0]), k[:1], k[:1])
 
 
+def test_evict_is_not_captured(monkeypatch):
+    """Its host table would be gone when the graph is replayed."""
+    eng = PrefillEngine(8, 2, 64, 4, 6, 2, kv_format="mx4", pool_fill=0, private_blocks=1)
+    db = eng.prepare([np.arange(20, dtype=np.int32)])
+    w = torch.zeros(1, 2, 20, device=DEV)
+    dst = np.array([[6]], dtype=np.int32)
+    for stream in (None, torch.cuda.Stream()):
+        with monkeypatch.context() as m:
+            m.setattr(torch.cuda, "is_current_stream_capturing", lambda: True)
+            with pytest.raises(ValueError, match="captured"):
+                eng.evict(db, w, 8, dst, stream=stream)
+    kept, _ = eng.evict(db, w, 8, dst)
+    assert kept[0, 0].tolist() == list(range(8))
+    eng.release()
+
+
 def test_checked_build_records_what_it_turns_away(monkeypatch):
     print_case("checked build, 4-bit calls")
     chk = _lib.load(CHECKED_LIB)
