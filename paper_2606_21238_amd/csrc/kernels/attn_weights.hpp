@@ -267,7 +267,9 @@ __global__ __launch_bounds__(256, MX4 || D == 64 ? 4 : 3) void attn_weights_stre
       a[i] = bf16x8_t{};
       if (c < rq.ncols) __builtin_memcpy(&a[i], q + row * D + wt_chunk<D, MX4>(i, hg) * 8, 16);
     }
-    // a column that is not there: q of zeros and a sum of infinity give a weight of zero
+    // A column that is not there: q of zeros and a sum of infinity give a weight of zero, over finite keys.  Zero times
+    // an infinite one is NaN, so with bf16 keys such columns are masked (of 4-bit keys what is not finite is NaN for the
+    // columns that are there too).
     const float mine = c < rq.ncols ? lse[row] * kLog2e : INFINITY;
     f32x4_t l4[4];
 #pragma unroll
@@ -286,7 +288,7 @@ __global__ __launch_bounds__(256, MX4 || D == 64 ? 4 : 3) void attn_weights_stre
         ph = block(min(sub + 2 * by, nsub - 1));
       }
       const int key = sub * 32 + l32;
-      const bool masked = sub * 32 + 31 > pos0 || rq.ncols <= cb;
+      const bool masked = sub * 32 + 31 > pos0 || (!MX4 && rq.ncols < cb + 8 * groups);
       auto sums = [&](int g) { return l4[g]; };
       const float mine32 = masked ? wt_sum<true>(s, sums, scale_log2, cb, hg, first_column(key, rq.P, G), rq.ncols, groups)
                                   : wt_sum<false>(s, sums, scale_log2, cb, hg, 0, rq.ncols, groups);
