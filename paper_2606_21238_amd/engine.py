@@ -351,8 +351,8 @@ class PrefillEngine:
         """Cuts every request of the batch down to at most `keep` tokens for each KV head: the first
         n_first, the last n_recent, and the heaviest others by `weights` (fp32 [n_reqs, Hkv, stride >= the
         longest request]).  Their K and V move into the blocks of dst_tables (host int32 [n_reqs, >=
-        ceil(keep / 16)]: the caller's own, none of them a block of the batch, none twice; see
-        private_blocks).  Returns (kept positions int32 [n_reqs, Hkv, keep], -1 behind a shorter request's;
+        ceil(keep / 16)]: private blocks of the caller's, num_phys and up, none twice and none of them a
+        block of the batch).  Returns (kept positions int32 [n_reqs, Hkv, keep], -1 behind a shorter request's;
         their weights, fp32).  Afterwards request r holds min(L_r, keep) tokens in dst_tables[r].  The
         batch must not have been released, and the stream must not be capturing (a graph takes
         evict_select and kv_compact, with tables on the device)."""
@@ -376,6 +376,8 @@ class PrefillEngine:
             # (entries of -1 look at the spare last place)
             if plan.block_tables.size and plan.block_tables.max() >= lo and uses[plan.block_tables].any():
                 raise ValueError("dst_tables names a block of the batch")
+            if lo < self.num_phys:
+                raise ValueError(f"dst_tables names block {lo} of the block cache (private blocks start at {self.num_phys})")
         with contextlib.nullcontext() if stream is None else torch.cuda.stream(self._torch_stream(stream)):
             if torch.cuda.is_current_stream_capturing():
                 raise ValueError("evict copies dst_tables from the host and cannot be captured")
