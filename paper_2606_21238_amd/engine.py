@@ -361,16 +361,18 @@ class PrefillEngine:
         self._check_weights(n, weights)
         if n and int(weights.shape[2]) < int(plan.seq_lens.max()):
             raise ValueError("weights must have an entry for every token of the longest request")
-        dst = np.ascontiguousarray(dst_tables, dtype=np.int32)
+        dst = np.asarray(dst_tables)
         nb = -(-keep // 16)
+        if dst.size and dst.dtype.kind not in "iu":
+            raise ValueError("dst_tables must hold integers")
         if dst.ndim != 2 or dst.shape[0] != n or dst.shape[1] < nb:
             raise ValueError(f"dst_tables must be [{n}, >= {nb}]")
         own = dst[:, :nb].ravel()
         if own.size:
-            lo, hi = int(own.min()), int(own.max())
+            lo, hi = int(own.min()), int(own.max())    # of the numbers as given: more than 32 bits would wrap
             if lo < 0 or hi >= self.num_blocks:
                 raise ValueError("dst_tables names blocks outside the pool")
-            uses = np.bincount(own, minlength=self.num_blocks + 1)
+            uses = np.bincount(own.astype(np.int64), minlength=self.num_blocks + 1)
             if uses.max() > 1:
                 raise ValueError("dst_tables names a block twice")
             # (entries of -1 look at the spare last place)

@@ -70,3 +70,13 @@ def test_other_refusals_name_what_is_wrong(evict):
                       ([[12, 13], [13, 14]], "twice"), ([[12, 13]], "dst_tables"), ([[12], [13]], "dst_tables")):
         with pytest.raises(ValueError, match=word):
             evict(np.array(dst, np.int32))
+
+
+def test_block_numbers_are_not_wrapped_or_rounded(evict):
+    """Numbers of more than 32 bits, whose low halves are private blocks, and numbers that are no integers."""
+    with pytest.raises(ValueError, match="outside"):
+        evict(np.array([[12, 13], [14, (1 << 32) + 15]], np.int64))
+    with pytest.raises(ValueError, match="outside"):
+        evict(np.array([[12, 13], [14, 15 - (1 << 32)]], np.int64))
+    with pytest.raises(ValueError, match="integers"):
+        evict(np.array([[12, 13], [14, 15.5]]))
