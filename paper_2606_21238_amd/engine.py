@@ -83,6 +83,9 @@ class PrefillEngine:
         self._stage_ev = [None] * self._ring
         self._dev_meta = [None] * self._ring
         self._turn = 0
+        # the stream (handle) of the last call: first the one that the pools are being filled on
+        self._last = _current_stream(self.device.index) if self.device.type == "cuda" else None
+        self._many = False      # whether there has been a second one
 
     # ---- host steps ----------------------------------------------------------------------
     def plan(self, token_lists) -> BatchPlan:
@@ -111,8 +114,7 @@ class PrefillEngine:
             if st == _lib.ENOSPC and (host is None or d["n_packed"] > host.size):
                 cap = max(d["n_packed"], 1 << 16) * 2
                 self._stage[t] = torch.empty(cap, dtype=torch.int32, pin_memory=True)
-                with torch.cuda.stream(ts):
-                    self._dev_meta[t] = torch.empty(cap, dtype=torch.int32, device=self.device)
+                self._dev_meta[t] = self._grow(self._dev_meta[t], cap, torch.int32, ts)
                 continue
             _lib.check(st, "arckv_prepare_batch")
             break
@@ -143,8 +145,7 @@ class PrefillEngine:
         if self._stage[t] is None or self._stage[t].numel() < n_int:
             cap = max(n_int, 1 << 16) * 2
             self._stage[t] = torch.empty(cap, dtype=torch.int32, pin_memory=True)
-            with torch.cuda.stream(ts):
-                self._dev_meta[t] = torch.empty(cap, dtype=torch.int32, device=self.device)
+            self._dev_meta[t] = self._grow(self._dev_meta[t], cap, torch.int32, ts)
         host = self._stage[t].numpy()
         o = 0
         for p in parts:
@@ -165,21 +166,59 @@ class PrefillEngine:
     # ---- streams ---------------------------------------------------------------------------
     # `stream` is None (torch's current stream), a torch.cuda.Stream or a raw hipStream_t
     # handle.  The metadata copy, its event and every (re)allocation of a device buffer run on
-    # that stream, the stream the kernels then run on: the kernels are ordered after the copy,
-    # and the caching allocator hands out a replaced buffer's memory again only in that
-    # stream's order, after the kernels that read it.
+    # that stream, the stream the kernels then run on: the kernels are ordered after the copy.
+    # The pools, the workspaces and the metadata ring are one set for all streams, so an engine's
+    # work runs in the order of its calls: a call on another stream than the call before makes
+    # its stream wait for what that one has queued (a raw handle stays valid until then).  A
+    # stream under capture waits for nothing (torch.cuda.graph starts a capture with the device idle).
     def _torch_stream(self, stream):
         import torch
         if stream is None:
-            return torch.cuda.current_stream(self.device)
-        if isinstance(stream, torch.cuda.Stream):
-            return stream
-        return torch.cuda.ExternalStream(int(stream), device=self.device)
+            stream = torch.cuda.current_stream(self.device)
+        elif not isinstance(stream, torch.cuda.Stream):
+            stream = torch.cuda.ExternalStream(int(stream), device=self.device)
+        self._in_order(stream.cuda_stream)
+        return stream
 
     def _stream(self, stream):
         if stream is None:
-            return _current_stream(self.device.index)
-        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+            handle = _current_stream(self.device.index)
+        else:
+            handle = stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+        self._in_order(handle)
+        return handle
+
+    def _in_order(self, handle: int):
+        if handle != self._last:
+            self._change_stream(handle)
+
+    def _change_stream(self, handle: int):
+        import torch
+
+        def of(h):
+            return torch.cuda.ExternalStream(h, device=self.device) if h else torch.cuda.default_stream(self.device)
+
+        for h in (handle, self._last):
+            if h is not None:
+                with torch.cuda.stream(of(h)):
+                    if torch.cuda.is_current_stream_capturing():
+                        return
+        if self._last is not None:
+            done = torch.cuda.Event()
+            done.record(of(self._last))
+            of(handle).wait_event(done)
+            self._many = True
+        self._last = handle
+
+    def _grow(self, old, n: int, dtype, ts):
+        """A device buffer of n elements, allocated in the order of stream ts, in place of `old`, whose memory goes
+        back to the order of the stream that it was allocated on.  That stream may be another, and knows
+        nothing of what ts has queued: then the host waits for it."""
+        import torch
+        if old is not None and old.numel() and self._many:
+            ts.synchronize()
+        with torch.cuda.stream(ts):
+            return torch.empty(n, dtype=dtype, device=self.device)
 
     def _call(self, name: str, stream, *args):
         """A library call on the engine's device (made the current one if it is not) and `stream`."""
@@ -211,8 +250,7 @@ class PrefillEngine:
     def _ensure_ws(self, nbytes: int, ts):
         if nbytes > self._ws.numel():
             import torch
-            with torch.cuda.stream(ts):
-                self._ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device)
+            self._ws = self._grow(self._ws, nbytes, torch.uint8, ts)
 
     # ---- device steps --------------------------------------------------------------------
     # The engine built every device buffer itself, so these calls skip the binding's per-call
@@ -257,8 +295,7 @@ class PrefillEngine:
                 raise ValueError("q / k_new / v_new must be contiguous 16-bit [n_tokens, heads, D]")
         need = 4 * t * self.d
         if self._y is None or self._y.numel() < need:
-            with torch.cuda.stream(self._torch_stream(stream)):
-                self._y = torch.empty(max(need, 1), dtype=torch.uint8, device=self.device)
+            self._y = self._grow(self._y, max(need, 1), torch.uint8, self._torch_stream(stream))
         _lib.check(lib().arckv_qkv_rope(x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
                                         db.cu_q.data_ptr(), db.seq_lens.data_ptr(), db.plan.n_reqs,
                                         float(rope_theta), self._y.data_ptr(), self._y.numel(),
@@ -280,8 +317,7 @@ class PrefillEngine:
             raise ValueError("q must be contiguous 16-bit [n_tokens, heads, D]")
         need = 4 * t * self.d
         if self._y is None or self._y.numel() < need:
-            with torch.cuda.stream(self._torch_stream(stream)):
-                self._y = torch.empty(max(need, 1), dtype=torch.uint8, device=self.device)
+            self._y = self._grow(self._y, max(need, 1), torch.uint8, self._torch_stream(stream))
         _lib.check(lib().arckv_qkv_rope_to_pool(
             x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d, db.cu_q.data_ptr(),
             db.seq_lens.data_ptr(), db.plan.n_reqs, float(rope_theta), self._y.data_ptr(), self._y.numel(),
