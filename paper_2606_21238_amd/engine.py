@@ -24,6 +24,9 @@ from . import _lib
 
 @dataclass
 class DeviceBatch:
+    """A planned batch on the device.  The arrays lie in the engine's ring of metadata buffers: they hold the batch
+    until the fourth prepare() or upload() after it.  Of a batch whose calls were captured into a graph they
+    stay, as long as the DeviceBatch (a graph's owner keeps it)."""
     plan: BatchPlan
     block_tables: object
     cu_q: object
@@ -102,6 +105,7 @@ class PrefillEngine:
         the ring, then one asynchronous copy on `stream` moves them to the device.  A caller that
         keeps its requests' block hashes passes `hashes` and `n_tokens` instead of token lists."""
         import torch
+        self._not_captured("prepare")
         ts = self._torch_stream(stream)
         t = self._turn
         self._turn = (t + 1) % self._ring
@@ -134,6 +138,7 @@ class PrefillEngine:
     def upload(self, plan: BatchPlan, stream=None) -> DeviceBatch:
         """The metadata of a plan() result to the device, copied on `stream`."""
         import torch
+        self._not_captured("upload")
         ts = self._torch_stream(stream)
         ap = attention_plan(plan.cu_q, plan.seq_lens, self.hq, self.hkv, self.d, self.num_cus)
         parts = [plan.block_tables.ravel(), plan.cu_q, plan.seq_lens, plan.slot_mapping, ap.work.ravel()]
@@ -210,6 +215,34 @@ class PrefillEngine:
             self._many = True
         self._last = handle
 
+    # Calls may be captured by torch.cuda.graph.  A replay reads the metadata and writes the workspaces that were
+    # captured, while the engine goes on with other batches and other graphs: so a captured call's
+    # workspace is the graph's own memory, and the ring lets go of its batch's buffer (the batch keeps it).
+    @staticmethod
+    def _not_captured(name: str):
+        import torch
+        if torch.cuda.is_current_stream_capturing():
+            raise ValueError(f"{name} copies from a staging buffer that it fills again, and cannot be captured")
+
+    def _captured(self, db: DeviceBatch) -> bool:
+        import torch
+        if not torch.cuda.is_current_stream_capturing():
+            return False
+        for t, dev in enumerate(self._dev_meta):
+            if dev is not None and 0 <= db.cu_q.data_ptr() - dev.data_ptr() < 4 * dev.numel():
+                self._dev_meta[t] = self._stage[t] = self._stage_ev[t] = None
+        return True
+
+    def _rope_table(self, db: DeviceBatch, stream):
+        """The workspace of the producer: a (cos, sin) table of the batch's tokens."""
+        import torch
+        need = max(4 * db.n_tokens * self.d, 1)
+        if self._captured(db):
+            return torch.empty(need, dtype=torch.uint8, device=self.device)
+        if self._y is None or self._y.numel() < need:
+            self._y = self._grow(self._y, need, torch.uint8, self._torch_stream(stream))
+        return self._y
+
     def _grow(self, old, n: int, dtype, ts):
         """A device buffer of n elements, allocated in the order of stream ts, in place of `old`, whose memory goes
         back to the order of the stream that it was allocated on.  That stream may be another, and knows
@@ -261,6 +294,7 @@ class PrefillEngine:
         shape = (db.n_tokens, self.hkv, self.d)
         if self._bad(k_new, shape) or self._bad(v_new, shape):
             raise ValueError(f"k_new / v_new must be contiguous 16-bit {shape}")
+        self._captured(db)
         rows = (k_new.data_ptr(), v_new.data_ptr(), db.slot_mapping.data_ptr(), db.n_tokens, self.num_blocks,
                 self.hkv, self.d)
         if self.kv_format == "mx4":
@@ -284,7 +318,6 @@ class PrefillEngine:
         """Q/K/V of the batch's computed tokens from their hidden states x [n_tokens, H]
         (projection by w_qkv [(Hq + 2 Hkv) D, H] and rotary embedding, arckv_qkv_rope);
         k_new / v_new then go to scatter()."""
-        import torch
         t, h = db.n_tokens, int(x.shape[1])
         n_out = (self.hq + 2 * self.hkv) * self.d
         if tuple(x.shape) != (t, h) or tuple(w_qkv.shape) != (n_out, h) or x.element_size() != 2 or \
@@ -293,19 +326,16 @@ class PrefillEngine:
         for a, c in ((q, self.hq), (k_new, self.hkv), (v_new, self.hkv)):
             if tuple(a.shape) != (t, c, self.d) or not a.is_contiguous() or a.element_size() != 2:
                 raise ValueError("q / k_new / v_new must be contiguous 16-bit [n_tokens, heads, D]")
-        need = 4 * t * self.d
-        if self._y is None or self._y.numel() < need:
-            self._y = self._grow(self._y, max(need, 1), torch.uint8, self._torch_stream(stream))
+        y = self._rope_table(db, stream)
         _lib.check(lib().arckv_qkv_rope(x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
                                         db.cu_q.data_ptr(), db.seq_lens.data_ptr(), db.plan.n_reqs,
-                                        float(rope_theta), self._y.data_ptr(), self._y.numel(),
+                                        float(rope_theta), y.data_ptr(), y.numel(),
                                         q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), self._stream(stream)),
                    "arckv_qkv_rope")
 
     def project_to_pool(self, db: DeviceBatch, x, w_qkv, q, rope_theta: float, stream=None):
         """project() with the KV scatter fused in (arckv_qkv_rope_to_pool): Q into q, the batch's
         K and V straight into the engine's pools at the plan's slots; no scatter() follows."""
-        import torch
         if self.kv_format != "bf16":
             raise ValueError("project_to_pool writes bf16 pools: a 4-bit pool takes project() and scatter()")
         t, h = db.n_tokens, int(x.shape[1])
@@ -315,12 +345,10 @@ class PrefillEngine:
             raise ValueError(f"x must be contiguous 16-bit [{t}, H] and w_qkv [{n_out}, H]")
         if tuple(q.shape) != (t, self.hq, self.d) or not q.is_contiguous() or q.element_size() != 2:
             raise ValueError("q must be contiguous 16-bit [n_tokens, heads, D]")
-        need = 4 * t * self.d
-        if self._y is None or self._y.numel() < need:
-            self._y = self._grow(self._y, max(need, 1), torch.uint8, self._torch_stream(stream))
+        y = self._rope_table(db, stream)
         _lib.check(lib().arckv_qkv_rope_to_pool(
             x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d, db.cu_q.data_ptr(),
-            db.seq_lens.data_ptr(), db.plan.n_reqs, float(rope_theta), self._y.data_ptr(), self._y.numel(),
+            db.seq_lens.data_ptr(), db.plan.n_reqs, float(rope_theta), y.data_ptr(), y.numel(),
             q.data_ptr(), self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.num_blocks,
             db.slot_mapping.data_ptr(), self._stream(stream)), "arckv_qkv_rope_to_pool")
 
@@ -330,14 +358,18 @@ class PrefillEngine:
         recorded by the library right before the attention kernel, between it and the split-KV
         combine, and after it.  `lse`: optional fp32 [n_tokens, Hq] that receives
         log sum_j exp(scale q . K[j]) of every row and head (for attention_weights)."""
+        import torch
         shape = (db.n_tokens, self.hq, self.d)
         if self._bad(q, shape) or self._bad(out, shape):
             raise ValueError(f"q / out must be contiguous 16-bit {shape}")
         if lse is not None:
             self._check_lse(db, lse)
+        ws = self._ws
+        if self._captured(db) and db.ws_bytes:
+            ws = torch.empty(db.ws_bytes, dtype=torch.uint8, device=self.device)
         args = (db.block_tables.data_ptr(), int(db.block_tables.shape[1]), db.cu_q.data_ptr(), db.seq_lens.data_ptr(),
                 db.plan.n_reqs, db.n_tokens, self.num_blocks, db.work_ptr, db.n_work, db.n_combine, db.tile_cols,
-                self.hq, self.hkv, self.d, self.scale, self._ws.data_ptr() if db.ws_bytes else None, db.ws_bytes)
+                self.hq, self.hkv, self.d, self.scale, ws.data_ptr() if db.ws_bytes else None, db.ws_bytes)
         qo = (q.data_ptr(), out.data_ptr())
         if self.kv_format == "mx4":
             if events is not None:
@@ -371,6 +403,7 @@ class PrefillEngine:
         self._check_lse(db, lse)
         n = db.plan.n_reqs
         self._check_weights(n, weights)
+        self._captured(db)
         mx4 = self.kv_format == "mx4"
         self._call("arckv_attention_weights", stream, (self.kv_pool if mx4 else self.k_pool).data_ptr(),
                    _lib.LAYOUT_MX4 if mx4 else _lib.LAYOUT_V1, q.data_ptr(), lse.data_ptr(), db.block_tables.data_ptr(),
