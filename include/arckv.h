@@ -549,7 +549,7 @@ int32_t arckv_prefill_attention_mx4(const void* kv_pool, const void* q, void* ou
  * may be shared with other requests and are only read).  The session then attends with the
  * destination blocks as its block table and the kept number of tokens as its length: the causal
  * rule needs only that its new tokens come last (rotated keys keep the position they were rotated
- * for, so a producer goes on with the true positions).
+ * for, so the producer goes on with the true positions: its seq_lens are the prompts' true lengths).
  * ------------------------------------------------------------------------------------- */
 
 /* weights[r][h][j] += (accumulate 0: =) sum over the new tokens of request r and the query heads of

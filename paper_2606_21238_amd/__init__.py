@@ -109,6 +109,8 @@ class BatchPlan:
     slot_mapping: np.ndarray   # int32 [n_slots]
     max_q_len: int
     max_seq_len: int
+    true_lens: np.ndarray | None = None   # int32 [n_reqs]: prompt lengths that the producer's positions go by, where
+                                          # the cache holds fewer tokens than that (sessions that were cut)
 
     @property
     def n_reqs(self) -> int:

@@ -39,6 +39,7 @@ class DeviceBatch:
     tile_cols: int
     n_tokens: int = 0          # computed (suffix) tokens of the batch: rows of q / k_new / v_new
     work_ptr: int = 0          # device address of the work array
+    true_lens: object = None   # of plan.true_lens: the lengths that project() counts positions by (None: seq_lens)
 
 
 class PrefillEngine:
@@ -142,6 +143,10 @@ class PrefillEngine:
         ts = self._torch_stream(stream)
         ap = attention_plan(plan.cu_q, plan.seq_lens, self.hq, self.hkv, self.d, self.num_cus)
         parts = [plan.block_tables.ravel(), plan.cu_q, plan.seq_lens, plan.slot_mapping, ap.work.ravel()]
+        if plan.true_lens is not None:
+            if len(plan.true_lens) != plan.n_reqs:
+                raise ValueError("true_lens must hold one length per request")
+            parts.append(plan.true_lens)
         n_int = sum(p.size for p in parts)
         t = self._turn
         self._turn = (t + 1) % self._ring
@@ -163,10 +168,42 @@ class PrefillEngine:
         cu = dev[o:o + n + 1]; o += n + 1
         sl = dev[o:o + n]; o += n
         sm = dev[o:o + len(plan.slot_mapping)]; o += len(plan.slot_mapping)
-        wk = dev[o:o + ap.work.size].view(-1, 8)
+        wk = dev[o:o + ap.work.size].view(-1, 8); o += ap.work.size
         self._ensure_ws(ap.ws_bytes, ts)
         return DeviceBatch(plan, bt, cu, sl, sm, wk, ap.n_work, ap.n_combine, ap.ws_bytes, ap.tile_cols,
-                           int(plan.cu_q[-1]), wk.data_ptr())
+                           int(plan.cu_q[-1]), wk.data_ptr(), None if plan.true_lens is None else dev[o:o + n])
+
+    def resume(self, tables, held, new, true_lens, stream=None) -> DeviceBatch:
+        """The next batch of sessions that evict() cut: request r holds held[r] tokens in the private blocks
+        tables[r] and computes new[r] more behind them, which are the last of the true_lens[r] tokens of
+        its prompt: project() rotates them for those positions, as the held ones were for theirs.
+        Host integers, tables [n_reqs, >= ceil((held + new) / 16) of the longest]."""
+        tables, held, new, true_lens = (np.asarray(x) for x in (tables, held, new, true_lens))
+        n = len(held)
+        if tables.ndim != 2 or any(x.ndim != 1 for x in (held, new, true_lens)) or \
+                not len(tables) == n == len(new) == len(true_lens):
+            raise ValueError("tables must be [n_reqs, blocks], held, new and true_lens [n_reqs]")
+        if any(x.size and x.dtype.kind not in "iu" for x in (tables, held, new, true_lens)):
+            raise ValueError("tables and lengths must hold integers")
+        held, new, true_lens = (x.astype(np.int64) for x in (held, new, true_lens))
+        seq = held + new
+        if n and (min(held.min(), new.min()) < 0 or (true_lens < seq).any() or true_lens.max() > np.iinfo(np.int32).max):
+            raise ValueError("a session has no fewer tokens than it holds and computes: 0 <= held, new; held + new <= true_lens")
+        blocks = -(-seq // 16)
+        if n and blocks.max() > tables.shape[1]:
+            raise ValueError(f"tables must have {int(blocks.max())} blocks for the longest session")
+        used = np.arange(tables.shape[1]) < blocks[:, None]
+        if used.any() and (tables[used].min() < self.num_phys or tables[used].max() >= self.num_blocks):
+            raise ValueError(f"tables must name private blocks, {self.num_phys} to {self.num_blocks - 1}")
+        bt = np.where(used, tables, -1).astype(np.int32)
+        at = [np.arange(h, s) for h, s in zip(held, seq)]
+        slots = [bt[r, i // 16].astype(np.int64) * 16 + i % 16 for r, i in enumerate(at)]
+        slots = np.concatenate([*slots, np.zeros(0, np.int64)])
+        if len(np.unique(slots)) < len(slots):
+            raise ValueError("tables let two sessions write one slot")
+        i32 = [x.astype(np.int32) for x in (np.concatenate([[0], np.cumsum(new)]), seq, held, held // 16, slots, true_lens)]
+        plan = BatchPlan(bt, *i32[:5], int(new.max(initial=0)), int(seq.max(initial=0)), i32[5])
+        return self.upload(plan, stream)
 
     # ---- streams ---------------------------------------------------------------------------
     # `stream` is None (torch's current stream), a torch.cuda.Stream or a raw hipStream_t
@@ -314,9 +351,14 @@ class PrefillEngine:
         self._call("arckv_kv_gather_mx4", stream, self.kv_pool.data_ptr(), k_out.data_ptr(), v_out.data_ptr(),
                    slots.data_ptr(), shape[0], self.num_blocks, self.hkv, self.d)
 
+    @staticmethod
+    def _position_lens(db: DeviceBatch) -> int:
+        return (db.seq_lens if db.true_lens is None else db.true_lens).data_ptr()
+
     def project(self, db: DeviceBatch, x, w_qkv, q, k_new, v_new, rope_theta: float, stream=None):
         """Q/K/V of the batch's computed tokens from their hidden states x [n_tokens, H]
-        (projection by w_qkv [(Hq + 2 Hkv) D, H] and rotary embedding, arckv_qkv_rope);
+        (projection by w_qkv [(Hq + 2 Hkv) D, H] and rotary embedding, arckv_qkv_rope), rotated for the
+        last positions of each request (of its true length, where the batch has them);
         k_new / v_new then go to scatter()."""
         t, h = db.n_tokens, int(x.shape[1])
         n_out = (self.hq + 2 * self.hkv) * self.d
@@ -328,7 +370,7 @@ class PrefillEngine:
                 raise ValueError("q / k_new / v_new must be contiguous 16-bit [n_tokens, heads, D]")
         y = self._rope_table(db, stream)
         _lib.check(lib().arckv_qkv_rope(x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
-                                        db.cu_q.data_ptr(), db.seq_lens.data_ptr(), db.plan.n_reqs,
+                                        db.cu_q.data_ptr(), self._position_lens(db), db.plan.n_reqs,
                                         float(rope_theta), y.data_ptr(), y.numel(),
                                         q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), self._stream(stream)),
                    "arckv_qkv_rope")
@@ -348,7 +390,7 @@ class PrefillEngine:
         y = self._rope_table(db, stream)
         _lib.check(lib().arckv_qkv_rope_to_pool(
             x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d, db.cu_q.data_ptr(),
-            db.seq_lens.data_ptr(), db.plan.n_reqs, float(rope_theta), y.data_ptr(), y.numel(),
+            self._position_lens(db), db.plan.n_reqs, float(rope_theta), y.data_ptr(), y.numel(),
             q.data_ptr(), self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.num_blocks,
             db.slot_mapping.data_ptr(), self._stream(stream)), "arckv_qkv_rope_to_pool")
 
@@ -422,7 +464,8 @@ class PrefillEngine:
         longest request]).  Their K and V move into the blocks of dst_tables (host int32 [n_reqs, >=
         ceil(keep / 16)]: private blocks of the caller's, num_phys and up, none twice and none of them a
         block of the batch).  Returns (kept positions int32 [n_reqs, Hkv, keep], -1 behind a shorter request's;
-        their weights, fp32).  Afterwards request r holds min(L_r, keep) tokens in dst_tables[r].  The
+        their weights, fp32).  Afterwards request r holds min(L_r, keep) tokens in dst_tables[r], and goes on
+        by resume().  The
         batch must not have been released, and the stream must not be capturing (a graph takes
         evict_select and kv_compact, with tables on the device)."""
         import torch
