@@ -58,7 +58,7 @@ class PrefillEngine:
             raise ValueError("private_blocks must not be negative")
         self.hq, self.hkv, self.d = num_q_heads, num_kv_heads, head_dim
         self.scale = head_dim ** -0.5
-        self.device = torch.device(device)
+        self.device = self._device_of(device)
         self.num_phys = num_phys
         self.num_blocks = num_phys + private_blocks
         self.kv_format = kv_format
@@ -90,6 +90,15 @@ class PrefillEngine:
         # the stream (handle) of the last call: first the one that the pools are being filled on
         self._last = _current_stream(self.device.index) if self.device.type == "cuda" else None
         self._many = False      # whether there has been a second one
+
+    @staticmethod
+    def _device_of(device):
+        """With its index: the engine stays on the device that is current now, whichever is later."""
+        import torch
+        device = torch.device(device)
+        if device.type == "cuda" and device.index is None:
+            device = torch.device("cuda", torch.cuda.current_device())
+        return device
 
     # ---- host steps ----------------------------------------------------------------------
     def plan(self, token_lists) -> BatchPlan:
@@ -290,15 +299,15 @@ class PrefillEngine:
         with torch.cuda.stream(ts):
             return torch.empty(n, dtype=dtype, device=self.device)
 
-    def _call(self, name: str, stream, *args):
+    def _call(self, name: str, stream, *args, events=()):
         """A library call on the engine's device (made the current one if it is not) and `stream`."""
         import torch
         index = self.device.index
         if index is None or index == torch.cuda.current_device():
-            _lib.check(getattr(lib(), name)(*args, self._stream(stream)), name)
+            _lib.check(getattr(lib(), name)(*args, self._stream(stream), *events), name)
         else:
             with torch.cuda.device(index):
-                _lib.check(getattr(lib(), name)(*args, self._stream(stream)), name)
+                _lib.check(getattr(lib(), name)(*args, self._stream(stream), *events), name)
 
     @staticmethod
     def _bad(t, shape, size: int = 2) -> bool:
@@ -369,11 +378,9 @@ class PrefillEngine:
             if tuple(a.shape) != (t, c, self.d) or not a.is_contiguous() or a.element_size() != 2:
                 raise ValueError("q / k_new / v_new must be contiguous 16-bit [n_tokens, heads, D]")
         y = self._rope_table(db, stream)
-        _lib.check(lib().arckv_qkv_rope(x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
-                                        db.cu_q.data_ptr(), self._position_lens(db), db.plan.n_reqs,
-                                        float(rope_theta), y.data_ptr(), y.numel(),
-                                        q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), self._stream(stream)),
-                   "arckv_qkv_rope")
+        self._call("arckv_qkv_rope", stream, x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
+                   db.cu_q.data_ptr(), self._position_lens(db), db.plan.n_reqs, float(rope_theta), y.data_ptr(), y.numel(),
+                   q.data_ptr(), k_new.data_ptr(), v_new.data_ptr())
 
     def project_to_pool(self, db: DeviceBatch, x, w_qkv, q, rope_theta: float, stream=None):
         """project() with the KV scatter fused in (arckv_qkv_rope_to_pool): Q into q, the batch's
@@ -388,11 +395,9 @@ class PrefillEngine:
         if tuple(q.shape) != (t, self.hq, self.d) or not q.is_contiguous() or q.element_size() != 2:
             raise ValueError("q must be contiguous 16-bit [n_tokens, heads, D]")
         y = self._rope_table(db, stream)
-        _lib.check(lib().arckv_qkv_rope_to_pool(
-            x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d, db.cu_q.data_ptr(),
-            self._position_lens(db), db.plan.n_reqs, float(rope_theta), y.data_ptr(), y.numel(),
-            q.data_ptr(), self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.num_blocks,
-            db.slot_mapping.data_ptr(), self._stream(stream)), "arckv_qkv_rope_to_pool")
+        self._call("arckv_qkv_rope_to_pool", stream, x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
+                   db.cu_q.data_ptr(), self._position_lens(db), db.plan.n_reqs, float(rope_theta), y.data_ptr(), y.numel(),
+                   q.data_ptr(), self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.num_blocks, db.slot_mapping.data_ptr())
 
     def attention(self, db: DeviceBatch, q, out, stream=None, events=None, lse=None):
         """Attention of the batch over the engine's pools.  `events` (bf16 pools): optional (begin,
@@ -423,9 +428,7 @@ class PrefillEngine:
         if events is not None:
             if lse is not None:
                 raise ValueError("the timed call writes no lse")
-            _lib.check(lib().arckv_prefill_attention_timed(*pools, *qo, *args, self._stream(stream),
-                                                           *(e.cuda_event for e in events)),
-                       "arckv_prefill_attention_timed")
+            self._call("arckv_prefill_attention_timed", stream, *pools, *qo, *args, events=[e.cuda_event for e in events])
         elif lse is not None:
             self._call("arckv_prefill_attention_lse", stream, *pools, *qo, lse.data_ptr(), *args)
         else:
