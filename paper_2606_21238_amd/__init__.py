@@ -396,10 +396,10 @@ def kv_scatter(k_pool, v_pool, k_new, v_new, slot_mapping, stream=None):
         raise ValueError("pools must be [blocks, Hkv, 16, D] (K) and [blocks, Hkv, D, 16] (V)")
     if slot_mapping.numel() != n:
         raise ValueError("slot_mapping must hold one slot per token")
-    _lib.check(lib().arckv_kv_scatter(_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"),
-                                      _dev(k_new, 16, "k_new"), _dev(v_new, 16, "v_new"),
-                                      _dev(slot_mapping, 32, "slot_mapping"), int(k_new.shape[0]), nb,
-                                      hkv, d, C.c_void_p(_stream(stream))), "arckv_kv_scatter")
+    args = (_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"), _dev(k_new, 16, "k_new"), _dev(v_new, 16, "v_new"),
+            _dev(slot_mapping, 32, "slot_mapping"), n, nb, hkv, d)
+    with _on(stream, k_pool, v_pool, k_new, v_new, slot_mapping) as st:
+        _lib.check(lib().arckv_kv_scatter(*args, st), "arckv_kv_scatter")
 
 
 def mx4_pool_bytes(num_blocks: int, num_kv_heads: int, head_dim: int) -> int:
@@ -448,12 +448,12 @@ def qkv_rope(x, w_qkv, cu_q, seq_lens, num_q_heads: int, num_kv_heads: int, rope
         raise ValueError("q_out / k_out / v_out shapes do not match x and the head counts")
     if cu_q.numel() != seq_lens.numel() + 1:
         raise ValueError("cu_q must have len(seq_lens) + 1 entries")
-    _lib.check(lib().arckv_qkv_rope(
-        _dev(x, 16, "x"), _dev(w_qkv, 16, "w_qkv"), t, h, num_q_heads, num_kv_heads, d,
-        _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), int(seq_lens.numel()), float(rope_theta),
-        _dev(workspace, None, "workspace"), int(workspace.numel() * workspace.element_size()),
-        _dev(q_out, 16, "q_out"), _dev(k_out, 16, "k_out"), _dev(v_out, 16, "v_out"),
-        C.c_void_p(_stream(stream))), "arckv_qkv_rope")
+    args = (_dev(x, 16, "x"), _dev(w_qkv, 16, "w_qkv"), t, h, num_q_heads, num_kv_heads, d,
+            _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), int(seq_lens.numel()), float(rope_theta),
+            _dev(workspace, None, "workspace"), int(workspace.numel() * workspace.element_size()),
+            _dev(q_out, 16, "q_out"), _dev(k_out, 16, "k_out"), _dev(v_out, 16, "v_out"))
+    with _on(stream, x, w_qkv, cu_q, seq_lens, workspace, q_out, k_out, v_out) as st:
+        _lib.check(lib().arckv_qkv_rope(*args, st), "arckv_qkv_rope")
 
 
 def qkv_rope_to_pool(x, w_qkv, cu_q, seq_lens, num_q_heads: int, num_kv_heads: int, rope_theta: float,
@@ -473,12 +473,13 @@ def qkv_rope_to_pool(x, w_qkv, cu_q, seq_lens, num_q_heads: int, num_kv_heads: i
         raise ValueError("k_pool / v_pool must be layout V1 with matching heads and head_dim")
     if slot_mapping.numel() != t or cu_q.numel() != seq_lens.numel() + 1:
         raise ValueError("slot_mapping must have one slot per token, cu_q len(seq_lens) + 1 entries")
-    _lib.check(lib().arckv_qkv_rope_to_pool(
-        _dev(x, 16, "x"), _dev(w_qkv, 16, "w_qkv"), t, h, num_q_heads, num_kv_heads, d,
-        _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), int(seq_lens.numel()), float(rope_theta),
-        _dev(workspace, None, "workspace"), int(workspace.numel() * workspace.element_size()),
-        _dev(q_out, 16, "q_out"), _dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"), nb,
-        _dev(slot_mapping, 32, "slot_mapping"), C.c_void_p(_stream(stream))), "arckv_qkv_rope_to_pool")
+    args = (_dev(x, 16, "x"), _dev(w_qkv, 16, "w_qkv"), t, h, num_q_heads, num_kv_heads, d,
+            _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), int(seq_lens.numel()), float(rope_theta),
+            _dev(workspace, None, "workspace"), int(workspace.numel() * workspace.element_size()),
+            _dev(q_out, 16, "q_out"), _dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"), nb,
+            _dev(slot_mapping, 32, "slot_mapping"))
+    with _on(stream, x, w_qkv, cu_q, seq_lens, workspace, q_out, k_pool, v_pool, slot_mapping) as st:
+        _lib.check(lib().arckv_qkv_rope_to_pool(*args, st), "arckv_qkv_rope_to_pool")
 
 
 @dataclass
@@ -574,13 +575,12 @@ def prefill_attention(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work
     args = _attention_args(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work, n_work, n_combine,
                            tile_cols, scale)
     ws = _workspace(workspace, ws_bytes)
-    if lse is None:
-        _lib.check(lib().arckv_prefill_attention(*args, ws, int(ws_bytes), C.c_void_p(_stream(stream))),
-                   "arckv_prefill_attention")
-        return
     with _on(stream, k_pool, v_pool, q, out, lse, block_tables, cu_q, seq_lens, work, workspace) as st:
-        _lib.check(lib().arckv_prefill_attention_lse(*args[:4], _lse(lse, q), *args[4:], ws, int(ws_bytes), st),
-                   "arckv_prefill_attention_lse")
+        if lse is None:
+            _lib.check(lib().arckv_prefill_attention(*args, ws, int(ws_bytes), st), "arckv_prefill_attention")
+        else:
+            _lib.check(lib().arckv_prefill_attention_lse(*args[:4], _lse(lse, q), *args[4:], ws, int(ws_bytes), st),
+                       "arckv_prefill_attention_lse")
 
 
 def prefill_attention_mx4(kv_pool, q, out, block_tables, cu_q, seq_lens, work, n_work: int, n_combine: int,
@@ -604,8 +604,8 @@ def prefill_attention_noalloc(k_pool, v_pool, q, out, block_tables, cu_q, seq_le
     in time on one device must not be issued (they share the scratch)."""
     args = _attention_args(k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work, n_work, n_combine,
                            tile_cols, scale)
-    _lib.check(lib().arckv_prefill_attention_noalloc(*args, int(ws_bytes), C.c_void_p(_stream(stream))),
-               "arckv_prefill_attention_noalloc")
+    with _on(stream, k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, work) as st:
+        _lib.check(lib().arckv_prefill_attention_noalloc(*args, int(ws_bytes), st), "arckv_prefill_attention_noalloc")
 
 
 # ------------------------------------------------------------------------------------------
