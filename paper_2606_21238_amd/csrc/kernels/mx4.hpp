@@ -5,7 +5,7 @@
 // format of the OCP Microscaling specification).  The scale is the smallest power of two for
 // which the group's largest magnitude is at most 7 times it (up to 7 rounds to 6): over normal,
 // heavy-tailed and uniform groups that leaves a root-mean-square error of 11.2, 12.9 and 9.9 % of
-// the values', against 11.5, 13.9 and 9.9 % for "at most 6" and 11.5, 13.1 and 14.4 % for the
+// the values', against 11.5, 13.9 and 9.9 % for "at most 6" and 11.5, 13.1 and 14.1 % for the
 // specification's floor rule.  b stays in [2, 252], so that every value a code stands for
 // is a normal bf16 number or zero: a stored value is exact in bf16, and attention over the cache
 // rounds nothing more than attention over bf16 rows does.  A group with an infinity or a NaN has

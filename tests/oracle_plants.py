@@ -125,6 +125,24 @@ PLANTS = [
      "v = rope(y[:, nq + nk:nq + 2 * nk].reshape(t, num_kv_heads, head_dim), positions, theta)", None),
     ("positions_from_zero", "oracle/qkv.py", "out.append(np.arange(int(seq_lens[r]) - s, int(seq_lens[r])))",
      "out.append(np.arange(0, s))", None),
+    # ---- 4-bit cache (oracle/mx4.py)
+    ("mx4_at_most_6", "oracle/mx4.py", "top > 7 * 2.0 ** (k - 1)", "top > 6 * 2.0 ** (k - 1)", None),
+    ("mx4_under_7", "oracle/mx4.py", "top > 7 * 2.0 ** (k - 1)", "top >= 7 * 2.0 ** (k - 1)", None),
+    ("mx4_smallest_scale", "oracle/mx4.py", "e = np.full(top.shape, -125)", "e = np.full(top.shape, -126)", None),
+    ("mx4_largest_scale", "oracle/mx4.py", "for k in range(-124, 126):", "for k in range(-124, 127):", None),
+    ("mx4_ties_down", "oracle/mx4.py", "(i % 2 == 1), i + 1, i)", "(i % 2 == 1), i, i)", None),
+    ("mx4_ties_up", "oracle/mx4.py", "(nearest.sum(axis=-1) == 2) & (i % 2 == 1)", "(nearest.sum(axis=-1) == 2)", None),
+    ("mx4_sign_lost", "oracle/mx4.py", "code = i + 8 * np.signbit(g)", "code = i", None),
+    ("mx4_infinity_kept", "oracle/mx4.py", "bad = ~np.isfinite(g).all(axis=-1)", "bad = np.isnan(g).any(axis=-1)", None),
+    ("mx4_scale_bias", "oracle/mx4.py", "astype(np.float64) - 127)", "astype(np.float64) - 126)", None),
+    ("mx4_nan_scale_is_a_number", "oracle/mx4.py", "    v = np.where(scale_bytes[..., None] == 255, np.nan, v)\n", "", None),
+    ("mx4_halves_of_a_byte", "oracle/mx4.py", "kp[0, :, o] = code[:, 0::2] | code[:, 1::2] << 4",
+     "kp[0, :, o] = code[:, 1::2] | code[:, 0::2] << 4", None),
+    ("mx4_v_token_order", "oracle/mx4.py", "vp[0, :, o // 8, :, o % 8] = ", "vp[0, :, o % 2, :, o // 2] = ", None),
+    ("mx4_v_scale_order", "oracle/mx4.py", "vs[0, :, :, o] = byte", "vs[0, :, :, 15 - o] = byte", None),
+    ("mx4_scales_swapped", "oracle/mx4.py", "for x in (kp, vp, ks, vs)]", "for x in (kp, vp, vs, ks)]", None),
+    ("mx4_gather_halves", "oracle/mx4.py", "np.stack([x & 15, x >> 4], axis=-1)", "np.stack([x >> 4, x & 15], axis=-1)", None),
+    ("mx4_gather_v_half", "oracle/mx4.py", "v = values(codes(vp[b, :, o // 8, :, o % 8])", "v = values(codes(vp[b, :, 1 - o // 8, :, o % 8])", None),
 ]
 
 
