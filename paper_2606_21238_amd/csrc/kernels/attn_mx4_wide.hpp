@@ -7,7 +7,7 @@
 // loaded in M(j) for tile j + 3, and in M(j + 1) writes them as bf16 into the stage of that tile, between
 // the MFMAs.  (Codes in LDS and decoded by each wave for its own 32 columns would be 8 times the
 // conversions: about 1.6 times the MFMAs' own time.)  LDS then holds what the bf16 kernel's does, in
-// the same swizzled places.
+// the same swizzled places.  Probabilities are rounded to bf16 for P.V, as in the narrow kernel.
 //
 // What bounds it is the matrix units with the conversions beside them: 2048 tokens on 32768, 64 / 8 heads of
 // 128, 1.91 to 1.98 ms (1.15 to 1.19 PFLOP/s; the bf16 kernel 1.79, a large matrix product's rate 1.71).

@@ -10,10 +10,12 @@
 // and the barriers between, 24 to 26 us there; 512 ragged rows of up to 4096, two to a unit: 20 us.
 // kv_compact: the kept tokens' K and V into other blocks, position i of the result from position
 // kept[i]; a head's tokens move on their own, so the same slot may hold another token for another
-// head.  A work-group writes one block (4 bits: four) of one head.  The bound is the lines it reads, not the tokens: V has a token
-// every 32 bytes (4 bits: every 8), so of 1 token kept in 2 nearly every line of V comes in, and half of
-// K's.  64 requests of about 2600 down to 1024, 8 heads of 128: 92 us for 332 MB read and 132 written (5.05 TB/s).
-// 4 requests of 32768 down to 8192 at 4 bits: 24.8 us for 66 and 18 MB (3.4 TB/s), in pieces of lines.
+// head.  A work-group writes one block (4 bits: four) of one head.  The bound is the lines it reads, not the tokens: a line
+// of V is 4 dimensions of a block's 16 tokens (4 bits: 32 dimensions of 8 tokens), and comes in where one of them is kept.
+// 64 requests of 192 to 16272 (2600 on average) down to 512, 1 token in 5, 8 heads of 128: four fifths of V's lines, 273 MB
+// by that count, beside the kept rows of K, 66: 92 us for the 332 MB that are read and 132 written (5.05 TB/s).
+// 4 requests of 32768 down to 4096, 1 in 8, at 4 bits: two thirds of V's lines and a quarter of K's, of which two tokens
+// share one: 24.8 us for 66 and 18 MB (3.4 TB/s), gathered byte by byte.
 #pragma once
 
 #include "mx4.hpp"
@@ -275,7 +277,7 @@ __global__ __launch_bounds__(256) void kv_compact_kernel(
 }
 
 // A block has few bytes in 4 bits: a work-group takes 4, whose loads are in flight together (one block each:
-// 27.5 us for 4 requests of 32768 down to 8192).
+// 27.5 us for 4 requests of 32768 down to 4096).
 constexpr int kMoveBlocks = 4;
 
 template <int D>
