@@ -89,7 +89,8 @@ class PrefillEngine:
         self._turn = 0
         # the stream (handle) of the last call: first the one that the pools are being filled on
         self._last = _current_stream(self.device.index) if self.device.type == "cuda" else None
-        self._many = False      # whether there has been a second one
+        self._done = None       # an event behind all it has queued, where there is one
+        self._home = {}         # of a buffer's address: the stream that it was allocated on
 
     @staticmethod
     def _device_of(device):
@@ -220,8 +221,9 @@ class PrefillEngine:
     # that stream, the stream the kernels then run on: the kernels are ordered after the copy.
     # The pools, the workspaces and the metadata ring are one set for all streams, so an engine's
     # work runs in the order of its calls: a call on another stream than the call before makes
-    # its stream wait for what that one has queued (a raw handle stays valid until then).  A
-    # stream under capture waits for nothing (torch.cuda.graph starts a capture with the device idle).
+    # its stream wait for what that one has queued.  The event for that is recorded when the stream
+    # changes; of a raw handle, which its owner may have destroyed by then, behind every call.  A stream
+    # under capture waits for nothing (torch.cuda.graph starts a capture with the device idle).
     def _torch_stream(self, stream):
         import torch
         if stream is None:
@@ -242,28 +244,38 @@ class PrefillEngine:
     def _in_order(self, handle: int):
         if handle != self._last:
             self._change_stream(handle)
+        else:
+            self._done = None
 
     def _change_stream(self, handle: int):
+        if self._capturing(handle):
+            return
+        if self._done is None and self._last is not None:
+            if self._capturing(self._last):
+                return
+            self._mark(self._last)
+        if self._done is not None:
+            self._handle(handle).wait_event(self._done)
+        self._last, self._done = handle, None
+
+    def _handle(self, handle: int):
         import torch
+        return torch.cuda.ExternalStream(handle, device=self.device) if handle else torch.cuda.default_stream(self.device)
 
-        def of(h):
-            return torch.cuda.ExternalStream(h, device=self.device) if h else torch.cuda.default_stream(self.device)
+    def _capturing(self, handle: int) -> bool:
+        import torch
+        with torch.cuda.stream(self._handle(handle)):
+            return torch.cuda.is_current_stream_capturing()
 
-        for h in (handle, self._last):
-            if h is not None:
-                with torch.cuda.stream(of(h)):
-                    if torch.cuda.is_current_stream_capturing():
-                        return
-        if self._last is not None:
-            done = torch.cuda.Event()
-            done.record(of(self._last))
-            of(handle).wait_event(done)
-            self._many = True
-        self._last = handle
+    def _mark(self, handle: int):
+        import torch
+        self._done = torch.cuda.Event()
+        self._done.record(self._handle(handle))
 
     # Calls may be captured by torch.cuda.graph.  A replay reads the metadata and writes the workspaces that were
     # captured, while the engine goes on with other batches and other graphs: so a captured call's
     # workspace is the graph's own memory, and the ring lets go of its batch's buffer (the batch keeps it).
+    # A replay is the caller's work, who orders it with the engine's calls on the same blocks.
     @staticmethod
     def _not_captured(name: str):
         import torch
@@ -294,10 +306,12 @@ class PrefillEngine:
         back to the order of the stream that it was allocated on.  That stream may be another, and knows
         nothing of what ts has queued: then the host waits for it."""
         import torch
-        if old is not None and old.numel() and self._many:
+        if old is not None and self._home.pop(old.data_ptr(), ts.cuda_stream) != ts.cuda_stream:
             ts.synchronize()
         with torch.cuda.stream(ts):
-            return torch.empty(n, dtype=dtype, device=self.device)
+            new = torch.empty(n, dtype=dtype, device=self.device)
+        self._home[new.data_ptr()] = ts.cuda_stream
+        return new
 
     def _call(self, name: str, stream, *args, events=()):
         """A library call on the engine's device (made the current one if it is not) and `stream`."""
@@ -308,6 +322,8 @@ class PrefillEngine:
         else:
             with torch.cuda.device(index):
                 _lib.check(getattr(lib(), name)(*args, self._stream(stream), *events), name)
+        if isinstance(stream, int) and not self._capturing(stream):
+            self._mark(stream)
 
     @staticmethod
     def _bad(t, shape, size: int = 2) -> bool:
@@ -323,7 +339,7 @@ class PrefillEngine:
             dev.copy_(self._stage[t][:n_int], non_blocking=True)
             ev = torch.cuda.Event()
             ev.record(ts)
-        self._stage_ev[t] = ev
+        self._stage_ev[t] = self._done = ev
         return dev
 
     def _ensure_ws(self, nbytes: int, ts):

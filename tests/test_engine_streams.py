@@ -99,6 +99,11 @@ def world(monkeypatch):
 
 
 def attend(w, stream):
+    """stream: None, a number (of a torch stream), or "raw" and a handle."""
+    if isinstance(stream, tuple):
+        stream = stream[1]
+    elif stream is not None:
+        stream = torch.cuda.Stream(stream)
     w.eng.attention(w.db, Tensor(5, HQ, D), Tensor(5, HQ, D), stream=stream)
 
 
@@ -129,7 +134,7 @@ def test_every_kind_of_call_takes_part(world):
     for n, call in enumerate(calls):
         attend(world, 100 + n)
         world.log.clear()
-        call(200 + n)
+        call(torch.cuda.Stream(200 + n))
         (kind, ev, old), wait, rest = world.log[0], world.log[1], world.log[2:]
         assert (kind, old) == ("record", 100 + n) and wait == ("wait", 200 + n, ev)
         assert [e[2] for e in rest] == [200 + n]
@@ -139,19 +144,24 @@ def test_a_buffer_is_replaced_once_every_stream_is_done_with_it(world):
     """Its memory goes back to the order of the stream that it was allocated on, which may not be the last user's:
     the host waits first.  With one stream alone that order is enough."""
     eng = world.eng
+    on = {n: torch.cuda.Stream(n) for n in (11, 22, 33)}
     attend(world, 11)
-    eng._ensure_ws(8192, eng._torch_stream(11))
-    assert eng._ws.numel() == 8192 and ("host waits", 11) not in world.log
+    eng._ensure_ws(8192, eng._torch_stream(on[11]))
+    eng._ensure_ws(8193, eng._torch_stream(on[11]))
+    assert eng._ws.numel() == 8193 and ("host waits", 11) not in world.log
     attend(world, 22)
-    eng._ensure_ws(9000, eng._torch_stream(22))
+    eng._ensure_ws(9000, eng._torch_stream(on[22]))
     assert eng._ws.numel() == 9000 and world.log[-1] == ("host waits", 22)
+    attend(world, 11)
+    eng._ensure_ws(9001, eng._torch_stream(on[22]))                     # 22 waits for 11 in its own order
+    assert ("host waits", 22) not in world.log[-3:]
     rows, q = Tensor(5, HKV, D), Tensor(5, HQ, D)
     for _ in range(2):
-        eng.project(world.db, Tensor(5, 32), Tensor((HQ + 2 * HKV) * D, 32), q, rows, rows, 1e4, stream=33)
+        eng.project(world.db, Tensor(5, 32), Tensor((HQ + 2 * HKV) * D, 32), q, rows, rows, 1e4, stream=on[33])
     assert ("host waits", 33) not in world.log               # the first table replaces none
-    eng._y = torch.zeros(1, dtype=torch.uint8)
-    eng.project_to_pool(world.db, Tensor(5, 32), Tensor((HQ + 2 * HKV) * D, 32), q, 1e4, stream=33)
-    assert ("host waits", 33) in world.log
+    eng._y = eng._y[:1]                                      # too small now
+    eng.project_to_pool(world.db, Tensor(5, 32), Tensor((HQ + 2 * HKV) * D, 32), q, 1e4, stream=on[22])
+    assert ("host waits", 22) in world.log
 
 
 def test_a_capturing_stream_waits_for_nothing(world):
@@ -171,3 +181,21 @@ def test_a_stream_that_is_captured_meanwhile_is_not_waited_for(world):
     world.log.clear()
     attend(world, 22)
     assert world.log == [("call", "arckv_prefill_attention", 22)]
+
+
+def test_a_raw_handle_is_not_touched_after_its_call(world):
+    """Its owner may have destroyed it: the event is there already when the stream changes."""
+    call = "arckv_prefill_attention"
+    attend(world, ("raw", 11))
+    attend(world, ("raw", 11))
+    attend(world, 22)
+    assert world.log == [("call", call, 11), ("record", 1, 11), ("call", call, 11), ("record", 2, 11), ("wait", 22, 2), ("call", call, 22)]
+    world.log.clear()
+    attend(world, ("raw", 22))           # the same stream by its handle
+    attend(world, 22)                    # what follows has no event yet
+    attend(world, 33)
+    assert world.log == [("call", call, 22), ("record", 3, 22), ("call", call, 22), ("record", 4, 22), ("wait", 33, 4), ("call", call, 33)]
+    world.capturing.add(44)
+    world.log.clear()
+    attend(world, ("raw", 44))           # an event of a capture is of no use outside it
+    assert world.log == [("call", call, 44)]

@@ -65,26 +65,28 @@ def test_two_split_batches_on_two_streams(fmt):
     rows = [[0, 1, 2], [3, 4, 5]]
     qs = [randn_bf16((3, HQ, D), 5 + k) for k in range(2)]
 
-    def run(streams, rounds):
+    def run(streams, rounds, raw=False):
         """Both batches `rounds` times in turn, the second one's longer for more rounds than the ring is deep."""
         res = []
         for k in range(rounds):
             for x, st in enumerate(streams):
-                db = eng.upload(batch([lens[r] - k for r in rows[x]], [1] * 3, tables[rows[x]]), stream=st)
+                given = st.cuda_stream if raw else st
+                db = eng.upload(batch([lens[r] - k for r in rows[x]], [1] * 3, tables[rows[x]]), stream=given)
                 assert db.n_combine > 0 and db.ws_bytes > 0
                 out, lse = torch.full_like(qs[x], float("nan")), torch.full((3, HQ), float("nan"), device=DEV)
                 if st is not None:
                     st.wait_stream(torch.cuda.current_stream())        # `out` and `lse` are filled
                     with torch.cuda.stream(st):
                         busy(1 + k % 2)
-                eng.attention(db, qs[x], out, stream=st, lse=lse)
+                eng.attention(db, qs[x], out, stream=given, lse=lse)
                 res += [out, lse]
         torch.cuda.synchronize()
         return res
 
     want = run([None, None], 7)
-    for streams in ([torch.cuda.Stream(), torch.cuda.Stream()], [None, torch.cuda.Stream()]):
-        got = run(streams, 7)
+    two = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for streams, raw in ((two, False), ([None, torch.cuda.Stream()], False), (two, True)):
+        got = run(streams, 7, raw)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
 
 
