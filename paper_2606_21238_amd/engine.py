@@ -387,11 +387,10 @@ class PrefillEngine:
         k_new / v_new then go to scatter()."""
         t, h = db.n_tokens, int(x.shape[1])
         n_out = (self.hq + 2 * self.hkv) * self.d
-        if tuple(x.shape) != (t, h) or tuple(w_qkv.shape) != (n_out, h) or x.element_size() != 2 or \
-                not (x.is_contiguous() and w_qkv.is_contiguous()):
+        if self._bad(x, (t, h)) or self._bad(w_qkv, (n_out, h)):
             raise ValueError(f"x must be contiguous 16-bit [{t}, H] and w_qkv [{n_out}, H]")
         for a, c in ((q, self.hq), (k_new, self.hkv), (v_new, self.hkv)):
-            if tuple(a.shape) != (t, c, self.d) or not a.is_contiguous() or a.element_size() != 2:
+            if self._bad(a, (t, c, self.d)):
                 raise ValueError("q / k_new / v_new must be contiguous 16-bit [n_tokens, heads, D]")
         y = self._rope_table(db, stream)
         self._call("arckv_qkv_rope", stream, x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
@@ -405,10 +404,9 @@ class PrefillEngine:
             raise ValueError("project_to_pool writes bf16 pools: a 4-bit pool takes project() and scatter()")
         t, h = db.n_tokens, int(x.shape[1])
         n_out = (self.hq + 2 * self.hkv) * self.d
-        if tuple(x.shape) != (t, h) or tuple(w_qkv.shape) != (n_out, h) or x.element_size() != 2 or \
-                not (x.is_contiguous() and w_qkv.is_contiguous()):
+        if self._bad(x, (t, h)) or self._bad(w_qkv, (n_out, h)):
             raise ValueError(f"x must be contiguous 16-bit [{t}, H] and w_qkv [{n_out}, H]")
-        if tuple(q.shape) != (t, self.hq, self.d) or not q.is_contiguous() or q.element_size() != 2:
+        if self._bad(q, (t, self.hq, self.d)):
             raise ValueError("q must be contiguous 16-bit [n_tokens, heads, D]")
         y = self._rope_table(db, stream)
         self._call("arckv_qkv_rope_to_pool", stream, x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
