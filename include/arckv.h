@@ -598,6 +598,52 @@ int32_t arckv_kv_compact_mx4(void* kv_pool, const int32_t* block_tables, int32_t
                              int32_t dst_stride, int32_t n_reqs, int64_t num_blocks,
                              int32_t num_kv_heads, int32_t head_dim, void* stream);
 
+/* ---------------------------------------------------------------------------------------
+ * Device: a decode loop that stays on the device.  Between two steps nothing comes from the host: the maps
+ * of a step are made from the requests' lengths where they are, so that whole steps can be captured into a
+ * graph and replayed while the requests grow.
+ * ------------------------------------------------------------------------------------- */
+
+/* The norm in front of the producer.  h = x + residual (fp32; without a residual h = x), residual_out = h as
+ * bf16, y = h / sqrt(mean(h^2) + eps) * weight (fp32, of the unrounded h), and out as out_format says:
+ *   ARCKV_OUT_BF16  out: bf16 [n_tokens][hidden], y rounded to nearest even;
+ *   ARCKV_OUT_E4M3  out: 8-bit floats (E4M3 without infinities) [n_tokens][hidden], scales: fp32 [n_tokens],
+ *                   scale = max|y| / 448 over the row, out = y / scale rounded to nearest even (0 where scale is 0).
+ * A row with a NaN or an infinity gives what these formulas give (its scale may be NaN, its codes 0x7F).
+ * x: device bf16, rows x_stride elements apart (x_stride >= hidden).  residual and residual_out: device bf16
+ * [n_tokens][hidden], both or neither; weight: device bf16 [hidden].  residual_out may be residual or (x_stride =
+ * hidden) x, a bf16 out may be any of them that residual_out is not; no other overlap.  Rows may start at
+ * any bf16 address and hidden may be odd (hidden a multiple of 8 and 16-byte aligned rows run faster); scales 4-byte
+ * aligned.  hidden at most 32768 (EUNSUPPORTED), n_tokens at most 2^31 - 1; n_tokens = 0 is a no-op.  h^2 is summed
+ * in fp32, so h beyond 1e18 gives a y of 0. */
+#define ARCKV_OUT_BF16 0
+#define ARCKV_OUT_E4M3 1
+int32_t arckv_add_rms_norm(const void* x, int64_t x_stride, const void* residual, void* residual_out,
+                           const void* weight, int64_t n_tokens, int32_t hidden, float eps, void* out,
+                           int32_t out_format, float* scales, void* stream);
+
+/* The maps of a step.  Request r holds held[r] tokens and wants new_tokens[r] more.  It needs a block for every
+ * table entry from ceil(held / 16) up to ceil((held + new) / 16); these are taken from the top of the stack
+ * free_blocks[0 .. *free_count) (its last entry first), in the order of the requests and of their tokens.  With B and W the
+ * sums of the blocks and tokens wanted by the requests up to it (those below that can never have theirs left out),
+ * request r gets all its tokens where W <= slot_cap and (B <= *free_count or it needs no block); otherwise none, and
+ * its entries stay.  A request whose new_tokens or held is negative or whose tokens pass 16 bt_stride or 2^31 - 1
+ * gets none either.
+ * Written: seq_lens[r] = held[r] + what it got; cu_q [n_reqs + 1], the running sums of what they got; the new entries
+ * of block_tables [n_reqs][bt_stride]; slot_mapping[t] for t < cu_q[n_reqs] (-1 where the table's block is outside
+ * [0, num_blocks)), and -1 from there up to slot_cap, so that a producer or scatter over slot_cap rows stores
+ * the step's tokens only; *free_left, the number of blocks that stay on the stack; where true_lens is given, true_lens[r] =
+ * seq_lens[r] + true_offset[r] (the lengths by which a producer counts the positions of cut sessions).
+ * All device int32; free_blocks has free_cap entries (a larger *free_count counts as free_cap, a negative one as 0).
+ * seq_lens may be held and free_left may be free_count: a replayed step then goes on from the last one.  One launch
+ * for small steps, two for large ones, nothing allocated.  EINVAL on bad sizes (n_reqs at most 2^24, slot_cap at most 2^30,
+ * num_blocks in [1, 2^27]) or NULL (slot_mapping may be NULL if slot_cap is 0, free_blocks if free_cap is 0). */
+int32_t arckv_batch_maps(const int32_t* new_tokens, const int32_t* held, int32_t n_reqs, int32_t* block_tables,
+                         int32_t bt_stride, const int32_t* free_blocks, int64_t free_cap,
+                         const int32_t* free_count, int32_t* free_left, int32_t* cu_q, int32_t* seq_lens,
+                         const int32_t* true_offset, int32_t* true_lens, int32_t* slot_mapping, int64_t slot_cap,
+                         int64_t num_blocks, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -690,3 +690,71 @@ def kv_compact_mx4(kv_pool, block_tables, kept, dst_tables, stream=None):
     args = _compact_args(block_tables, kept, dst_tables, nb, hkv, row // 17)
     with _on(stream, kv_pool, block_tables, kept, dst_tables) as st:
         _lib.check(lib().arckv_kv_compact_mx4(_dev(kv_pool, 8, "kv_pool"), *args, st), "arckv_kv_compact_mx4")
+
+
+# ------------------------------------------------------------------------------------------
+# device: a decode loop that stays on the device
+# ------------------------------------------------------------------------------------------
+
+def _null():
+    return C.c_void_p(0)
+
+
+def add_rms_norm(x, weight, out, eps: float, residual=None, residual_out=None, scales=None, stream=None):
+    """out <- h / sqrt(mean(h^2) + eps) * weight, h = x + residual, which goes to residual_out as bf16 (None:
+    into residual itself).  x bf16 [n, hidden] (rows may lie further apart), weight bf16 [hidden], residual bf16 [n, hidden].
+    out: bf16 [n, hidden]; with scales (fp32 [n]) 8-bit codes (torch.float8_e4m3fn or uint8 [n, hidden]) that
+    stand for code * scale."""
+    if x.dim() != 2:
+        raise ValueError("x must be [n_tokens, hidden]")
+    n, h = int(x.shape[0]), int(x.shape[1])
+    if not x.is_cuda or (x.numel() and int(x.stride(1)) != 1) or x.element_size() != 2 or \
+            any(str(t.dtype) == "torch.float16" for t in (x, weight, out, residual, residual_out) if t is not None):
+        raise ValueError("x must be a bf16 device tensor with the values of a row next to each other")
+    stride = int(x.stride(0)) if n > 1 else h
+    if stride < h:
+        raise ValueError("the rows of x must not overlap")
+    if residual is None and residual_out is not None:
+        raise ValueError("residual_out needs a residual")
+    if residual is not None and residual_out is None:
+        residual_out = residual
+    if tuple(out.shape) != (n, h) or tuple(weight.shape) != (h,) or \
+            any(t is not None and tuple(t.shape) != (n, h) for t in (residual, residual_out)):
+        raise ValueError("residual, residual_out and out must be [n_tokens, hidden], weight [hidden]")
+    if scales is not None and int(scales.numel()) != n:
+        raise ValueError("scales must hold one scale per row")
+    args = (C.c_void_p(x.data_ptr()), stride, _null() if residual is None else _dev(residual, 16, "residual"),
+            _null() if residual_out is None else _dev(residual_out, 16, "residual_out"), _dev(weight, 16, "weight"), n, h,
+            float(eps), _dev(out, 16 if scales is None else 8, "out"), _lib.OUT_BF16 if scales is None else _lib.OUT_E4M3,
+            _null() if scales is None else _f32(scales, "scales"))
+    with _on(stream, x, weight, out, residual, residual_out, scales) as st:
+        _lib.check(lib().arckv_add_rms_norm(*args, st), "arckv_add_rms_norm")
+
+
+def batch_maps(new_tokens, held, block_tables, free_blocks, free_count, cu_q, seq_lens, slot_mapping, free_left,
+               num_blocks: int, true_offset=None, true_lens=None, stream=None):
+    """The maps of a step, from device int32 tensors: request r holds held[r] tokens and gets new_tokens[r] more, whose
+    blocks come from the top of the stack free_blocks[:free_count] (in request order; one that does not fit gets
+    none).  Written: seq_lens [n], cu_q [n + 1], the new entries of block_tables [n, stride], slot_mapping (-1 behind the
+    step's tokens), free_left [1] and true_lens = seq_lens + true_offset (both or neither).  seq_lens may be held,
+    free_left may be free_count."""
+    n = int(held.numel())
+    if block_tables.dim() != 2 or int(block_tables.shape[0]) != n or new_tokens.numel() != n or seq_lens.numel() != n \
+            or cu_q.numel() != n + 1:
+        raise ValueError("new_tokens, held and seq_lens must be [n], block_tables [n, stride] and cu_q [n + 1]")
+    if free_count.numel() != 1 or free_left.numel() != 1:
+        raise ValueError("free_count and free_left must hold one number")
+    if (true_offset is None) != (true_lens is None) or \
+            any(t is not None and t.numel() != n for t in (true_offset, true_lens)):
+        raise ValueError("true_offset and true_lens must be [n], both or neither")
+    ints = dict(new_tokens=new_tokens, held=held, block_tables=block_tables, free_blocks=free_blocks, free_count=free_count,
+                free_left=free_left, cu_q=cu_q, seq_lens=seq_lens, true_offset=true_offset, true_lens=true_lens,
+                slot_mapping=slot_mapping)
+    if any(t is not None and t.is_floating_point() for t in ints.values()):
+        raise ValueError("the maps are int32")
+    p = {k: _null() if t is None else _dev(t, 32, k) for k, t in ints.items()}
+    with _on(stream, *ints.values()) as st:
+        _lib.check(lib().arckv_batch_maps(p["new_tokens"], p["held"], n, p["block_tables"], int(block_tables.shape[1]),
+                                          p["free_blocks"], int(free_blocks.numel()), p["free_count"], p["free_left"],
+                                          p["cu_q"], p["seq_lens"], p["true_offset"], p["true_lens"], p["slot_mapping"],
+                                          int(slot_mapping.numel()), int(num_blocks), st), "arckv_batch_maps")

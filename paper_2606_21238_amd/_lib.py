@@ -15,6 +15,7 @@ POLICY = {"arc": 0, "lru": 1, "dbl": 2, "frc": 3}
 REF_ORDER = {"tail_first": 0, "head_first": 1}
 WORK_INTS = 8
 LAYOUT_V1, LAYOUT_MX4 = 1, 2
+OUT_BF16, OUT_E4M3 = 0, 1
 CHECK_SLOT, CHECK_BLOCK, CHECK_WORK = 1, 2, 4
 
 i32, i64, u64, f32, f64, vp = C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_double, C.c_void_p
@@ -87,6 +88,8 @@ _SIGS = {
     "arckv_evict_select": (i32, [vp, i64, vp, i32, i32, i32, i32, i32, vp, vp, i64, vp]),
     "arckv_kv_compact": (i32, [vp, vp, vp, i32, vp, i32, vp, i32, i32, i64, i32, i32, vp]),
     "arckv_kv_compact_mx4": (i32, [vp, vp, i32, vp, i32, vp, i32, i32, i64, i32, i32, vp]),
+    "arckv_add_rms_norm": (i32, [vp, i64, vp, vp, vp, i64, i32, f32, vp, i32, vp, vp]),
+    "arckv_batch_maps": (i32, [vp, vp, i32, vp, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, i64, vp]),
     "arckv_mx4_pool_bytes": (i64, [i64, i32, i32]),
     "arckv_kv_scatter_mx4": (i32, [vp, vp, vp, vp, i64, i64, i32, i32, vp]),
     "arckv_kv_gather_mx4": (i32, [vp, vp, vp, vp, i64, i64, i32, i32, vp]),

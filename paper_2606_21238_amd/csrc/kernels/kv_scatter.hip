@@ -216,3 +216,4 @@ extern "C" int32_t arckv_kv_scatter(void* k_pool, void* v_pool, const void* k_ne
 
 #include "kv_mx4.hpp"
 #include "kv_evict.hpp"
+#include "batch_maps.hpp"

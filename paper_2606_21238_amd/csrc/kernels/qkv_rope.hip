@@ -768,3 +768,5 @@ extern "C" int32_t arckv_qkv_rope_to_pool(const void* x, const void* w_qkv, int6
                          cu_q, seq_lens, n_reqs, rope_theta, workspace, ws_bytes, q_out, k_pool, v_pool, true,
                          num_blocks, slot_mapping, stream);
 }
+
+#include "add_rms_norm.hpp"
