@@ -644,6 +644,44 @@ int32_t arckv_batch_maps(const int32_t* new_tokens, const int32_t* held, int32_t
                          const int32_t* true_offset, int32_t* true_lens, int32_t* slot_mapping, int64_t slot_cap,
                          int64_t num_blocks, void* stream);
 
+/* Attention of a batch whose requests share long prefixes, each read once for all of its requests.  What it
+ * computes is what arckv_prefill_attention computes (the same softmax over all of a request's keys [0, j]); only the
+ * order of the sums differs.  Requests group_start[g] .. group_start[g + 1] - 1 (in order, groups apart) are group g, and its
+ * requests hold the same first prefix_lens[g] tokens: their table rows name the same blocks for them.  Of these the
+ * whole tiles of 64 keys that every row of the group sees are read through the first request's table, for all rows at
+ * once; the rest, and requests in no group, go through their own tables.
+ * No host plan: shared_prefix_plan writes the work items on the device, from lengths on the device (once a
+ * step; layers share it), so that a captured step holds while the requests grow.  What the host has to know are bounds:
+ * max_q, the rows of q (cu_q[n_reqs] may be less); max_group_q, the most rows of a group, and max_new, of a request (a step that
+ * passes these two is right, but slower); bt_stride.  The three calls of a step take the same bounds, heads and num_cus. */
+
+/* Ints of the plan and bytes of the workspace for these bounds (host only). */
+int32_t arckv_shared_prefix_sizes(int32_t n_reqs, int32_t n_groups, int64_t max_q, int64_t max_group_q,
+                                  int64_t max_new, int32_t bt_stride, int32_t num_q_heads,
+                                  int32_t num_kv_heads, int32_t head_dim, int32_t num_cus,
+                                  int64_t* plan_ints, int64_t* ws_bytes);
+
+/* The plan of a step.  group_start [n_groups + 1], prefix_lens [n_groups], cu_q [n_reqs + 1], seq_lens [n_reqs], plan
+ * [plan_ints]: device int32, the plan 16-byte aligned.  0 <= max_group_q, max_new <= max_q <= 2^24, n_groups <=
+ * n_reqs <= 2^20 (else EINVAL); ENOSPC if plan_ints is too small. */
+int32_t arckv_shared_prefix_plan(const int32_t* group_start, const int32_t* prefix_lens, int32_t n_groups,
+                                 const int32_t* cu_q, const int32_t* seq_lens, int32_t n_reqs, int64_t max_q,
+                                 int64_t max_group_q, int64_t max_new, int32_t bt_stride,
+                                 int32_t num_q_heads, int32_t num_kv_heads, int32_t head_dim,
+                                 int32_t num_cus, int32_t* plan, int64_t plan_ints, void* stream);
+
+/* The attention.  Pools (layout V1), q, out, tables, head counts, scale and what out-of-range table entries do as for
+ * arckv_prefill_attention; lse (may be NULL) as for arckv_prefill_attention_lse.  Rows of q and out: max_q, of which
+ * those behind cu_q[n_reqs] are neither read nor written.  workspace: device, 16-byte aligned, ws_bytes as
+ * arckv_shared_prefix_sizes says (ENOSPC); calls that overlap in time must not share it.  num_blocks in [1, 2^27]. */
+int32_t arckv_shared_prefix_attention(const void* k_pool, const void* v_pool, const void* q, void* out,
+                                      float* lse, const int32_t* block_tables, int32_t bt_stride,
+                                      const int32_t* cu_q, const int32_t* seq_lens, int32_t n_reqs,
+                                      int32_t n_groups, int64_t max_q, int64_t max_group_q, int64_t max_new,
+                                      int64_t num_blocks, int32_t num_q_heads, int32_t num_kv_heads,
+                                      int32_t head_dim, int32_t num_cus, float scale, const int32_t* plan,
+                                      void* workspace, int64_t ws_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

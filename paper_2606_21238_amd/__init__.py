@@ -758,3 +758,71 @@ def batch_maps(new_tokens, held, block_tables, free_blocks, free_count, cu_q, se
                                           p["free_blocks"], int(free_blocks.numel()), p["free_count"], p["free_left"],
                                           p["cu_q"], p["seq_lens"], p["true_offset"], p["true_lens"], p["slot_mapping"],
                                           int(slot_mapping.numel()), int(num_blocks), st), "arckv_batch_maps")
+
+
+@dataclass(frozen=True)
+class SharedBounds:
+    """What the host knows of a step's batch before it is made: the sizes that the three shared_prefix calls of a step
+    have in common.  max_q: rows of q; max_group_q: most rows of a group, max_new: of a request (a step that passes
+    these two is right, but slower)."""
+    n_reqs: int
+    n_groups: int
+    max_q: int
+    max_group_q: int
+    max_new: int
+    bt_stride: int
+    num_q_heads: int
+    num_kv_heads: int
+    head_dim: int
+    num_cus: int = 256
+
+    def heads(self):
+        return self.num_q_heads, self.num_kv_heads, self.head_dim, self.num_cus
+
+
+def shared_prefix_sizes(b: SharedBounds):
+    """(ints of the plan, bytes of the workspace) of the shared_prefix calls with these bounds."""
+    ints, ws = _lib.i64(), _lib.i64()
+    _lib.check(lib().arckv_shared_prefix_sizes(b.n_reqs, b.n_groups, b.max_q, b.max_group_q, b.max_new, b.bt_stride, *b.heads(),
+                                               C.byref(ints), C.byref(ws)), "arckv_shared_prefix_sizes")
+    return int(ints.value), int(ws.value)
+
+
+def shared_prefix_plan(b: SharedBounds, group_start, prefix_lens, cu_q, seq_lens, plan, stream=None):
+    """The work of a step's shared_prefix_attention calls into `plan`, from lengths on the device: group g is requests
+    group_start[g] .. group_start[g + 1] - 1, whose first prefix_lens[g] tokens lie in the same blocks."""
+    if group_start.numel() != b.n_groups + 1 or prefix_lens.numel() != b.n_groups:
+        raise ValueError("group_start must be [n_groups + 1] and prefix_lens [n_groups]")
+    if cu_q.numel() != b.n_reqs + 1 or seq_lens.numel() != b.n_reqs:
+        raise ValueError("cu_q must be [n_reqs + 1] and seq_lens [n_reqs]")
+    ints = dict(group_start=group_start, prefix_lens=prefix_lens, cu_q=cu_q, seq_lens=seq_lens, plan=plan)
+    if any(t.is_floating_point() for t in ints.values()):
+        raise ValueError("groups, lengths and the plan are int32")
+    p = {k: _dev(t, 32, k) for k, t in ints.items()}
+    with _on(stream, *ints.values()) as st:
+        _lib.check(lib().arckv_shared_prefix_plan(p["group_start"], p["prefix_lens"], b.n_groups, p["cu_q"], p["seq_lens"], b.n_reqs,
+                                                  b.max_q, b.max_group_q, b.max_new, b.bt_stride, *b.heads(), p["plan"],
+                                                  int(plan.numel()), st), "arckv_shared_prefix_plan")
+
+
+def shared_prefix_attention(b: SharedBounds, k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, plan, scale: float, workspace,
+                            lse=None, stream=None):
+    """prefill_attention of a step planned by shared_prefix_plan, each group's shared keys read once for all of its rows.
+    q / out [max_q, Hq, D] bf16 (rows behind cu_q[-1] are left as they are), lse (optional) fp32 [max_q, Hq]."""
+    hq, hkv, d, _ = b.heads()
+    nb = int(k_pool.shape[0])
+    if tuple(k_pool.shape) != (nb, hkv, 16, d) or tuple(v_pool.shape) != (nb, hkv, d, 16):
+        raise ValueError("pools must be [blocks, Hkv, 16, D] (K) and [blocks, Hkv, D, 16] (V)")
+    if tuple(q.shape) != (b.max_q, hq, d) or tuple(out.shape) != (b.max_q, hq, d):
+        raise ValueError("q and out must be [max_q, Hq, D]")
+    if tuple(block_tables.shape) != (b.n_reqs, b.bt_stride) or cu_q.numel() != b.n_reqs + 1 or seq_lens.numel() != b.n_reqs:
+        raise ValueError("block_tables must be [n_reqs, bt_stride], cu_q [n_reqs + 1] and seq_lens [n_reqs]")
+    ints, ws = shared_prefix_sizes(b)
+    if plan.numel() < ints:
+        raise ValueError(f"plan must have {ints} entries")
+    args = (_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"), _dev(q, 16, "q"), _dev(out, 16, "out"), _lse(lse, q),
+            _dev(block_tables, 32, "block_tables"), b.bt_stride, _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), b.n_reqs,
+            b.n_groups, b.max_q, b.max_group_q, b.max_new, nb, *b.heads(), float(scale), _dev(plan, 32, "plan"),
+            _workspace(workspace, ws), int(workspace.numel() * workspace.element_size()))
+    with _on(stream, k_pool, v_pool, q, out, lse, block_tables, cu_q, seq_lens, plan, workspace) as st:
+        _lib.check(lib().arckv_shared_prefix_attention(*args, st), "arckv_shared_prefix_attention")

@@ -90,6 +90,10 @@ _SIGS = {
     "arckv_kv_compact_mx4": (i32, [vp, vp, i32, vp, i32, vp, i32, i32, i64, i32, i32, vp]),
     "arckv_add_rms_norm": (i32, [vp, i64, vp, vp, vp, i64, i32, f32, vp, i32, vp, vp]),
     "arckv_batch_maps": (i32, [vp, vp, i32, vp, i32, vp, i64, vp, vp, vp, vp, vp, vp, vp, i64, i64, vp]),
+    "arckv_shared_prefix_sizes": (i32, [i32, i32, i64, i64, i64, i32, i32, i32, i32, i32, P_i64, P_i64]),
+    "arckv_shared_prefix_plan": (i32, [vp, vp, i32, vp, vp, i32, i64, i64, i64, i32, i32, i32, i32, i32, vp, i64, vp]),
+    "arckv_shared_prefix_attention": (i32, [vp, vp, vp, vp, vp, vp, i32, vp, vp, i32, i32, i64, i64, i64, i64, i32, i32,
+                                            i32, i32, f32, vp, vp, i64, vp]),
     "arckv_mx4_pool_bytes": (i64, [i64, i32, i32]),
     "arckv_kv_scatter_mx4": (i32, [vp, vp, vp, vp, i64, i64, i32, i32, vp]),
     "arckv_kv_gather_mx4": (i32, [vp, vp, vp, vp, i64, i64, i32, i32, vp]),

@@ -1558,3 +1558,4 @@ extern "C" int32_t arckv_prefill_attention_noalloc(
 
 #include "attn_mx4.hpp"
 #include "attn_weights.hpp"
+#include "shared_attn.hpp"

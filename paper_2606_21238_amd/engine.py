@@ -6,6 +6,8 @@ computed tokens' K/V -> prefix-cached prefill attention -> release.
 kv_format="mx4" holds K and V in 4 bits and runs the same steps over them; gather() reads rows back.
 attention_weights() after attention(lse=) adds up what every cached token received, evict() moves
 the heaviest tokens into blocks that the caller owns.
+step_batch() takes running requests over to the device: advance() then makes each step's maps and plan there, and
+shared_attention() reads prefixes that requests share once, so whole steps can be captured into a graph and replayed.
 Every step is a libarckv call; this class owns the device buffers (PyTorch tensors used
 only as device memory) and the host cache handle.  plan() + upload() are the same first
 steps as separate calls.
@@ -18,7 +20,8 @@ from dataclasses import dataclass
 
 import numpy as np
 
-from . import (BlockCache, BatchPlan, _current_stream, attention_plan, hash_blocks_batch, lib, unpack_prepared)
+from . import (BlockCache, BatchPlan, SharedBounds, _current_stream, attention_plan, hash_blocks_batch, lib,
+               shared_prefix_sizes, unpack_prepared)
 from . import _lib
 
 
@@ -40,6 +43,30 @@ class DeviceBatch:
     n_tokens: int = 0          # computed (suffix) tokens of the batch: rows of q / k_new / v_new
     work_ptr: int = 0          # device address of the work array
     true_lens: object = None   # of plan.true_lens: the lengths that project() counts positions by (None: seq_lens)
+
+
+@dataclass
+class StepPlan:
+    """What the host knows of a StepBatch: the number of its requests."""
+    n_reqs: int
+
+
+@dataclass
+class StepBatch(DeviceBatch):
+    """Running requests whose lengths, tables and maps live on the device (PrefillEngine.step_batch).  n_tokens is the
+    most tokens of a step; rows behind cu_q[-1] belong to no request: their slots are -1.  seq_lens (the tokens
+    held), block_tables, free_blocks, free_count and what else is here may be changed between steps by the caller, in the order of
+    the engine's calls.  Calls for one StepBatch must not overlap in time."""
+    bounds: SharedBounds = None
+    group_start: object = None
+    prefix_lens: object = None
+    free_blocks: object = None
+    free_count: object = None
+    true_offset: object = None
+    work_plan: object = None
+    workspace: object = None
+    home: int = 0              # the stream that its memory was allocated on
+    memory: list = None
 
 
 class PrefillEngine:
@@ -215,6 +242,83 @@ class PrefillEngine:
         plan = BatchPlan(bt, *i32[:5], int(new.max(initial=0)), int(seq.max(initial=0)), i32[5])
         return self.upload(plan, stream)
 
+    def step_batch(self, tables, held, group_sizes, prefix_lens, max_tokens: int, max_new: int | None = None, free_blocks=(),
+                   true_lens=None, stream=None) -> StepBatch:
+        """Running requests for steps that need nothing from the host: request r holds held[r] tokens in the blocks
+        tables[r] (host integers [n_reqs, stride]; entries behind them are room for advance()).  Consecutive requests form
+        groups of group_sizes[g] requests (of all of them, or () for none) whose first prefix_lens[g] tokens are in the same blocks.
+        max_tokens: the most new tokens of a step, max_new: of a request in it (a step that passes that is right, but
+        slower).  free_blocks: private blocks for the tokens to come, the last one is taken first.  true_lens: of cut sessions,
+        as for resume(): project() counts positions by them.
+        The blocks stay the caller's, who keeps them from other requests as long as the steps run (blocks of the block cache: by
+        not releasing their batch); a request's last block, if it is not full, is written and must be its own."""
+        import torch
+        if self.kv_format != "bf16":
+            raise ValueError("step_batch works on bf16 pools")
+        self._not_captured("step_batch")
+        tables, held, sizes, prefix, free = (np.asarray(x) for x in (tables, held, group_sizes, prefix_lens, free_blocks))
+        n = len(held)
+        true = held if true_lens is None else np.asarray(true_lens)
+        if tables.ndim != 2 or any(x.ndim != 1 for x in (held, sizes, prefix, free, true)) or len(tables) != n or \
+                len(sizes) != len(prefix) or len(true) != n:
+            raise ValueError("tables must be [n_reqs, stride], held and true_lens [n_reqs], group_sizes and prefix_lens one per group")
+        if any(x.size and x.dtype.kind not in "iu" for x in (tables, held, sizes, prefix, free, true)):
+            raise ValueError("tables, lengths and blocks must hold integers")
+        tables, held, sizes, prefix, free, true = (x.astype(np.int64) for x in (tables, held, sizes, prefix, free, true))
+        stride = tables.shape[1]
+        if max_tokens < 0 or (max_new is not None and max_new < 0):
+            raise ValueError("max_tokens and max_new must not be negative")
+        if n and (held.min() < 0 or held.max() > 16 * stride or (true < held).any() or true.max() > np.iinfo(np.int32).max):
+            raise ValueError("a request holds 0 <= held <= 16 stride tokens, and no more than its true length")
+        if sizes.size and (sizes.min() < 1 or sizes.sum() != n):
+            raise ValueError("the groups must be of one request or more and hold all requests")
+        used = np.arange(stride) < -(-held // 16)[:, None]
+        named = tables[used]
+        if named.size and (named.min() < 0 or named.max() >= self.num_blocks):
+            raise ValueError("tables names blocks outside the pool")
+        if free.size and (free.min() < self.num_phys or free.max() >= self.num_blocks):
+            raise ValueError(f"free_blocks must be private blocks, {self.num_phys} to {self.num_blocks - 1}")
+        uses = np.bincount(free, minlength=self.num_blocks)
+        if uses.max(initial=0) > 1 or uses[named].any():
+            raise ValueError("free_blocks names a block twice or one that a request holds")
+        open_rows = np.flatnonzero(held % 16)
+        written = tables[open_rows, held[open_rows] // 16]
+        if np.bincount(named, minlength=self.num_blocks)[written].max(initial=0) > 1:
+            raise ValueError("a last block that is not full belongs to two requests")
+        start = np.concatenate([[0], np.cumsum(sizes)]).astype(np.int64)
+        for g, p in enumerate(prefix):
+            rows = slice(start[g], start[g + 1])
+            if p < 0 or p > held[rows].min():
+                raise ValueError(f"group {g} cannot share {p} tokens: one of its requests holds fewer")
+            if (tables[rows, :-(-int(p) // 16)] != tables[start[g], :-(-int(p) // 16)]).any():
+                raise ValueError(f"the requests of group {g} hold their first {p} tokens in different blocks")
+        max_new = max_tokens if max_new is None else min(max_new, max_tokens)
+        bounds = SharedBounds(n, len(sizes), max_tokens, min(max_tokens, int(sizes.max(initial=0)) * max_new), max_new, stride,
+                              self.hq, self.hkv, self.d, self.num_cus)
+        ints, ws_bytes = shared_prefix_sizes(bounds)
+        parts = [np.where(used, tables, -1).ravel(), held, start, prefix, free, [len(free)], true - held]
+        ts = self._torch_stream(stream)
+        with torch.cuda.stream(ts):
+            host = torch.empty(sum(len(p) for p in parts), dtype=torch.int32, pin_memory=True)
+            host.numpy()[:] = np.concatenate(parts)
+            meta = host.to(self.device, non_blocking=True)
+            dev, at = [], 0
+            for p in parts:
+                dev.append(meta[at:at + len(p)])
+                at += len(p)
+            cu, slots = (torch.zeros(k, dtype=torch.int32, device=self.device) for k in (n + 1, max_tokens))
+            slots.fill_(-1)
+            plan = torch.zeros(ints, dtype=torch.int32, device=self.device)
+            ws = torch.empty(ws_bytes, dtype=torch.uint8, device=self.device)
+            lens = None if true_lens is None else torch.empty(n, dtype=torch.int32, device=self.device)
+            self._done = torch.cuda.Event()
+            self._done.record(ts)
+        bt, sl, gs, pl, fb, fc, off = dev
+        return StepBatch(StepPlan(n), bt.view(n, stride), cu, sl, slots, None, 0, 0, ws_bytes, 0, max_tokens, 0, lens, bounds=bounds,
+                         group_start=gs, prefix_lens=pl, free_blocks=fb, free_count=fc,
+                         true_offset=None if true_lens is None else off, work_plan=plan, workspace=ws, home=ts.cuda_stream,
+                         memory=[t for t in (meta, cu, slots, plan, ws, lens) if t is not None])
+
     # ---- streams ---------------------------------------------------------------------------
     # `stream` is None (torch's current stream), a torch.cuda.Stream or a raw hipStream_t
     # handle.  The metadata copy, its event and every (re)allocation of a device buffer run on
@@ -352,6 +456,52 @@ class PrefillEngine:
     # tensor checks and pass raw addresses straight to the C ABI (the library still validates
     # sizes); they only check the shapes of the caller's q / k / v / out.
 
+    def advance(self, sb: StepBatch, new_tokens, stream=None):
+        """The next step of a StepBatch: request r gets new_tokens[r] more tokens (device int32 [n_reqs]; 0 or less: none) where
+        blocks and rows last (arckv_batch_maps).  Afterwards sb.seq_lens, cu_q, block_tables and slot_mapping are the step's,
+        as is the plan of its shared_attention() calls."""
+        b = sb.bounds
+        self._held(sb, stream)
+        if self._bad(new_tokens, (b.n_reqs,), 4) or new_tokens.is_floating_point():
+            raise ValueError(f"new_tokens must be contiguous int32 [{b.n_reqs}] on the device")
+        true = (None, None) if sb.true_lens is None else (sb.true_offset.data_ptr(), sb.true_lens.data_ptr())
+        held, count, cu = sb.seq_lens.data_ptr(), sb.free_count.data_ptr(), sb.cu_q.data_ptr()
+        self._call("arckv_batch_maps", stream, new_tokens.data_ptr(), held, b.n_reqs, sb.block_tables.data_ptr(), b.bt_stride,
+                   sb.free_blocks.data_ptr(), int(sb.free_blocks.numel()), count, count, cu, held, *true, sb.slot_mapping.data_ptr(),
+                   b.max_q, self.num_blocks)
+        self._call("arckv_shared_prefix_plan", stream, sb.group_start.data_ptr(), sb.prefix_lens.data_ptr(), b.n_groups, cu, held,
+                   b.n_reqs, b.max_q, b.max_group_q, b.max_new, b.bt_stride, *b.heads(), sb.work_plan.data_ptr(),
+                   int(sb.work_plan.numel()))
+
+    def shared_attention(self, sb: StepBatch, q, out, lse=None, stream=None):
+        """Attention of a StepBatch's step (q / out [max_tokens, Hq, D]; rows behind cu_q[-1] are left as they are), the
+        prefixes that its groups share read once for all of a group's rows.  lse as for attention()."""
+        shape = (sb.n_tokens, self.hq, self.d)
+        if self._bad(q, shape) or self._bad(out, shape):
+            raise ValueError(f"q / out must be contiguous 16-bit {shape}")
+        if lse is not None:
+            self._check_lse(sb, lse)
+        b = sb.bounds
+        self._held(sb, stream)
+        self._call("arckv_shared_prefix_attention", stream, self.k_pool.data_ptr(), self.v_pool.data_ptr(), q.data_ptr(),
+                   out.data_ptr(), None if lse is None else lse.data_ptr(), sb.block_tables.data_ptr(), b.bt_stride,
+                   sb.cu_q.data_ptr(), sb.seq_lens.data_ptr(), b.n_reqs, b.n_groups, b.max_q, b.max_group_q, b.max_new,
+                   self.num_blocks, *b.heads(), self.scale, sb.work_plan.data_ptr(), sb.workspace.data_ptr(), sb.ws_bytes)
+
+    def _held(self, sb: StepBatch, stream):
+        """A StepBatch's memory, which may be let go of right after a call, is not given away before the call's stream is
+        done with it, where that is not the stream that it was allocated on."""
+        handle = self._stream(stream)
+        if handle != sb.home and not self._capturing(handle):
+            ts = self._handle(handle)
+            for t in sb.memory:
+                t.record_stream(ts)
+
+    @staticmethod
+    def _planned(db: DeviceBatch, name: str):
+        if isinstance(db, StepBatch):
+            raise ValueError(f"{name} takes a batch of prepare(), upload() or resume(), not a StepBatch")
+
     def scatter(self, db: DeviceBatch, k_new, v_new, stream=None):
         shape = (db.n_tokens, self.hkv, self.d)
         if self._bad(k_new, shape) or self._bad(v_new, shape):
@@ -420,6 +570,7 @@ class PrefillEngine:
         combine, and after it.  `lse`: optional fp32 [n_tokens, Hq] that receives
         log sum_j exp(scale q . K[j]) of every row and head (for attention_weights)."""
         import torch
+        self._planned(db, "attention (shared_attention attends for a StepBatch)")
         shape = (db.n_tokens, self.hq, self.d)
         if self._bad(q, shape) or self._bad(out, shape):
             raise ValueError(f"q / out must be contiguous 16-bit {shape}")
@@ -486,6 +637,7 @@ class PrefillEngine:
         batch must not have been released, and the stream must not be capturing (a graph takes
         evict_select and kv_compact, with tables on the device)."""
         import torch
+        self._planned(db, "evict")
         plan, n = db.plan, db.plan.n_reqs
         self._check_weights(n, weights)
         if n and int(weights.shape[2]) < int(plan.seq_lens.max()):
