@@ -696,8 +696,38 @@ def kv_compact_mx4(kv_pool, block_tables, kept, dst_tables, stream=None):
 # device: a decode loop that stays on the device
 # ------------------------------------------------------------------------------------------
 
-def _null():
-    return C.c_void_p(0)
+_BITS = {}
+
+
+def _kinds():
+    """Dtypes by what their bits may be taken for (an integer tensor of that size holds patterns)."""
+    if not _BITS:
+        import torch
+        _BITS.update(bf16=(torch.bfloat16, torch.int16, torch.uint16), f32=(torch.float32,), i32=(torch.int32, torch.uint32),
+                     e4m3=(torch.float8_e4m3fn, torch.uint8, torch.int8))
+    return _BITS
+
+
+def _address(t, kinds, shape, index: int, name: str) -> int:
+    """The address of a contiguous tensor of one of these dtypes, of this shape (None: any) and on device `index`."""
+    if t.dtype not in kinds or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be contiguous {kinds[0]}{'' if shape is None else ' of shape ' + str(tuple(shape))}")
+    if t.get_device() != index:
+        raise ValueError(f"{name}: the tensors of a call must be on one device")
+    return t.data_ptr()
+
+
+def _launch(name: str, index: int, stream, *args):
+    """A library call on device `index` (made the current one if it is not) and `stream`, or that device's current one."""
+    import torch
+    f = getattr(lib(), name)
+    if index == torch.cuda.current_device():
+        status = f(*args, _current_stream(index) if stream is None else stream)
+    else:
+        with torch.cuda.device(index):
+            status = f(*args, _current_stream(index) if stream is None else stream)
+    if status:
+        _lib.check(status, name)
 
 
 def add_rms_norm(x, weight, out, eps: float, residual=None, residual_out=None, scales=None, stream=None):
@@ -705,30 +735,29 @@ def add_rms_norm(x, weight, out, eps: float, residual=None, residual_out=None, s
     into residual itself).  x bf16 [n, hidden] (rows may lie further apart), weight bf16 [hidden], residual bf16 [n, hidden].
     out: bf16 [n, hidden]; with scales (fp32 [n]) 8-bit codes (torch.float8_e4m3fn or uint8 [n, hidden]) that
     stand for code * scale."""
-    if x.dim() != 2:
+    shape, kinds = x.shape, _kinds()
+    if len(shape) != 2:
         raise ValueError("x must be [n_tokens, hidden]")
-    n, h = int(x.shape[0]), int(x.shape[1])
-    if not x.is_cuda or (x.numel() and int(x.stride(1)) != 1) or x.element_size() != 2 or \
-            any(str(t.dtype) == "torch.float16" for t in (x, weight, out, residual, residual_out) if t is not None):
-        raise ValueError("x must be a bf16 device tensor with the values of a row next to each other")
-    stride = int(x.stride(0)) if n > 1 else h
-    if stride < h:
-        raise ValueError("the rows of x must not overlap")
-    if residual is None and residual_out is not None:
+    n, h = shape
+    index, bf16 = x.get_device(), kinds["bf16"]
+    if index < 0 or x.dtype not in bf16:
+        raise ValueError("x must be a bf16 device tensor")
+    row = h
+    if not x.is_contiguous():
+        row = x.stride(0) if n > 1 else h
+        if x.stride(1) != 1 or row < h:
+            raise ValueError("the values of a row of x must be next to each other, and rows must not overlap")
+    res = sums = scale = None
+    if residual is not None:
+        res = _address(residual, bf16, shape, index, "residual")
+        sums = res if residual_out is None else _address(residual_out, bf16, shape, index, "residual_out")
+    elif residual_out is not None:
         raise ValueError("residual_out needs a residual")
-    if residual is not None and residual_out is None:
-        residual_out = residual
-    if tuple(out.shape) != (n, h) or tuple(weight.shape) != (h,) or \
-            any(t is not None and tuple(t.shape) != (n, h) for t in (residual, residual_out)):
-        raise ValueError("residual, residual_out and out must be [n_tokens, hidden], weight [hidden]")
-    if scales is not None and int(scales.numel()) != n:
-        raise ValueError("scales must hold one scale per row")
-    args = (C.c_void_p(x.data_ptr()), stride, _null() if residual is None else _dev(residual, 16, "residual"),
-            _null() if residual_out is None else _dev(residual_out, 16, "residual_out"), _dev(weight, 16, "weight"), n, h,
-            float(eps), _dev(out, 16 if scales is None else 8, "out"), _lib.OUT_BF16 if scales is None else _lib.OUT_E4M3,
-            _null() if scales is None else _f32(scales, "scales"))
-    with _on(stream, x, weight, out, residual, residual_out, scales) as st:
-        _lib.check(lib().arckv_add_rms_norm(*args, st), "arckv_add_rms_norm")
+    fmt = _lib.OUT_BF16
+    if scales is not None:
+        scale, fmt = _address(scales, kinds["f32"], (n,), index, "scales"), _lib.OUT_E4M3
+    _launch("arckv_add_rms_norm", index, stream, x.data_ptr(), row, res, sums, _address(weight, bf16, (h,), index, "weight"), n, h,
+            eps, _address(out, bf16 if scale is None else kinds["e4m3"], shape, index, "out"), fmt, scale)
 
 
 def batch_maps(new_tokens, held, block_tables, free_blocks, free_count, cu_q, seq_lens, slot_mapping, free_left,
@@ -738,26 +767,22 @@ def batch_maps(new_tokens, held, block_tables, free_blocks, free_count, cu_q, se
     none).  Written: seq_lens [n], cu_q [n + 1], the new entries of block_tables [n, stride], slot_mapping (-1 behind the
     step's tokens), free_left [1] and true_lens = seq_lens + true_offset (both or neither).  seq_lens may be held,
     free_left may be free_count."""
-    n = int(held.numel())
-    if block_tables.dim() != 2 or int(block_tables.shape[0]) != n or new_tokens.numel() != n or seq_lens.numel() != n \
-            or cu_q.numel() != n + 1:
-        raise ValueError("new_tokens, held and seq_lens must be [n], block_tables [n, stride] and cu_q [n + 1]")
-    if free_count.numel() != 1 or free_left.numel() != 1:
-        raise ValueError("free_count and free_left must hold one number")
-    if (true_offset is None) != (true_lens is None) or \
-            any(t is not None and t.numel() != n for t in (true_offset, true_lens)):
-        raise ValueError("true_offset and true_lens must be [n], both or neither")
-    ints = dict(new_tokens=new_tokens, held=held, block_tables=block_tables, free_blocks=free_blocks, free_count=free_count,
-                free_left=free_left, cu_q=cu_q, seq_lens=seq_lens, true_offset=true_offset, true_lens=true_lens,
-                slot_mapping=slot_mapping)
-    if any(t is not None and t.is_floating_point() for t in ints.values()):
-        raise ValueError("the maps are int32")
-    p = {k: _null() if t is None else _dev(t, 32, k) for k, t in ints.items()}
-    with _on(stream, *ints.values()) as st:
-        _lib.check(lib().arckv_batch_maps(p["new_tokens"], p["held"], n, p["block_tables"], int(block_tables.shape[1]),
-                                          p["free_blocks"], int(free_blocks.numel()), p["free_count"], p["free_left"],
-                                          p["cu_q"], p["seq_lens"], p["true_offset"], p["true_lens"], p["slot_mapping"],
-                                          int(slot_mapping.numel()), int(num_blocks), st), "arckv_batch_maps")
+    if len(held.shape) != 1 or len(block_tables.shape) != 2:
+        raise ValueError("held must be [n] and block_tables [n, stride]")
+    i32, index, per = _kinds()["i32"], held.get_device(), held.shape
+    if index < 0:
+        raise ValueError("held must be a device tensor")
+    n, stride = per[0], block_tables.shape[1]
+    if (true_offset is None) != (true_lens is None):
+        raise ValueError("true_offset and true_lens go together")
+    offset = None if true_offset is None else _address(true_offset, i32, per, index, "true_offset")
+    true = None if true_lens is None else _address(true_lens, i32, per, index, "true_lens")
+    _launch("arckv_batch_maps", index, stream, _address(new_tokens, i32, per, index, "new_tokens"),
+            _address(held, i32, per, index, "held"), n, _address(block_tables, i32, (n, stride), index, "block_tables"), stride,
+            _address(free_blocks, i32, None, index, "free_blocks"), free_blocks.numel(),
+            _address(free_count, i32, (1,), index, "free_count"), _address(free_left, i32, (1,), index, "free_left"),
+            _address(cu_q, i32, (n + 1,), index, "cu_q"), _address(seq_lens, i32, per, index, "seq_lens"), offset, true,
+            _address(slot_mapping, i32, None, index, "slot_mapping"), slot_mapping.numel(), num_blocks)
 
 
 @dataclass(frozen=True)
@@ -796,13 +821,12 @@ def shared_prefix_plan(b: SharedBounds, group_start, prefix_lens, cu_q, seq_lens
     if cu_q.numel() != b.n_reqs + 1 or seq_lens.numel() != b.n_reqs:
         raise ValueError("cu_q must be [n_reqs + 1] and seq_lens [n_reqs]")
     ints = dict(group_start=group_start, prefix_lens=prefix_lens, cu_q=cu_q, seq_lens=seq_lens, plan=plan)
-    if any(t.is_floating_point() for t in ints.values()):
-        raise ValueError("groups, lengths and the plan are int32")
-    p = {k: _dev(t, 32, k) for k, t in ints.items()}
-    with _on(stream, *ints.values()) as st:
-        _lib.check(lib().arckv_shared_prefix_plan(p["group_start"], p["prefix_lens"], b.n_groups, p["cu_q"], p["seq_lens"], b.n_reqs,
-                                                  b.max_q, b.max_group_q, b.max_new, b.bt_stride, *b.heads(), p["plan"],
-                                                  int(plan.numel()), st), "arckv_shared_prefix_plan")
+    index = plan.get_device()
+    if index < 0:
+        raise ValueError("plan must be a device tensor")
+    p = {k: _address(t, _kinds()["i32"], None, index, k) for k, t in ints.items()}
+    _launch("arckv_shared_prefix_plan", index, stream, p["group_start"], p["prefix_lens"], b.n_groups, p["cu_q"], p["seq_lens"],
+            b.n_reqs, b.max_q, b.max_group_q, b.max_new, b.bt_stride, *b.heads(), p["plan"], plan.numel())
 
 
 def shared_prefix_attention(b: SharedBounds, k_pool, v_pool, q, out, block_tables, cu_q, seq_lens, plan, scale: float, workspace,
@@ -813,16 +837,21 @@ def shared_prefix_attention(b: SharedBounds, k_pool, v_pool, q, out, block_table
     nb = int(k_pool.shape[0])
     if tuple(k_pool.shape) != (nb, hkv, 16, d) or tuple(v_pool.shape) != (nb, hkv, d, 16):
         raise ValueError("pools must be [blocks, Hkv, 16, D] (K) and [blocks, Hkv, D, 16] (V)")
-    if tuple(q.shape) != (b.max_q, hq, d) or tuple(out.shape) != (b.max_q, hq, d):
-        raise ValueError("q and out must be [max_q, Hq, D]")
-    if tuple(block_tables.shape) != (b.n_reqs, b.bt_stride) or cu_q.numel() != b.n_reqs + 1 or seq_lens.numel() != b.n_reqs:
-        raise ValueError("block_tables must be [n_reqs, bt_stride], cu_q [n_reqs + 1] and seq_lens [n_reqs]")
+    if cu_q.numel() != b.n_reqs + 1 or seq_lens.numel() != b.n_reqs:
+        raise ValueError("cu_q must be [n_reqs + 1] and seq_lens [n_reqs]")
+    kinds, index, rows = _kinds(), q.get_device(), (b.max_q, hq, d)
+    if index < 0:
+        raise ValueError("q must be a device tensor")
     ints, ws = shared_prefix_sizes(b)
-    if plan.numel() < ints:
-        raise ValueError(f"plan must have {ints} entries")
-    args = (_dev(k_pool, 16, "k_pool"), _dev(v_pool, 16, "v_pool"), _dev(q, 16, "q"), _dev(out, 16, "out"), _lse(lse, q),
-            _dev(block_tables, 32, "block_tables"), b.bt_stride, _dev(cu_q, 32, "cu_q"), _dev(seq_lens, 32, "seq_lens"), b.n_reqs,
-            b.n_groups, b.max_q, b.max_group_q, b.max_new, nb, *b.heads(), float(scale), _dev(plan, 32, "plan"),
-            _workspace(workspace, ws), int(workspace.numel() * workspace.element_size()))
-    with _on(stream, k_pool, v_pool, q, out, lse, block_tables, cu_q, seq_lens, plan, workspace) as st:
-        _lib.check(lib().arckv_shared_prefix_attention(*args, st), "arckv_shared_prefix_attention")
+    if plan.numel() < ints or workspace.numel() * workspace.element_size() < ws:
+        raise ValueError(f"plan must have {ints} entries and the workspace {ws} bytes")
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise ValueError("workspace must be contiguous, on the device of the call's tensors")
+    bf16, i32 = kinds["bf16"], kinds["i32"]
+    _launch("arckv_shared_prefix_attention", index, stream, _address(k_pool, bf16, None, index, "k_pool"),
+            _address(v_pool, bf16, None, index, "v_pool"), _address(q, bf16, rows, index, "q"), _address(out, bf16, rows, index, "out"),
+            None if lse is None else _address(lse, kinds["f32"], (b.max_q, hq), index, "lse"),
+            _address(block_tables, i32, (b.n_reqs, b.bt_stride), index, "block_tables"), b.bt_stride,
+            _address(cu_q, i32, None, index, "cu_q"), _address(seq_lens, i32, None, index, "seq_lens"), b.n_reqs, b.n_groups, b.max_q,
+            b.max_group_q, b.max_new, nb, *b.heads(), scale, _address(plan, i32, None, index, "plan"), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size())

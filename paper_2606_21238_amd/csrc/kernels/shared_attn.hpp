@@ -17,8 +17,8 @@
 namespace {
 
 constexpr int kTailCols = 16;             // columns of an item of the tail kernel
-constexpr int kTailThreads = 256;
-constexpr int kTailPerUnit = 4;           // tail work-groups that a compute unit holds at a time
+constexpr int kTailPerUnit = 3;           // tail work-groups (of four waves) that a compute unit holds at a time
+constexpr int kTailWhole = 1024;          // own keys of a request that are not cut
 constexpr int kPlanThreads = 1024;
 constexpr int kMaxPieceTiles = arckv::kMaxItemKeys / kBK;
 
@@ -29,11 +29,14 @@ struct SharedSizes {
   int64_t off_group, off_req, off_row, off_cu, off_len, off_work_p, off_work_o, n_ints;
   int64_t ws_floats;
 };
-// plan entries of a group / of a request: pieces are [i len, (i + 1) len) tiles of 64 keys from the part's start
+// Plan entry of a group / of a request.  Its units are (column tile, head) pairs, head fastest; the first `whole` of them
+// have pieces_w pieces of len_w tiles of 64 keys, the others `pieces` of `len`, from the part's first key on.  Slots, from
+// `base`: the whole units piece by piece, then the others piece by piece.
 struct Part {
-  int32_t base, pieces, len, tiles, row0, rows, keys0, keys1;   // first slot; pieces; tiles of a piece; column tiles;
-};                                                               // first row; rows; the part's keys [keys0, keys1)
-static_assert(sizeof(Part) == 32, "eight ints");
+  int32_t base, tiles, whole, pieces_w, len_w, pieces, len, row0, rows, keys0, keys1, group;
+};
+constexpr int kPartInts = 12;
+static_assert(sizeof(Part) == kPartInts * sizeof(int32_t), "twelve ints");
 
 SharedSizes shared_sizes(int64_t n_reqs, int64_t n_groups, int64_t max_q, int64_t max_group_q, int64_t max_new,
                          int64_t bt_stride, int hq, int hkv, int head_dim, int64_t num_cus) {
@@ -44,15 +47,15 @@ SharedSizes shared_sizes(int64_t n_reqs, int64_t n_groups, int64_t max_q, int64_
   const int64_t longest = (bt_stride * 16 + arckv::kMaxItemKeys - 1) / arckv::kMaxItemKeys;   // pieces at least
   auto items = [&](int64_t parts, int64_t cols, int64_t units) {
     const int64_t tiles = (max_q * G / cols + std::min(parts, max_q)) * hkv * std::max<int64_t>(longest, 1);
-    return tiles <= units ? units : 2 * tiles;
+    return tiles <= units ? std::max(units, 4 * tiles) : tiles + units;
   };
   z.items_p = n_groups > 0 ? items(n_groups, z.tile_p, num_cus) : 0;
   z.items_o = items(n_reqs, z.tile_o, z.tile_o == kTailCols ? kTailPerUnit * num_cus : num_cus);
   auto per = [](int tile) { return tile == arckv::kNarrowCols ? int64_t{arckv::kListItems} : int64_t{1}; };   // lists of one item
   int64_t at = 16;
   auto take = [&](int64_t n) { const int64_t o = at; at += (n + 15) / 16 * 16; return o; };
-  z.off_group = take(n_groups * 8);
-  z.off_req = take(n_reqs * 8);
+  z.off_group = take(n_groups * kPartInts);
+  z.off_req = take(n_reqs * kPartInts);
   z.off_row = take(max_q * 2);
   z.off_cu = take(n_reqs + 1);
   z.off_len = take(n_reqs);
@@ -61,6 +64,12 @@ SharedSizes shared_sizes(int64_t n_reqs, int64_t n_groups, int64_t max_q, int64_
   z.n_ints = at;
   z.ws_floats = (z.items_p * z.tile_p + z.items_o * z.tile_o) * (head_dim + 1);
   return z;
+}
+
+// Few and short requests read all of their keys in one launch, shared or not: the shared ones come from the caches
+// then, and the launches that would save them cost more.
+bool short_route(const SharedSizes& z, int64_t n_reqs, int64_t bt_stride, int hkv, int head_dim) {
+  return z.tile_o == kTailCols && bt_stride * 16 <= 1024 && n_reqs * bt_stride * 16 * hkv * head_dim * 4 <= (int64_t{32} << 20);
 }
 
 // ---- the plan ---------------------------------------------------------------------------------
@@ -77,9 +86,9 @@ struct PlanShared {
   int32_t cap;
 };
 
-// Cuts n parts (column tiles and key tiles of part i from `size`) into at most `most` items: a piece has at most cap
-// key tiles, where cap is the one of 64 (the longest part in 1, 2, .. 64 pieces) whose rounds of the chip take least: a round
-// of `units` items takes its longest piece and `over` key tiles more.
+// The most key tiles of a piece, for n parts (units to cut and key tiles of part i from `size`) in at most `most` items: of 64
+// candidates (the longest part in 1, 2, .. 64 pieces) the one whose rounds of the chip take least: a round of `units`
+// items takes its longest piece and `over` key tiles more.
 template <class Size>
 __device__ __forceinline__ int choose_cap(int n, int64_t most, int units, int min_cap, int over, Size size, PlanShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -149,29 +158,64 @@ __device__ __forceinline__ int64_t sums_before(int64_t v, int64_t& total, PlanSh
   return before + s - v;
 }
 
-// Pieces and slots of the parts, then their work items: item of part i, piece p, column tile c, head h at slot
-// base + (p tiles + c) heads + h, so that items of the same keys lie `heads` apart (with 8 heads on one XCD).
-template <class ReqOf>
-__device__ void emit_items(Part* parts, int n, int cap, int hkv, int tile_cols, int per, Work* work, int64_t most, ReqOf req_of,
-                           PlanShared& sh) {
+// Pieces and slots of the parts, then their work items.  With more units than the chip takes at a time, whole rounds of
+// them stay whole, and only what is left is cut, so that it fills a last, shorter round (320 tiles of 128 key tiles on 256
+// units: 272 us, and 339 with every tile cut in two).  Units of the same keys lie `heads` apart: with 8 heads on one XCD.
+// DIRECT: a unit of one piece that nothing joins has slot -1, and its kernel writes the result.  Returns whether any unit
+// has several pieces.
+template <bool DIRECT, class ReqOf>
+__device__ bool emit_items(Part* parts, int n, int hkv, int units, int min_cap, int over, int tile_cols, int per, Work* work,
+                           int64_t most, ReqOf req_of, PlanShared& sh) {
   const int tid = threadIdx.x;
-  int64_t at = 0;
+  auto keys_of = [](const Part& p) { return p.tiles > 0 ? (p.keys1 - p.keys0 + kBK - 1) / kBK : 0; };
+  int64_t all = 0, total;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
     const int i = i0 + tid;
-    int64_t mine = 0, total;
+    all += (sums_before(i < n && keys_of(parts[i]) > 0 ? static_cast<int64_t>(parts[i].tiles) * hkv : 0, total, sh), total);
+  }
+  const int64_t first_cut = all / units * units;      // units before this one stay whole
+  int64_t at = 0, at_w = 0;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    const int keys = i < n ? keys_of(parts[i]) : 0;
+    const int64_t mine = keys > 0 ? static_cast<int64_t>(parts[i].tiles) * hkv : 0;
+    const int64_t before = at + sums_before(mine, total, sh);
+    at += total;
+    int64_t items = 0;
+    if (i < n) {
+      Part& p = parts[i];
+      p.whole = static_cast<int>(min(max(first_cut - before, int64_t{0}), mine));
+      p.pieces_w = (keys + kMaxPieceTiles - 1) / kMaxPieceTiles;
+      p.len_w = p.pieces_w > 0 ? (keys + p.pieces_w - 1) / p.pieces_w : 0;
+      items = static_cast<int64_t>(p.whole) * p.pieces_w;
+    }
+    sums_before(items, total, sh);
+    at_w += total;
+  }
+  __syncthreads();
+  const int cap = choose_cap(n, most - at_w, units, min_cap, over, [=](int i, int& cut, int& keys) {
+    keys = keys_of(parts[i]);
+    cut = keys > 0 ? parts[i].tiles * hkv - parts[i].whole : 0;
+  }, sh);
+  at = 0;
+  bool cut_any = false;
+  for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
+    const int i = i0 + tid;
+    int64_t mine = 0;
     Part p = {};
     if (i < n) {
       p = parts[i];
-      const int keys = p.tiles > 0 ? (p.keys1 - p.keys0 + kBK - 1) / kBK : 0;
+      const int keys = keys_of(p);
       p.pieces = keys > 0 ? (keys + cap - 1) / cap : 0;
       p.len = p.pieces > 0 ? (keys + p.pieces - 1) / p.pieces : 0;
       p.pieces = p.pieces > 0 ? (keys + p.len - 1) / p.len : 0;
-      mine = static_cast<int64_t>(p.pieces) * p.tiles * hkv;
+      mine = static_cast<int64_t>(p.whole) * p.pieces_w + (static_cast<int64_t>(p.tiles) * hkv - p.whole) * p.pieces;
     }
     const int64_t before = at + sums_before(mine, total, sh);
+    cut_any |= (p.whole > 0 && p.pieces_w > 1) || (p.tiles * hkv > p.whole && p.pieces > 1);
     if (i < n) {
       p.base = static_cast<int32_t>(min(before, most));
-      if (before + mine > most) p.tiles = p.pieces = 0;     // (lengths or groups that pass the bounds: no slot for it)
+      if (before + mine > most) p.tiles = p.whole = p.pieces = 0;     // (lengths or groups that pass the bounds: no slot for it)
       parts[i] = p;
     }
     at += total;
@@ -187,20 +231,26 @@ __device__ void emit_items(Part* parts, int n, int cap, int hkv, int tile_cols, 
         if (parts[mid].base <= e) lo = mid; else hi = mid - 1;
       }
       const Part p = parts[lo];
-      if (p.tiles > 0) {
-        const int k = static_cast<int>(e) - p.base;
-        const int piece = k / (hkv * p.tiles);
+      int k = static_cast<int>(e) - p.base;
+      const int whole_items = p.whole * p.pieces_w, cut = p.tiles * hkv - p.whole;
+      const bool is_whole = k < whole_items;
+      if (is_whole || cut > 0) {
+        if (!is_whole) k -= whole_items;
+        const int piece = k / (is_whole ? p.whole : cut), unit = k % (is_whole ? p.whole : cut) + (is_whole ? 0 : p.whole);
+        const int len = is_whole ? p.len_w : p.len, pieces = is_whole ? p.pieces_w : p.pieces;
         w.req = req_of(lo);
-        w.kvh = k % hkv;
-        w.col_start = k / hkv % p.tiles * tile_cols;
-        w.kv_start = p.keys0 + piece * p.len * kBK;
-        w.kv_end = min(w.kv_start + p.len * kBK, p.keys1);
-        w.slot = static_cast<int32_t>(e);
+        w.kvh = unit % hkv;
+        w.col_start = unit / hkv * tile_cols;
+        w.kv_start = p.keys0 + piece * len * kBK;
+        w.kv_end = min(w.kv_start + len * kBK, p.keys1);
+        w.slot = DIRECT && p.keys0 == 0 && pieces == 1 ? -1 : static_cast<int32_t>(e);
+        w.pad0 = pieces;
       }
     }
     work[e * per] = w;
     if (per > 1) work[e * per + 1].req = -1;
   }
+  return __syncthreads_or(cut_any);
 }
 
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
@@ -223,7 +273,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
     Part p = {};
     p.row0 = row(r0);
     p.rows = max(row(r1) - p.row0, 0);
-    p.pieces = r0;                                     // until the cut: the group's first request
+    p.group = r0;                                      // of a group: its first request
     p.keys1 = static_cast<int32_t>(min(static_cast<int64_t>(max(prefix_lens[g], 0)), room));
     groups[g] = p;
   }
@@ -245,278 +295,397 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
       g = r < start(lo + 1) ? lo : -1;
     }
     const int L = max(seq_lens[r], 0), q0 = row(r), S = max(row(r + 1) - q0, 0);
-    if (g >= 0 && S > 0) atomicMin(&groups[g].keys1, max(L - S, 0));
+    if (g >= 0 && S > 0) {
+      atomicMin(&groups[g].keys1, max(L - S, 0));
+      atomicAdd(&groups[g].whole, static_cast<int>((static_cast<int64_t>(S) * G + z.tile_o - 1) / z.tile_o));
+    }
     Part p = {};
     p.row0 = q0;
     p.rows = S;
     p.keys1 = static_cast<int32_t>(min(static_cast<int64_t>(L), room));
-    p.base = g;                                        // until the cut: the request's group
+    p.group = g;
     reqs[r] = p;
   }
   __syncthreads();
   for (int g = tid; g < n_groups; g += kPlanThreads) {
-    const int shared = __hip_atomic_load(&groups[g].keys1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) / kBK * kBK;
+    int shared = __hip_atomic_load(&groups[g].keys1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) / kBK * kBK;
+    const int apart = __hip_atomic_load(&groups[g].whole, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     Part& p = groups[g];
-    p.tiles = shared > 0 ? static_cast<int>((static_cast<int64_t>(p.rows) * G + z.tile_p - 1) / z.tile_p) : 0;
-    p.len = shared;
+    const int together = static_cast<int>((static_cast<int64_t>(p.rows) * G + z.tile_p - 1) / z.tile_p);
+    // Requests that fill their own wide tiles read their keys once for 256 columns anyhow: sharing that saves no more than
+    // an eighth of the tiles is not worth a second item and the join (2 x 1024 rows on 16384: 978 us shared)
+    if (z.tile_o == arckv::kWideCols && z.tile_p == arckv::kWideCols && 8 * apart <= 9 * together) shared = 0;
+    p.tiles = shared > 0 ? together : 0;
+    p.keys1 = shared;
     if (p.tiles > 0) {                                 // the group as a request of the kernels above
-      cu[p.pieces] = p.row0;
-      cu[p.pieces + 1] = p.row0 + p.rows;
-      len[p.pieces] = shared + p.rows;
+      cu[p.group] = p.row0;
+      cu[p.group + 1] = p.row0 + p.rows;
+      len[p.group] = shared + p.rows;
     }
   }
   __syncthreads();
   for (int r = tid; r < n_reqs; r += kPlanThreads) {
     Part& p = reqs[r];
-    const int g = p.base;
-    p.keys0 = g >= 0 && p.rows > 0 ? groups[g].len : 0;
+    p.keys0 = p.group >= 0 && p.rows > 0 ? groups[p.group].keys1 : 0;
     p.tiles = p.keys1 > p.keys0 ? static_cast<int>((static_cast<int64_t>(p.rows) * G + z.tile_o - 1) / z.tile_o) : 0;
-    for (int i = 0; i < p.rows; ++i) row_of[p.row0 + i] = make_int2(r, g);
   }
-  __syncthreads();
-  for (int g = tid; g < n_groups; g += kPlanThreads) groups[g].keys1 = groups[g].len;
+  const int total = row(n_reqs);
+  for (int t = tid; t < total; t += kPlanThreads) {    // a row's request and group
+    int lo = 0, hi = n_reqs - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (row(mid) <= t) lo = mid; else hi = mid - 1;
+    }
+    row_of[t] = make_int2(lo, reqs[lo].group);
+  }
   __syncthreads();
   // ---- the cuts and the items ------------------------------------------------------------------
-  auto sizes = [&](const Part* parts) {
-    return [=](int i, int& tiles, int& keys) {
-      tiles = parts[i].tiles * hkv;
-      keys = (parts[i].keys1 - parts[i].keys0 + kBK - 1) / kBK;
-    };
-  };
   auto per = [](int tile) { return tile == arckv::kNarrowCols ? arckv::kListItems : 1; };
-  if (n_groups > 0) {
-    const int cap = choose_cap(n_groups, z.items_p, num_cus, z.tile_p == arckv::kWideCols ? 8 : 4, 6, sizes(groups), sh);
-    emit_items(groups, n_groups, cap, hkv, z.tile_p, per(z.tile_p), reinterpret_cast<Work*>(plan + z.off_work_p), z.items_p,
-               [&](int g) { return start(g); }, sh);
+  if (n_groups > 0)
+    emit_items<false>(groups, n_groups, hkv, num_cus, z.tile_p == arckv::kWideCols ? 8 : 4, z.tile_p == arckv::kWideCols ? 8 : 5,
+                      z.tile_p, per(z.tile_p), reinterpret_cast<Work*>(plan + z.off_work_p), z.items_p,
+                      [&](int g) { return groups[g].group; }, sh);
+  auto* own = reinterpret_cast<Work*>(plan + z.off_work_o);
+  bool join;
+  if (z.tile_o == kTailCols) {
+    join = emit_items<false>(reqs, n_reqs, hkv, kTailPerUnit * num_cus, kTailWhole / kBK, 8, z.tile_o, 1,
+                             own, z.items_o, [](int r) { return r; }, sh);
+  } else {
+    const bool wide = z.tile_o == arckv::kWideCols;
+    join = emit_items<true>(reqs, n_reqs, hkv, num_cus, wide ? 8 : 4, wide ? 8 : 5, z.tile_o,
+                            per(z.tile_o), own, z.items_o, [](int r) { return r; }, sh);
+    bool shared = false;
+    for (int g = tid; g < n_groups; g += kPlanThreads) shared |= groups[g].tiles > 0;
+    join |= __syncthreads_or(shared);
   }
-  const bool tail = z.tile_o == kTailCols;
-  const int cap = choose_cap(n_reqs, z.items_o, tail ? kTailPerUnit * num_cus : num_cus, tail ? 4 : z.tile_o == arckv::kWideCols ? 8 : 4,
-                             6, sizes(reqs), sh);
-  emit_items(reqs, n_reqs, cap, hkv, z.tile_o, per(z.tile_o), reinterpret_cast<Work*>(plan + z.off_work_o), z.items_o,
-             [](int r) { return r; }, sh);
+  if (tid == 0) plan[0] = join;
+}
+
+// ---- joining pieces --------------------------------------------------------------------------------
+// D / 4 lanes have a (row, head), four dims each: its partial results (fp32, normalised) and their lse (base 2).
+typedef float acc4_t __attribute__((ext_vector_type(4)));
+struct Joined {
+  float m = -INFINITY, sum = 0.f;
+  acc4_t acc = {};
+};
+// Adds pieces i0, i0 + step, .. < n.  Their lse come in 16 at a time (a lane each), the partial results four at a time and the
+// first four beside the lse.
+template <class Lse, class Row>
+__device__ __forceinline__ void add_pieces(Joined& j, int i0, int step, int n, Lse lse_of, Row row_of) {
+  constexpr int kBatch = 16, kPre = 4;
+  const int sub = threadIdx.x % kBatch, mine = (threadIdx.x & 63) / kBatch * kBatch;
+  for (; i0 < n; i0 += step * kBatch) {
+    auto piece = [&](int k) -> acc4_t { return i0 + k * step < n ? *row_of(i0 + k * step) : acc4_t{}; };
+    const float l = i0 + sub * step < n ? lse_of(i0 + sub * step) : -INFINITY;
+    acc4_t v[kPre];
+#pragma unroll
+    for (int k = 0; k < kPre; ++k) v[k] = piece(k);
+    float top = l;
+#pragma unroll
+    for (int d = kBatch / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
+    const float m_new = fmaxf(j.m, top);
+    const float mu = m_new == -INFINITY ? 0.f : m_new;
+    const float alpha = j.m == -INFINITY ? 0.f : fast_exp2(j.m - mu);
+    const float wt = l == -INFINITY ? 0.f : fast_exp2(l - mu);
+    j.m = m_new;
+    j.sum *= alpha;
+    j.acc *= alpha;
+    const int nb = min(kBatch, (n - i0 + step - 1) / step);
+    for (int k0 = 0; k0 < nb; k0 += kPre) {
+      acc4_t next[kPre];
+#pragma unroll
+      for (int k = 0; k < kPre; ++k) next[k] = k0 + kPre < nb ? piece(k0 + kPre + k) : acc4_t{};
+#pragma unroll
+      for (int k = 0; k < kPre; ++k) {
+        const float a = __shfl(wt, mine + (k0 + k) % kBatch);
+        if (k0 + k < nb) {
+          j.sum += a;
+          j.acc += a * v[k];
+        }
+        v[k] = next[k];
+      }
+    }
+  }
+}
+// another sum of exponentials (not normalised) into j
+__device__ __forceinline__ void add_sum(Joined& j, float m, float sum, const acc4_t& acc) {
+  const float m_new = fmaxf(j.m, m);
+  const float a = j.m == -INFINITY ? 0.f : fast_exp2(j.m - m_new), b = m == -INFINITY ? 0.f : fast_exp2(m - m_new);
+  j.m = m_new;
+  j.sum = a * j.sum + b * sum;                            // (0 times a NaN stays NaN)
+  j.acc = a * j.acc + b * acc;
+}
+__device__ __forceinline__ void write_joined(const Joined& j, uint16_t* out, float* lse_out, int64_t row_head, int d, int d4) {
+  const float inv = j.sum > 0.f ? 1.f / j.sum : 0.f;
+  store_out<true>(out + row_head * d + 4 * d4, __builtin_convertvector(j.acc * inv, bf16x4_t));
+  if (lse_out != nullptr && d4 == 0)
+    lse_out[row_head] = j.sum > 0.f ? (j.m + __log2f(j.sum)) * kLn2 : j.sum == 0.f ? -INFINITY : j.sum;
+}
+// Pieces of column `c` (row - row0 times G, and the head of the group) of a part, and where its first piece lies and how far
+// apart they are, in columns.
+__device__ __forceinline__ int pieces_of(const Part& p, int64_t c, int kvh, int hkv, int tile_cols, int64_t& first, int64_t& step) {
+  const int64_t unit = c / tile_cols * hkv + kvh;
+  const bool whole = unit < p.whole;
+  first = (p.base + (whole ? unit : static_cast<int64_t>(p.whole) * p.pieces_w + unit - p.whole)) * tile_cols + c % tile_cols;
+  step = (whole ? p.whole : static_cast<int64_t>(p.tiles) * hkv - p.whole) * tile_cols;
+  return p.tiles == 0 ? 0 : whole ? p.pieces_w : p.pieces;
 }
 
 // ---- the own keys of decode steps --------------------------------------------------------------
 // An item is up to 16 columns (token x head of one KV group) of a request over a range of keys.  Too few columns to share
-// a tile: K and V go from memory straight into the operands of v_mfma_f32_16x16x32_bf16, 32 keys a step, four waves taking
-// every fourth step, and nothing passes through LDS but the waves' results at the end.  What bounds it is the
-// bytes of K and V, and the chain of waits (item, lengths, table, keys) of items of a few steps; four work-groups share a
-// compute unit.
+// a tile: K and V go from memory straight into the operands of v_mfma_f32_16x16x32_bf16, 32 keys a step, the waves taking
+// steps in turn, and nothing passes through LDS but the waves' results at the end.  An item that has all of its columns' own
+// keys joins them with the pieces over shared keys, which an earlier launch has written, and writes the result; one of
+// several pieces writes a partial result.  What bounds it is the
+// bytes of K and V, and the chain of waits (item, lengths, table, keys) of items of a few steps; three work-groups of four
+// waves share a compute unit.  With fewer items than units (WAVES = 8) an item's keys are spread over twice the waves.
 //   S^T (16 keys x 16 columns, twice): lane (i = l % 16, g = l / 16) holds row i's dims 32 k + 8 g ..; row i of
 //   product m is key 8 (i / 4) + 4 m + i % 4, so that the lane's results, rows 4 g + e, are the keys 8 g + 4 m + e
 //   of its column: the eight keys that it holds as the operand of P.V.
 //   O^T (16 dims x 16 columns): lane's V operand is dim 16 d + i, keys 8 g ..: 16 bytes of the dim-major block.
-template <int D, int G>
-__global__ __launch_bounds__(kTailThreads, 3) void shared_tail_kernel(
+// SHORT: no plan; a work-group has a request's columns for a head, and all of their keys, shared or not.
+template <int D, int G, int WAVES, bool SHORT>
+__global__ __launch_bounds__(64 * WAVES, 3) void shared_tail_kernel(
     const uint16_t* __restrict__ k_pool, const uint16_t* __restrict__ v_pool, const uint16_t* __restrict__ q,
-    const int32_t* __restrict__ block_tables, int bt_stride, const int32_t* __restrict__ cu_q,
-    const int32_t* __restrict__ seq_lens, int n_reqs, const Work* __restrict__ work, int64_t n_q, int64_t num_blocks, int hq,
-    int hkv, float scale_log2, float* __restrict__ ws_o, float* __restrict__ ws_lse, int64_t ws_slots) {
-  typedef float acc4 __attribute__((ext_vector_type(4)));
-  constexpr int KS = D / 32, DM = D / 16, kWaves = kTailThreads / 64;
+    uint16_t* __restrict__ out, float* __restrict__ lse_out, const int32_t* __restrict__ block_tables, int bt_stride,
+    const int32_t* __restrict__ cu_q, const int32_t* __restrict__ seq_lens, int n_reqs, int n_groups, int64_t n_q,
+    int64_t num_blocks, int hq, int hkv, float scale_log2, const int32_t* __restrict__ plan, SharedSizes z,
+    const float* __restrict__ ws_op, const float* __restrict__ ws_lp, float* __restrict__ ws_oo, float* __restrict__ ws_lo) {
+  constexpr int KS = D / 32, DM = D / 16, LANES = D / 4, SETS = 64 * WAVES / LANES;
   constexpr int PO = D + 4;                               // a column's row of the waves' results (floats)
-  __shared__ __attribute__((aligned(16))) float part_o[kWaves][kTailCols][PO];
-  __shared__ float part_m[kWaves][kTailCols], part_l[kWaves][kTailCols];
-  const Work w = work[blockIdx.x];
-  if (w.req < 0 || w.req >= n_reqs || w.kvh < 0 || w.kvh >= hkv || w.col_start < 0 || w.slot < 0 || w.slot >= ws_slots) return;
+  __shared__ __attribute__((aligned(16))) float part_o[WAVES][kTailCols][PO];
+  __shared__ float part_m[WAVES][kTailCols], part_l[WAVES][kTailCols];
+  __shared__ acc4_t set_o[SHORT ? 1 : SETS][LANES];
+  __shared__ float set_m[SETS], set_s[SETS];
+  Work w = {static_cast<int>(blockIdx.x), static_cast<int>(blockIdx.y), 0, 0, INT32_MAX, 0, 1, 0};
+  if constexpr (!SHORT) w = reinterpret_cast<const Work*>(plan + z.off_work_o)[blockIdx.x];
+  if (w.req < 0 || w.req >= n_reqs || w.kvh < 0 || w.kvh >= hkv || w.col_start < 0 || (!SHORT && w.slot >= z.items_o)) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i16 = lane & 15, g4 = lane >> 4;
   const int32_t* bt = block_tables + static_cast<int64_t>(w.req) * bt_stride;
   const int q0 = cu_q[w.req], S = cu_q[w.req + 1] - q0, L = seq_lens[w.req];
-  const int P = L - S, ncols = S * G, held = min(L, bt_stride * 16);
-  const int col = w.col_start + i16, tok = col / G;
-  const bool cval = col < ncols && q0 + tok < n_q;
-  const int pos = cval ? P + tok : -1;
-  const int last_tok = (min(w.col_start + kTailCols, ncols) - 1) / G;
-  const int kv_lo = max(w.kv_start, 0), kv_hi = min(min(w.kv_end, P + last_tok + 1), held);
-  const int min_pos = P + w.col_start / G;
-  const int steps = kv_hi > kv_lo ? (kv_hi - kv_lo + 31) / 32 : 0;
-  const int nblk = (held + 15) >> 4;
+  const int P = L - S, ncols = S * G, held = min(L, bt_stride * 16), nblk = (held + 15) >> 4;
   const uint32_t nb32 = static_cast<uint32_t>(min(num_blocks, static_cast<int64_t>(INT32_MAX)));
   const int64_t blk_stride = static_cast<int64_t>(hkv) * 16 * D;
   const int64_t head = static_cast<int64_t>(w.kvh) * 16 * D;
-
-  bf16x8_t qf[KS];
-  {
-    const int64_t at = cval ? (static_cast<int64_t>(q0 + tok) * hq + w.kvh * G + col % G) * D : 0;
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      u32x4_t v;
-      __builtin_memcpy(&v, q + at + 32 * ks + 8 * g4, 16);
-      qf[ks] = cval ? __builtin_bit_cast(bf16x8_t, v) : bf16x8_t{};
-    }
+  Part group = {};
+  if constexpr (!SHORT) {
+    const int g = reinterpret_cast<const Part*>(plan + z.off_req)[w.req].group;
+    if (g >= 0 && g < n_groups && w.pad0 == 1) group = reinterpret_cast<const Part*>(plan + z.off_group)[g];
   }
-  auto block_of = [&](int b) -> int64_t {                 // (uniform)
-    const int32_t ph = b < nblk ? bt[b] : 0;
-    ARCKV_CHECK_WAVE(ph < 0 || ph >= num_blocks, ARCKV_CHECK_BLOCK);
-    return (static_cast<uint32_t>(ph) >= nb32 ? 0 : ph) * blk_stride + head;
-  };
-  acc4 o[DM];
-#pragma unroll
-  for (int d = 0; d < DM; ++d) o[d] = acc4{};
-  float m_run = -INFINITY, l_run = 0.f;
-  for (int s = wave; s < steps; s += kWaves) {
-    const int k0 = kv_lo + 32 * s;
-    const int64_t b0 = block_of(k0 >> 4), b1 = block_of((k0 >> 4) + 1);
-    bf16x8_t kf[2][KS], vf[DM];
-#pragma unroll
-    for (int m = 0; m < 2; ++m) {
-      const int key = 8 * (i16 >> 2) + 4 * m + (i16 & 3);
-      const uint16_t* src = k_pool + (i16 >= 8 ? b1 : b0) + (key & 15) * D + 8 * g4;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) kf[m][ks] = *reinterpret_cast<const bf16x8_t*>(src + 32 * ks);
-    }
+  const int set = tid / LANES, d4 = tid % LANES;
+  for (int col0 = w.col_start; col0 < (SHORT ? ncols : w.col_start + 1); col0 += kTailCols) {
+    const int n_here = min(ncols - col0, kTailCols);      // columns that are there
+    if (n_here <= 0) return;                              // (uniform)
+    // ---- pieces over shared keys: sets_per sets of lanes have a column -------------------------
+    const int sets_per = n_here * 8 <= SETS ? 8 : n_here * 4 <= SETS ? 4 : n_here * 2 <= SETS ? 2 : 1;
+    auto shared = [&](int c, int from) -> Joined {
+      Joined j;
+      if constexpr (!SHORT) {
+        const int at = col0 + c;
+        const int64_t row = q0 + at / G - group.row0;
+        if (c < n_here && group.tiles > 0 && row >= 0 && row < group.rows) {
+          int64_t first, step;
+          const int n = pieces_of(group, row * G + at % G, w.kvh, hkv, z.tile_p, first, step);
+          add_pieces(j, from, sets_per, n, [&](int i) { return ws_lp[first + i * step]; },
+                     [&](int i) { return reinterpret_cast<const acc4_t*>(ws_op + (first + i * step) * D + 4 * d4); });
+        }
+      }
+      return j;
+    };
+    Joined mine = shared(set / sets_per, set % sets_per);
+    // ---- the keys ------------------------------------------------------------------------------
+    const int col = col0 + i16, tok = col / G;
+    const bool cval = col < ncols && q0 + tok < n_q;
+    const int pos = cval ? P + tok : -1;
+    const int last_tok = (col0 + n_here - 1) / G;
+    const int kv_lo = max(w.kv_start, 0), kv_hi = min(min(w.kv_end, P + last_tok + 1), held);
+    const int min_pos = P + col0 / G;
+    const int steps = kv_hi > kv_lo ? (kv_hi - kv_lo + 31) / 32 : 0;
+    bf16x8_t qf[KS];
     {
-      const uint16_t* src = v_pool + (g4 >= 2 ? b1 : b0) + i16 * 16 + 8 * (g4 & 1);
+      const int64_t at = cval ? (static_cast<int64_t>(q0 + tok) * hq + w.kvh * G + col % G) * D : 0;
 #pragma unroll
-      for (int d = 0; d < DM; ++d) vf[d] = *reinterpret_cast<const bf16x8_t*>(src + d * 256);
-    }
-    acc4 sc[2] = {acc4{}, acc4{}};
-#pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-      for (int m = 0; m < 2; ++m) sc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[m][ks], qf[ks], sc[m], 0, 0, 0);
-    const int key0 = k0 + 8 * g4;
-    if (k0 + 31 > min_pos || k0 + 32 > kv_hi) {           // (uniform) keys that some column does not see
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (key0 + j > pos || key0 + j >= kv_hi) sc[j / 4][j % 4] = -INFINITY;
-    }
-    if (k0 + 32 > held) {                                 // past the request's end the block may hold anything, NaN too
-#pragma unroll
-      for (int d = 0; d < DM; ++d) {
-        u32x4_t v = __builtin_bit_cast(u32x4_t, vf[d]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          v[j] = key0 + 2 * j >= held ? 0 : key0 + 2 * j + 1 >= held ? v[j] & 0xFFFFu : v[j];
-        vf[d] = __builtin_bit_cast(bf16x8_t, v);
+      for (int ks = 0; ks < KS; ++ks) {
+        u32x4_t v;
+        __builtin_memcpy(&v, q + at + 32 * ks + 8 * g4, 16);
+        qf[ks] = cval ? __builtin_bit_cast(bf16x8_t, v) : bf16x8_t{};
       }
     }
-    float mx = -INFINITY;
+    auto entry = [&](int b) -> int32_t { return b < nblk ? bt[b] : 0; };      // (uniform)
+    auto block_of = [&](int32_t ph) -> int64_t {
+      ARCKV_CHECK_WAVE(ph < 0 || ph >= num_blocks, ARCKV_CHECK_BLOCK);
+      return (static_cast<uint32_t>(ph) >= nb32 ? 0 : ph) * blk_stride + head;
+    };
+    acc4_t o[DM];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) mx = fmaxf(mx, sc[j / 4][j % 4]);
-    mx = fmaxf(mx, __shfl_xor(mx, 16));
-    mx = max_halves(mx) * scale_log2;
-    const float m_new = fmaxf(m_run, mx);
-    const float mu = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
-    m_run = m_new;
-    float p[8], sum = 0.f;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      p[j] = fast_exp2(fmaf(sc[j / 4][j % 4], scale_log2, -mu));
-      sum += p[j];
+    for (int d = 0; d < DM; ++d) o[d] = acc4_t{};
+    float m_run = -INFINITY, l_run = 0.f;
+    int32_t e0 = 0, e1 = 0;                               // the step's table entries, read a step ahead
+    if (wave < steps) {
+      e0 = entry((kv_lo + 32 * wave) >> 4);
+      e1 = entry(((kv_lo + 32 * wave) >> 4) + 1);
     }
-    l_run = l_run * alpha + sum;
-    // probabilities enter P.V as bf16 (off by at most 2^-8 of themselves); the sum is of the unrounded ones
-    u32x4_t pw;
+    for (int s = wave; s < steps; s += WAVES) {
+      const int k0 = kv_lo + 32 * s;
+      const int64_t b0 = block_of(e0), b1 = block_of(e1);
+      bf16x8_t kf[2][KS], vf[DM];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      pw[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{p[2 * j], p[2 * j + 1]}, bf16x2_t));
+      for (int m = 0; m < 2; ++m) {
+        const int key = 8 * (i16 >> 2) + 4 * m + (i16 & 3);
+        const uint16_t* src = k_pool + (i16 >= 8 ? b1 : b0) + (key & 15) * D + 8 * g4;
 #pragma unroll
-    for (int d = 0; d < DM; ++d) {
-      o[d] *= alpha;
-      o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], __builtin_bit_cast(bf16x8_t, pw), o[d], 0, 0, 0);
+        for (int ks = 0; ks < KS; ++ks) kf[m][ks] = *reinterpret_cast<const bf16x8_t*>(src + 32 * ks);
+      }
+      {
+        const uint16_t* src = v_pool + (g4 >= 2 ? b1 : b0) + i16 * 16 + 8 * (g4 & 1);
+#pragma unroll
+        for (int d = 0; d < DM; ++d) vf[d] = *reinterpret_cast<const bf16x8_t*>(src + d * 256);
+      }
+      if (s + WAVES < steps) {
+        e0 = entry((k0 + 32 * WAVES) >> 4);
+        e1 = entry(((k0 + 32 * WAVES) >> 4) + 1);
+      }
+      acc4_t sc[2] = {acc4_t{}, acc4_t{}};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) sc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[m][ks], qf[ks], sc[m], 0, 0, 0);
+      const int key0 = k0 + 8 * g4;
+      if (k0 + 31 > min_pos || k0 + 32 > kv_hi) {         // (uniform) keys that some column does not see
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (key0 + j > pos || key0 + j >= kv_hi) sc[j / 4][j % 4] = -INFINITY;
+      }
+      if (k0 + 32 > held) {                               // past the request's end the block may hold anything, NaN too
+#pragma unroll
+        for (int d = 0; d < DM; ++d) {
+          u32x4_t v = __builtin_bit_cast(u32x4_t, vf[d]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j)
+            v[j] = key0 + 2 * j >= held ? 0 : key0 + 2 * j + 1 >= held ? v[j] & 0xFFFFu : v[j];
+          vf[d] = __builtin_bit_cast(bf16x8_t, v);
+        }
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) mx = fmaxf(mx, sc[j / 4][j % 4]);
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = max_halves(mx) * scale_log2;
+      const float m_new = fmaxf(m_run, mx);
+      const float mu = m_new == -INFINITY ? 0.f : m_new;
+      const float alpha = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
+      m_run = m_new;
+      float p[8], sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        p[j] = fast_exp2(fmaf(sc[j / 4][j % 4], scale_log2, -mu));
+        sum += p[j];
+      }
+      l_run = l_run * alpha + sum;
+      // probabilities enter P.V as bf16 (off by at most 2^-8 of themselves); the sum is of the unrounded ones
+      u32x4_t pw;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        pw[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{p[2 * j], p[2 * j + 1]}, bf16x2_t));
+#pragma unroll
+      for (int d = 0; d < DM; ++d) {
+        o[d] *= alpha;
+        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], __builtin_bit_cast(bf16x8_t, pw), o[d], 0, 0, 0);
+      }
     }
-  }
-  // ---- the waves' results: lane holds dims 16 d + 4 g .. + 3 of its column ---------------------
-  l_run += __shfl_xor(l_run, 16);
-  l_run = sum_halves(l_run);
+    // ---- the waves' results: lane holds dims 16 d + 4 g .. + 3 of its column -------------------
+    l_run += __shfl_xor(l_run, 16);
+    l_run = sum_halves(l_run);
 #pragma unroll
-  for (int d = 0; d < DM; ++d) *reinterpret_cast<acc4*>(&part_o[wave][i16][16 * d + 4 * g4]) = o[d];
-  if (g4 == 0) {
-    part_m[wave][i16] = m_run;
-    part_l[wave][i16] = l_run;
-  }
-  __syncthreads();
-  constexpr int kPer = kTailCols * (D / 4) / kTailThreads;   // float4 of a thread
-#pragma unroll
-  for (int k = 0; k < kPer; ++k) {
-    const int e = tid + k * kTailThreads, c = e / (D / 4), d4 = e % (D / 4);
-    float m = -INFINITY;
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) m = fmaxf(m, part_m[v][c]);
-    float l = 0.f;
-    acc4 sum = {};
-#pragma unroll
-    for (int v = 0; v < kWaves; ++v) {
-      const float a = part_m[v][c] == -INFINITY ? 0.f : fast_exp2(part_m[v][c] - m);
-      l += a * part_l[v][c];
-      sum += a * *reinterpret_cast<const acc4*>(&part_o[v][c][4 * d4]);
+    for (int d = 0; d < DM; ++d) *reinterpret_cast<acc4_t*>(&part_o[wave][i16][16 * d + 4 * g4]) = o[d];
+    if (g4 == 0) {
+      part_m[wave][i16] = m_run;
+      part_l[wave][i16] = l_run;
     }
-    const int at = w.col_start + c;
-    if (at >= ncols || q0 + at / G >= n_q) continue;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    *reinterpret_cast<acc4*>(ws_o + (static_cast<int64_t>(w.slot) * kTailCols + c) * D + 4 * d4) = sum * inv;
-    if (d4 == 0) ws_lse[static_cast<int64_t>(w.slot) * kTailCols + c] = l > 0.f ? m + __log2f(l) : l == 0.f ? -INFINITY : l;
+    for (int c0 = 0; c0 < n_here; c0 += SETS / sets_per) {
+      if (c0 > 0) mine = shared(c0 + set / sets_per, set % sets_per);
+      if (!SHORT && sets_per > 1) {
+        set_o[set][d4] = mine.acc;
+        if (d4 == 0) {
+          set_m[set] = mine.m;
+          set_s[set] = mine.sum;
+        }
+      }
+      __syncthreads();
+      const int c = c0 + set / sets_per;
+      if (c < n_here && set % sets_per == 0 && q0 + (col0 + c) / G < n_q) {
+        if (!SHORT)
+          for (int k = 1; k < sets_per; ++k) add_sum(mine, set_m[set + k], set_s[set + k], set_o[set + k][d4]);
+        Joined keys;
+#pragma unroll
+        for (int v = 0; v < WAVES; ++v)
+          add_sum(keys, part_m[v][c], part_l[v][c], *reinterpret_cast<const acc4_t*>(&part_o[v][c][4 * d4]));
+        if (SHORT || w.pad0 == 1) {
+          add_sum(mine, keys.m, keys.sum, keys.acc);
+          const int at = col0 + c;
+          write_joined(mine, out, lse_out, static_cast<int64_t>(q0 + at / G) * hq + w.kvh * G + at % G, D, d4);
+        } else {
+          const float inv = keys.sum > 0.f ? 1.f / keys.sum : 0.f;
+          const int64_t at = static_cast<int64_t>(w.slot) * kTailCols + c;
+          *reinterpret_cast<acc4_t*>(ws_oo + at * D + 4 * d4) = keys.acc * inv;
+          if (d4 == 0) ws_lo[at] = keys.sum > 0.f ? keys.m + __log2f(keys.sum) : keys.sum == 0.f ? -INFINITY : keys.sum;
+        }
+      }
+      __syncthreads();
+    }
   }
 }
 
 // ---- the join ------------------------------------------------------------------------------------
-// D / 4 lanes have a row and head, four dims each.  Its pieces are first those over shared keys, then its own; their lse come in
-// 16 at a time (a lane each), the pieces four at a time.  What bounds it is reading the partial results (fp32).
-template <int D>
+// What the items have not joined: rows over shared and own keys in tiles, and own keys in several pieces.  plan[0] says
+// whether there is any.  With few rows (SPLIT) a work-group has one row and head and its sets of lanes take the pieces in turn;
+// otherwise it has a row and its sets take the heads.  What bounds it is reading the partial results (fp32).
+constexpr int64_t kSplitPairs = 8192;   // most (row, head) pairs whose pieces are split over a work-group
+template <int D, bool SPLIT>
 __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__ out, float* __restrict__ lse_out,
                                                           const int32_t* __restrict__ plan, SharedSizes z,
                                                           const int32_t* __restrict__ cu_q, int n_reqs, int n_groups,
                                                           int64_t n_q, int hq, int hkv, int G, const float* __restrict__ ws_op,
                                                           const float* __restrict__ ws_lp, const float* __restrict__ ws_oo,
                                                           const float* __restrict__ ws_lo) {
-  typedef float acc4 __attribute__((ext_vector_type(4)));
-  constexpr int kLanes = D / 4, kRows = 256 / kLanes, kBatch = 16;
-  const int64_t pair = static_cast<int64_t>(blockIdx.x) * kRows + threadIdx.x / kLanes;
-  const int64_t t = pair / hq;
-  const int h = static_cast<int>(pair % hq), kvh = h / G, d4 = threadIdx.x % kLanes;
-  const int total = min(static_cast<int64_t>(max(cu_q[n_reqs], 0)), n_q);
-  if (t >= total) return;
+  constexpr int LANES = D / 4, SETS = 256 / LANES;
+  __shared__ acc4_t set_o[SPLIT ? SETS : 1][LANES];
+  __shared__ float set_m[SETS], set_s[SETS];
+  const int set = threadIdx.x / LANES, d4 = threadIdx.x % LANES;
+  const int64_t t = SPLIT ? blockIdx.x / hq : blockIdx.x;
+  if (plan[0] == 0 || t >= n_q || t >= cu_q[n_reqs]) return;
   const int2 of = reinterpret_cast<const int2*>(plan + z.off_row)[t];
   auto part = [&](int64_t off, int i, int n) {
     const Part p = i >= 0 && i < n ? reinterpret_cast<const Part*>(plan + off)[i] : Part{};
     return t >= p.row0 && t - p.row0 < p.rows ? p : Part{};
   };
   const Part pg = part(z.off_group, of.y, n_groups), pr = part(z.off_req, of.x, n_reqs);
-  // row `col` of slot `base + (piece tiles + tile) hkv + kvh`
-  auto place = [&](const Part& p, int tile_cols, int piece) -> int64_t {
-    const int64_t c = (t - p.row0) * G + h % G;
-    const int64_t tile = c / tile_cols;
-    return (p.base + (static_cast<int64_t>(piece) * p.tiles + tile) * hkv + kvh) * tile_cols + c % tile_cols;
-  };
-  const int np = pg.tiles > 0 ? pg.pieces : 0, n = np + (pr.tiles > 0 ? pr.pieces : 0);
-  const int64_t p0 = place(pg, z.tile_p, 0), ps = static_cast<int64_t>(pg.tiles) * hkv * z.tile_p;
-  const int64_t r0 = place(pr, z.tile_o, 0), rs = static_cast<int64_t>(pr.tiles) * hkv * z.tile_o;
-  float m = -INFINITY, sum = 0.f;
-  acc4 acc = {};
-  const int sub = threadIdx.x % kBatch;
-  for (int i0 = 0; i0 < n; i0 += kBatch) {
-    const int i = i0 + sub;
-    float l = -INFINITY;
-    if (i < n) l = i < np ? ws_lp[p0 + i * ps] : ws_lo[r0 + (i - np) * rs];
-    float top = l;
-#pragma unroll
-    for (int d = kBatch / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    const float m_new = fmaxf(m, top);
-    const float mu = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - mu);
-    const float wt = l == -INFINITY ? 0.f : fast_exp2(l - mu);
-    m = m_new;
-    sum *= alpha;
-    acc *= alpha;
-    const int nb = min(kBatch, n - i0);
-    const int first = (threadIdx.x & 63) / kBatch * kBatch;
-#pragma unroll 4
-    for (int k = 0; k < nb; ++k) {
-      const int j = i0 + k;
-      const float* src = j < np ? ws_op + (p0 + j * ps) * D : ws_oo + (r0 + (j - np) * rs) * D;
-      const float a = __shfl(wt, first + k);
-      sum += a;
-      acc += a * *reinterpret_cast<const acc4*>(src + 4 * d4);
+  for (int h = SPLIT ? blockIdx.x % hq : set; h < hq; h += SPLIT ? hq : SETS) {
+    const int kvh = h / G;
+    int64_t p0, ps, r0, rs;
+    const int np = pieces_of(pg, (t - pg.row0) * G + h % G, kvh, hkv, z.tile_p, p0, ps);
+    const int nr = pieces_of(pr, (t - pr.row0) * G + h % G, kvh, hkv, z.tile_o, r0, rs);
+    if (nr == 1 && (np == 0 || z.tile_o == kTailCols)) continue;     // its item has written the result
+    Joined j;
+    add_pieces(j, SPLIT ? set : 0, SPLIT ? SETS : 1, np + nr,
+               [&](int i) { return i < np ? ws_lp[p0 + i * ps] : ws_lo[r0 + (i - np) * rs]; },
+               [&](int i) {
+                 return reinterpret_cast<const acc4_t*>((i < np ? ws_op + (p0 + i * ps) * D : ws_oo + (r0 + (i - np) * rs) * D) + 4 * d4);
+               });
+    if constexpr (SPLIT) {
+      set_o[set][d4] = j.acc;
+      if (d4 == 0) {
+        set_m[set] = j.m;
+        set_s[set] = j.sum;
+      }
+      __syncthreads();
+      if (set > 0) return;
+      for (int k = 1; k < SETS; ++k) add_sum(j, set_m[k], set_s[k], set_o[k][d4]);
     }
+    write_joined(j, out, lse_out, t * hq + h, D, d4);
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
-  store_out<true>(out + (t * hq + h) * D + 4 * d4, __builtin_convertvector(acc * inv, bf16x4_t));
-  if (lse_out != nullptr && d4 == 0)
-    lse_out[t * hq + h] = sum > 0.f ? (m + __log2f(sum)) * kLn2 : sum == 0.f ? -INFINITY : sum;
 }
 
 // What the three calls check of the bounds that they share.
@@ -619,35 +788,45 @@ extern "C" int32_t arckv_shared_prefix_attention(
   auto go = [&](auto d_tag, auto g_tag) {
     constexpr int D = decltype(d_tag)::value, GG = decltype(g_tag)::value;
     // items over the keys of (cu, len): shared keys by the groups' rows, own keys by the requests'
-    auto part = [&](int tile, int64_t items, const int32_t* work, const int32_t* cu, const int32_t* len, float* wo, float* wl) {
+    auto part = [&](int tile, int64_t items, const int32_t* work, const int32_t* cu, const int32_t* len, float* wo, float* wl,
+                    float* lse_out) {
       auto* wk = reinterpret_cast<const Work*>(work);
       const dim3 grid(static_cast<unsigned>(items));
-      if (tile == kTailCols)
-        hipLaunchKernelGGL((shared_tail_kernel<D, GG>), grid, dim3(kTailThreads), 0, st, kp, vp, qp, block_tables, bt_stride, cu,
-                           len, n_reqs, wk, max_q, num_blocks, num_q_heads, num_kv_heads, scale_log2, wo, wl, items);
-      else if (tile == arckv::kWideCols && any_align)
-        hipLaunchKernelGGL((prefill_attn_pp_kernel<D, GG, false, true>), grid, dim3(512), 0, st, kp, vp, qp, op, block_tables,
-                           bt_stride, cu, len, n_reqs, wk, max_q, num_blocks, num_q_heads, num_kv_heads, scale_log2, wo, wl,
-                           items, static_cast<float*>(nullptr));
-      else if (tile == arckv::kWideCols)
-        hipLaunchKernelGGL((prefill_attn_pp_kernel<D, GG, false, false>), grid, dim3(512), 0, st, kp, vp, qp, op, block_tables,
-                           bt_stride, cu, len, n_reqs, wk, max_q, num_blocks, num_q_heads, num_kv_heads, scale_log2, wo, wl,
-                           items, static_cast<float*>(nullptr));
-      else if (any_align)
-        hipLaunchKernelGGL((prefill_attn_list_kernel<D, GG, true>), grid, dim3(512), 0, st, kp, vp, qp, op, block_tables,
-                           bt_stride, cu, len, n_reqs, wk, max_q, num_blocks, num_q_heads, num_kv_heads, scale_log2, wo, wl,
-                           items, static_cast<float*>(nullptr));
-      else
-        hipLaunchKernelGGL((prefill_attn_list_kernel<D, GG, false>), grid, dim3(512), 0, st, kp, vp, qp, op, block_tables,
-                           bt_stride, cu, len, n_reqs, wk, max_q, num_blocks, num_q_heads, num_kv_heads, scale_log2, wo, wl,
-                           items, static_cast<float*>(nullptr));
+      auto run = [&](auto kernel) {
+        hipLaunchKernelGGL(kernel, grid, dim3(512), 0, st, kp, vp, qp, op, block_tables, bt_stride, cu, len, n_reqs, wk, max_q,
+                           num_blocks, num_q_heads, num_kv_heads, scale_log2, wo, wl, items, lse_out);
+      };
+      if (tile == arckv::kWideCols && any_align) run(prefill_attn_pp_kernel<D, GG, false, true>);
+      else if (tile == arckv::kWideCols) run(prefill_attn_pp_kernel<D, GG, false, false>);
+      else if (any_align) run(prefill_attn_list_kernel<D, GG, true>);
+      else run(prefill_attn_list_kernel<D, GG, false>);
     };
-    if (z.items_p > 0) part(z.tile_p, z.items_p, plan + z.off_work_p, plan + z.off_cu, plan + z.off_len, ws_op, ws_lp);
-    part(z.tile_o, z.items_o, plan + z.off_work_o, cu_q, seq_lens, ws_oo, ws_lo);
-    constexpr int kRows = 256 / (D / 4);
+    auto tail = [&](auto waves, auto is_short, dim3 grid) {
+      hipLaunchKernelGGL((shared_tail_kernel<D, GG, decltype(waves)::value, decltype(is_short)::value>), grid,
+                         dim3(64 * decltype(waves)::value), 0, st, kp, vp, qp, op, lse, block_tables, bt_stride, cu_q, seq_lens, n_reqs,
+                         n_groups, max_q, num_blocks, num_q_heads, num_kv_heads, scale_log2, plan, z, ws_op, ws_lp, ws_oo, ws_lo);
+    };
+    using W4 = std::integral_constant<int, 4>;
+    using W8 = std::integral_constant<int, 8>;
+    if (short_route(z, n_reqs, bt_stride, num_kv_heads, head_dim)) {
+      tail(W8{}, std::true_type{}, dim3(static_cast<unsigned>(n_reqs), static_cast<unsigned>(num_kv_heads)));
+      return;
+    }
+    if (z.items_p > 0) part(z.tile_p, z.items_p, plan + z.off_work_p, plan + z.off_cu, plan + z.off_len, ws_op, ws_lp, nullptr);
+    if (z.tile_o != kTailCols) {
+      part(z.tile_o, z.items_o, plan + z.off_work_o, cu_q, seq_lens, ws_oo, ws_lo, lse);
+    } else {
+      const dim3 grid(static_cast<unsigned>(z.items_o));
+      if (std::min<int64_t>(n_reqs, max_q) * num_kv_heads <= num_cus) tail(W8{}, std::false_type{}, grid);
+      else tail(W4{}, std::false_type{}, grid);
+      if (bt_stride * 16 <= kTailWhole) return;           // no request's own keys can be cut
+    }
     const int64_t pairs = max_q * num_q_heads;
-    hipLaunchKernelGGL(shared_join_kernel<D>, dim3(static_cast<unsigned>((pairs + kRows - 1) / kRows)), dim3(256), 0, st, op, lse,
-                       plan, z, cu_q, n_reqs, n_groups, max_q, num_q_heads, num_kv_heads, GG, ws_op, ws_lp, ws_oo, ws_lo);
+    auto join = [&](auto split, int64_t groups) {
+      hipLaunchKernelGGL((shared_join_kernel<D, decltype(split)::value>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, st, op,
+                         lse, plan, z, cu_q, n_reqs, n_groups, max_q, num_q_heads, num_kv_heads, GG, ws_op, ws_lp, ws_oo, ws_lo);
+    };
+    if (pairs <= kSplitPairs) join(std::true_type{}, pairs); else join(std::false_type{}, max_q);
   };
   auto with_g = [&](auto d_tag) {
     switch (G) {

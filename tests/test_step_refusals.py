@@ -16,10 +16,28 @@ A, M = 0x20000, 0x20001          # an aligned and a misaligned address, never re
 
 
 class Tensor(_Tensor):
-    dtype = "torch.bfloat16"
+    """A contiguous device tensor, as far as the checks look; step, row: its strides, if it is not."""
+
+    def __init__(self, *shape, dtype=torch.bfloat16, index=1, step=1, row=None):
+        super().__init__(*shape, size=dtype.itemsize, index=index, real=dtype.is_floating_point)
+        self.dtype, self.index, self.strides = dtype, index, (row or (shape[-1] if len(shape) > 1 else 1), step)
+
+    def is_contiguous(self):
+        return self.strides[1] == 1 and (len(self.shape) != 2 or self.strides[0] == self.shape[1])
 
     def stride(self, k):
-        return getattr(self, "row", self.shape[1]) if k == 0 else getattr(self, "step", 1)
+        return self.strides[k]
+
+    def get_device(self):
+        return self.index
+
+
+def i32(*shape, **kw):
+    return Tensor(*shape, dtype=torch.int32, **kw)
+
+
+def f32(*shape, **kw):
+    return Tensor(*shape, dtype=torch.float32, **kw)
 
 
 def norm(x=A, x_stride=64, res=None, rout=None, w=A, n=4, h=64, eps=1e-6, out=A, fmt=0, scales=None):
@@ -53,42 +71,106 @@ def test_maps_refuse():
 def test_norm_binding_refuses():
     x, w, out = Tensor(5, 64), Tensor(64), Tensor(5, 64)
     call = lambda **kw: ak.add_rms_norm(**{**dict(x=x, weight=w, out=out, eps=1e-6), **kw})  # noqa: E731
-    gap = Tensor(5, 64)
-    gap.step = 2
-    over = Tensor(5, 64)
-    over.row = 60
-    half = Tensor(5, 64)
-    half.dtype = "torch.float16"
-    wide = Tensor(5, 64, size=4)
-    for kw in (dict(x=Tensor(5)), dict(x=gap), dict(x=over), dict(x=half), dict(x=wide), dict(out=Tensor(5, 63)), dict(weight=Tensor(63)),
-               dict(residual=Tensor(4, 64)), dict(residual_out=out), dict(residual=out, residual_out=Tensor(5, 1)),
-               dict(scales=Tensor(4, size=4, real=True)), dict(scales=Tensor(5, size=4, real=True)),       # (a 16-bit out)
-               dict(scales=Tensor(5, size=4), out=Tensor(5, 64, size=1)), dict(out=Tensor(5, 64, size=1)),
-               dict(weight=half), dict(x=SimpleNamespace(dim=lambda: 3))):
+    half, wide, u8 = (Tensor(5, 64, dtype=t) for t in (torch.float16, torch.float32, torch.uint8))
+    for kw in (dict(x=Tensor(5)), dict(x=Tensor(5, 64, step=2)), dict(x=Tensor(5, 64, row=60)), dict(x=half), dict(x=wide),
+               dict(x=Tensor(5, 64, index=-1)), dict(out=Tensor(5, 63)), dict(out=Tensor(5, 64, row=70)), dict(out=half), dict(out=u8),
+               dict(weight=Tensor(63)), dict(weight=Tensor(64, dtype=torch.float16)), dict(residual=Tensor(4, 64)), dict(residual=half),
+               dict(residual_out=out), dict(residual=out, residual_out=Tensor(5, 1)), dict(scales=f32(4), out=u8),
+               dict(scales=f32(5)), dict(scales=i32(5), out=u8), dict(weight=Tensor(64, index=-1))):
         with pytest.raises(ValueError):
             call(**kw)
 
 
-def test_maps_binding_refuses():
-    def i32(*s):
-        return Tensor(*s, size=4)
+def good_maps(index=1):
+    kw = dict(new_tokens=(3,), held=(3,), block_tables=(3, 4), free_blocks=(8,), free_count=(1,), cu_q=(4,), seq_lens=(3,),
+              slot_mapping=(9,), free_left=(1,))
+    return {**{k: i32(*v, index=index) for k, v in kw.items()}, "num_blocks": 100}
 
-    good = dict(new_tokens=i32(3), held=i32(3), block_tables=i32(3, 4), free_blocks=i32(8), free_count=i32(1), cu_q=i32(4),
-                seq_lens=i32(3), slot_mapping=i32(9), free_left=i32(1), num_blocks=100)
-    for kw in (dict(new_tokens=i32(2)), dict(block_tables=i32(12)), dict(block_tables=i32(2, 4)), dict(cu_q=i32(3)), dict(seq_lens=i32(4)),
-               dict(free_count=i32(2)), dict(free_left=i32(2)), dict(true_lens=i32(3)), dict(true_offset=i32(3)),
-               dict(true_lens=i32(3), true_offset=i32(2)), dict(held=Tensor(3, size=8)), dict(slot_mapping=Tensor(9, size=4, real=True))):
+
+def test_maps_binding_refuses():
+    for kw in (dict(new_tokens=i32(2)), dict(held=i32(3, 1)), dict(block_tables=i32(12)), dict(block_tables=i32(2, 4)), dict(cu_q=i32(3)),
+               dict(seq_lens=i32(4)), dict(free_count=i32(2)), dict(free_left=i32(2)), dict(true_lens=i32(3)), dict(true_offset=i32(3)),
+               dict(true_lens=i32(3), true_offset=i32(2)), dict(held=Tensor(3, dtype=torch.int64)), dict(slot_mapping=f32(9)),
+               dict(block_tables=i32(3, 4, row=8)), dict(held=i32(3, index=-1))):
         with pytest.raises(ValueError):
-            ak.batch_maps(**{**good, **kw})
+            ak.batch_maps(**{**good_maps(), **kw})
+
+
+BOUNDS = ak.SharedBounds(3, 2, 6, 4, 2, 5, 8, 2, 64, 256)
+
+
+def good_plan(index=1):
+    ints, _ = ak.shared_prefix_sizes(BOUNDS)
+    return dict(b=BOUNDS, **{k: i32(*v, index=index) for k, v in dict(group_start=(3,), prefix_lens=(2,), cu_q=(4,), seq_lens=(3,),
+                                                                   plan=(ints,)).items()})
+
+
+def good_attention(index=1):
+    ints, ws = ak.shared_prefix_sizes(BOUNDS)
+    t = lambda *s, **kw: Tensor(*s, index=index, **kw)  # noqa: E731
+    return dict(b=BOUNDS, k_pool=t(9, 2, 16, 64), v_pool=t(9, 2, 64, 16), q=t(6, 8, 64), out=t(6, 8, 64), lse=f32(6, 8, index=index),
+                block_tables=i32(3, 5, index=index), cu_q=i32(4, index=index), seq_lens=i32(3, index=index), plan=i32(ints, index=index),
+                scale=0.1, workspace=t(ws, dtype=torch.uint8))
+
+
+def test_shared_prefix_bindings_refuse(monkeypatch):
+    ints, ws = ak.shared_prefix_sizes(BOUNDS)
+    for kw in (dict(group_start=i32(2)), dict(prefix_lens=i32(3)), dict(cu_q=i32(3)), dict(seq_lens=i32(4)), dict(plan=f32(ints)),
+               dict(plan=i32(ints, index=-1)), dict(cu_q=i32(4, index=0))):
+        with pytest.raises(ValueError):
+            ak.shared_prefix_plan(**{**good_plan(), **kw})
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    with pytest.raises(ak.ArckvError, match="ENOSPC"):
+        ak.shared_prefix_plan(**{**good_plan(0), "plan": i32(ints - 1, index=0), "stream": 0})
+    for kw in (dict(k_pool=Tensor(9, 2, 16, 128)), dict(v_pool=Tensor(8, 2, 64, 16)), dict(q=Tensor(5, 8, 64)), dict(out=Tensor(6, 8, 32)),
+               dict(q=f32(6, 8, 64)), dict(lse=f32(6, 4)), dict(lse=Tensor(6, 8)), dict(block_tables=i32(3, 4)), dict(cu_q=i32(3)),
+               dict(seq_lens=i32(2)), dict(plan=i32(ints - 1)), dict(workspace=Tensor(ws - 1, dtype=torch.uint8)),
+               dict(workspace=Tensor(ws, dtype=torch.uint8, index=0)), dict(q=Tensor(6, 8, 64, index=-1))):
+        with pytest.raises(ValueError):
+            ak.shared_prefix_attention(**{**good_attention(), **kw})
+
+
+def sizes(n=3, g=2, q=6, gq=4, new=2, stride=5, hq=8, hkv=2, d=64, cus=256):
+    import ctypes as C
+    a, b = _lib.i64(), _lib.i64()
+    return _lib.load().arckv_shared_prefix_sizes(n, g, q, gq, new, stride, hq, hkv, d, cus, C.byref(a), C.byref(b))
+
+
+def test_shared_prefix_calls_refuse():
+    E, U, L = _lib.EINVAL, _lib.EUNSUPPORTED, _lib.load()
+    assert sizes() == _lib.OK
+    for kw in (dict(n=-1), dict(n=(1 << 20) + 1), dict(g=4), dict(g=-1), dict(q=-1), dict(q=(1 << 24) + 1), dict(gq=7), dict(gq=-1), dict(new=7),
+               dict(stride=-1), dict(stride=(1 << 26) + 1), dict(hq=9), dict(hq=0), dict(hkv=0), dict(cus=0)):
+        assert sizes(**kw) == E, kw
+    assert sizes(d=96) == sizes(hq=6) == U
+    assert L.arckv_shared_prefix_sizes(3, 2, 6, 4, 2, 5, 8, 2, 64, 256, None, None) == E
+    ints, ws = ak.shared_prefix_sizes(BOUNDS)
+
+    def plan(gs=A, pl=A, cu=A, sl=A, p=A, n=ints):
+        return L.arckv_shared_prefix_plan(gs, pl, 2, cu, sl, 3, 6, 4, 2, 5, 8, 2, 64, 256, p, n, None)
+
+    for kw in (dict(gs=None), dict(pl=None), dict(cu=None), dict(sl=None), dict(p=None), dict(p=A + 4)):
+        assert plan(**kw) == E, kw
+    assert plan(n=ints - 1) == _lib.ENOSPC
+
+    def attention(kp=A, vp=A, q=A, out=A, bt=A, cu=A, sl=A, nb=9, scale=0.1, p=A, w=A, n=ws):
+        return L.arckv_shared_prefix_attention(kp, vp, q, out, None, bt, 5, cu, sl, 3, 2, 6, 4, 2, nb, 8, 2, 64, 256, scale, p, w, n, None)
+
+    for kw in ({k: None} for k in ("kp", "vp", "q", "out", "bt", "cu", "sl", "p", "w")):
+        assert attention(**kw) == E, kw
+    for kw in (dict(nb=0), dict(nb=(1 << 27) + 1), dict(scale=0.0), dict(scale=float("nan")), dict(kp=A + 8), dict(vp=A + 8), dict(p=A + 8),
+               dict(w=A + 8)):
+        assert attention(**kw) == E, kw
+    assert attention(n=ws - 1) == _lib.ENOSPC
 
 
 @pytest.mark.parametrize("device", [0, 1])
 def test_calls_run_on_their_tensors_device(device, monkeypatch):
     """On the tensors' device, whichever is the current one; tensors of several are refused."""
-    from tests.test_binding_device import i32
     seen = []
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
     monkeypatch.setattr(ak, "_current_stream", lambda index=None: 100 + index)
+    real = ak.lib()
 
     class Guard:
         def __init__(self, index):
@@ -101,25 +183,24 @@ def test_calls_run_on_their_tensors_device(device, monkeypatch):
             return False
 
     monkeypatch.setattr(torch.cuda, "device", Guard)
-    fake = SimpleNamespace(arckv_add_rms_norm=lambda *a: seen.append(("norm", a[-1].value)) or 0,
-                           arckv_batch_maps=lambda *a: seen.append(("maps", a[-1].value)) or 0)
+    names = ("arckv_add_rms_norm", "arckv_batch_maps", "arckv_shared_prefix_plan", "arckv_shared_prefix_attention")
+    fake = SimpleNamespace(arckv_shared_prefix_sizes=real.arckv_shared_prefix_sizes,
+                           **{n: (lambda *a, n=n: seen.append((n, a[-1])) or 0) for n in names})
     monkeypatch.setattr(ak, "lib", lambda: fake)
-
-    def on(t, index=device):
-        t.device = SimpleNamespace(index=index)
-        t.dtype = "torch.int32"
-        return t
-
-    def t16(*s, index=device):
-        return on(Tensor(*s), index)
-
-    ak.add_rms_norm(t16(5, 64), t16(64), t16(5, 64), 1e-6)
-    ints = dict(new_tokens=i32(3), held=i32(3), block_tables=i32(3, 4), free_blocks=i32(8), free_count=i32(1), cu_q=i32(4),
-                seq_lens=i32(3), slot_mapping=i32(9), free_left=i32(1))
-    ak.batch_maps(**{k: on(v) for k, v in ints.items()}, num_blocks=100)
-    assert [s for s in seen if s[0] != "device"] == [("norm", 100 + device), ("maps", 100 + device)]
-    assert [s for s in seen if s[0] == "device"] == ([] if device == 0 else [("device", 1)] * 2)
-    with pytest.raises(ValueError, match="one device"):
-        ak.add_rms_norm(t16(5, 64), t16(64, index=device + 1), t16(5, 64), 1e-6)
-    with pytest.raises(ValueError, match="one device"):
-        ak.batch_maps(**{k: on(v, device + (k == "free_left")) for k, v in ints.items()}, num_blocks=100)
+    norm_args = lambda i: dict(x=Tensor(5, 64, index=i), weight=Tensor(64, index=i), out=Tensor(5, 64, index=i), eps=1e-6,  # noqa: E731
+                               residual=Tensor(5, 64, index=i))
+    calls = [(ak.add_rms_norm, norm_args), (ak.batch_maps, good_maps), (ak.shared_prefix_plan, good_plan),
+             (ak.shared_prefix_attention, good_attention)]
+    for f, args in calls:
+        f(**args(device))
+    assert [s for s in seen if s[0] != "device"] == [(n, 100 + device) for n in names]
+    assert [s for s in seen if s[0] == "device"] == ([] if device == 0 else [("device", 1)] * 4)
+    for f, args in calls:
+        other = args(device + 1)
+        for name, t in args(device).items():
+            if isinstance(t, Tensor):
+                with pytest.raises(ValueError):
+                    f(**{**args(device), name: other[name]})
+    f, args = calls[0]
+    f(**args(device), stream=7)
+    assert seen[-1] == (names[0], 7)
