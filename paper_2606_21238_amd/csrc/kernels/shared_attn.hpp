@@ -26,7 +26,7 @@ constexpr int kMaxPieceTiles = arckv::kMaxItemKeys / kBK;
 struct SharedSizes {
   int tile_p, tile_o;                     // columns of an item over shared / own keys
   int64_t items_p, items_o;               // most items of each
-  int64_t off_group, off_req, off_row, off_cu, off_len, off_work_p, off_work_o, n_ints;
+  int64_t off_group, off_req, off_row, off_list, off_cu, off_len, off_work_p, off_work_o, n_ints;
   int64_t ws_floats;
 };
 // Plan entry of a group / of a request.  Its units are (column tile, head) pairs, head fastest; the first `whole` of them
@@ -47,7 +47,7 @@ SharedSizes shared_sizes(int64_t n_reqs, int64_t n_groups, int64_t max_q, int64_
   const int64_t longest = (bt_stride * 16 + arckv::kMaxItemKeys - 1) / arckv::kMaxItemKeys;   // pieces at least
   auto items = [&](int64_t parts, int64_t cols, int64_t units) {
     const int64_t tiles = (max_q * G / cols + std::min(parts, max_q)) * hkv * std::max<int64_t>(longest, 1);
-    return tiles <= units ? std::max(units, 4 * tiles) : tiles + units;
+    return 2 * tiles <= units ? units : tiles <= units ? 4 * tiles : tiles + units;
   };
   z.items_p = n_groups > 0 ? items(n_groups, z.tile_p, num_cus) : 0;
   z.items_o = items(n_reqs, z.tile_o, z.tile_o == kTailCols ? kTailPerUnit * num_cus : num_cus);
@@ -57,6 +57,7 @@ SharedSizes shared_sizes(int64_t n_reqs, int64_t n_groups, int64_t max_q, int64_
   z.off_group = take(n_groups * kPartInts);
   z.off_req = take(n_reqs * kPartInts);
   z.off_row = take(max_q * 2);
+  z.off_list = take(max_q);
   z.off_cu = take(n_reqs + 1);
   z.off_len = take(n_reqs);
   z.off_work_p = take(z.items_p * ARCKV_WORK_INTS * per(z.tile_p));
@@ -79,7 +80,9 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int src) {
   return static_cast<int64_t>(static_cast<uint64_t>(static_cast<uint32_t>(hi)) << 32 | static_cast<uint32_t>(lo));
 }
 
+constexpr int kPlanParts = 1024;          // groups and requests whose entries are made in LDS
 struct PlanShared {
+  Part parts[kPlanParts];
   int64_t wave[kPlanThreads / 64];
   int64_t items[kPlanThreads / 64][64];   // of every candidate cut, by the wave that counted
   int32_t top[kPlanThreads / 64];
@@ -161,10 +164,9 @@ __device__ __forceinline__ int64_t sums_before(int64_t v, int64_t& total, PlanSh
 // Pieces and slots of the parts, then their work items.  With more units than the chip takes at a time, whole rounds of
 // them stay whole, and only what is left is cut, so that it fills a last, shorter round (320 tiles of 128 key tiles on 256
 // units: 272 us, and 339 with every tile cut in two).  Units of the same keys lie `heads` apart: with 8 heads on one XCD.
-// DIRECT: a unit of one piece that nothing joins has slot -1, and its kernel writes the result.  Returns whether any unit
-// has several pieces.
+// DIRECT: a unit of one piece that nothing joins has slot -1, and its kernel writes the result.
 template <bool DIRECT, class ReqOf>
-__device__ bool emit_items(Part* parts, int n, int hkv, int units, int min_cap, int over, int tile_cols, int per, Work* work,
+__device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, int over, int tile_cols, int per, Work* work,
                            int64_t most, ReqOf req_of, PlanShared& sh) {
   const int tid = threadIdx.x;
   auto keys_of = [](const Part& p) { return p.tiles > 0 ? (p.keys1 - p.keys0 + kBK - 1) / kBK : 0; };
@@ -198,7 +200,6 @@ __device__ bool emit_items(Part* parts, int n, int hkv, int units, int min_cap, 
     cut = keys > 0 ? parts[i].tiles * hkv - parts[i].whole : 0;
   }, sh);
   at = 0;
-  bool cut_any = false;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
     const int i = i0 + tid;
     int64_t mine = 0;
@@ -212,7 +213,6 @@ __device__ bool emit_items(Part* parts, int n, int hkv, int units, int min_cap, 
       mine = static_cast<int64_t>(p.whole) * p.pieces_w + (static_cast<int64_t>(p.tiles) * hkv - p.whole) * p.pieces;
     }
     const int64_t before = at + sums_before(mine, total, sh);
-    cut_any |= (p.whole > 0 && p.pieces_w > 1) || (p.tiles * hkv > p.whole && p.pieces > 1);
     if (i < n) {
       p.base = static_cast<int32_t>(min(before, most));
       if (before + mine > most) p.tiles = p.whole = p.pieces = 0;     // (lengths or groups that pass the bounds: no slot for it)
@@ -250,7 +250,7 @@ __device__ bool emit_items(Part* parts, int n, int hkv, int units, int min_cap, 
     work[e * per] = w;
     if (per > 1) work[e * per + 1].req = -1;
   }
-  return __syncthreads_or(cut_any);
+  __syncthreads();
 }
 
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
@@ -259,8 +259,10 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
     int hkv, int num_cus, SharedSizes z, int32_t* __restrict__ plan) {
   __shared__ PlanShared sh;
   const int tid = threadIdx.x;
-  auto* groups = reinterpret_cast<Part*>(plan + z.off_group);
-  auto* reqs = reinterpret_cast<Part*>(plan + z.off_req);
+  // small batches are planned in LDS (the plan's entries are copied out at the end): every step below waits for the last
+  const bool in_lds = n_groups + n_reqs <= kPlanParts;
+  Part* const groups = in_lds ? sh.parts : reinterpret_cast<Part*>(plan + z.off_group);
+  Part* const reqs = in_lds ? sh.parts + n_groups : reinterpret_cast<Part*>(plan + z.off_req);
   auto* row_of = reinterpret_cast<int2*>(plan + z.off_row);
   int32_t* cu = plan + z.off_cu;
   int32_t* len = plan + z.off_len;
@@ -334,7 +336,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
     int lo = 0, hi = n_reqs - 1;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1;
-      if (row(mid) <= t) lo = mid; else hi = mid - 1;
+      if (reqs[mid].row0 <= t) lo = mid; else hi = mid - 1;
     }
     row_of[t] = make_int2(lo, reqs[lo].group);
   }
@@ -346,19 +348,29 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
                       z.tile_p, per(z.tile_p), reinterpret_cast<Work*>(plan + z.off_work_p), z.items_p,
                       [&](int g) { return groups[g].group; }, sh);
   auto* own = reinterpret_cast<Work*>(plan + z.off_work_o);
-  bool join;
   if (z.tile_o == kTailCols) {
-    join = emit_items<false>(reqs, n_reqs, hkv, kTailPerUnit * num_cus, kTailWhole / kBK, 8, z.tile_o, 1,
-                             own, z.items_o, [](int r) { return r; }, sh);
+    emit_items<false>(reqs, n_reqs, hkv, kTailPerUnit * num_cus, kTailWhole / kBK, 8, z.tile_o, 1,
+                      own, z.items_o, [](int r) { return r; }, sh);
   } else {
     const bool wide = z.tile_o == arckv::kWideCols;
-    join = emit_items<true>(reqs, n_reqs, hkv, num_cus, wide ? 8 : 4, wide ? 8 : 5, z.tile_o,
-                            per(z.tile_o), own, z.items_o, [](int r) { return r; }, sh);
-    bool shared = false;
-    for (int g = tid; g < n_groups; g += kPlanThreads) shared |= groups[g].tiles > 0;
-    join |= __syncthreads_or(shared);
+    emit_items<true>(reqs, n_reqs, hkv, num_cus, wide ? 8 : 4, wide ? 8 : 5, z.tile_o,
+                     per(z.tile_o), own, z.items_o, [](int r) { return r; }, sh);
   }
-  if (tid == 0) plan[0] = join;
+  // ---- the rows that the join has to look at: those of several pieces, but for what the tail kernel joins itself
+  if (tid == 0) sh.cap = 0;
+  __syncthreads();
+  for (int t = tid; t < total; t += kPlanThreads) {
+    const int2 of = row_of[t];
+    const Part& p = reqs[of.x];
+    const bool cut = (p.whole > 0 && p.pieces_w > 1) || (p.tiles * hkv > p.whole && p.pieces > 1);
+    const bool shared = z.tile_o != kTailCols && of.y >= 0 && groups[of.y].tiles > 0;
+    if (cut || shared || p.tiles == 0) plan[z.off_list + atomicAdd(&sh.cap, 1)] = t;
+  }
+  if (in_lds)
+    for (int i = tid; i < (n_groups + n_reqs) * kPartInts; i += kPlanThreads)
+      plan[i < n_groups * kPartInts ? z.off_group + i : z.off_req + i - n_groups * kPartInts] = reinterpret_cast<int32_t*>(sh.parts)[i];
+  __syncthreads();
+  if (tid == 0) plan[0] = sh.cap;
 }
 
 // ---- joining pieces --------------------------------------------------------------------------------
@@ -368,18 +380,20 @@ struct Joined {
   float m = -INFINITY, sum = 0.f;
   acc4_t acc = {};
 };
-// Adds pieces i0, i0 + step, .. < n.  Their lse come in 16 at a time (a lane each), the partial results four at a time and the
-// first four beside the lse.
+// Adds pieces i0, i0 + step, .. < n.  Their lse come in 16 at a time (a lane each), the partial results eight at a time, the
+// first eight beside the lse.
 template <class Lse, class Row>
 __device__ __forceinline__ void add_pieces(Joined& j, int i0, int step, int n, Lse lse_of, Row row_of) {
-  constexpr int kBatch = 16, kPre = 4;
+  constexpr int kBatch = 16, kLoad = 8;
   const int sub = threadIdx.x % kBatch, mine = (threadIdx.x & 63) / kBatch * kBatch;
   for (; i0 < n; i0 += step * kBatch) {
-    auto piece = [&](int k) -> acc4_t { return i0 + k * step < n ? *row_of(i0 + k * step) : acc4_t{}; };
     const float l = i0 + sub * step < n ? lse_of(i0 + sub * step) : -INFINITY;
-    acc4_t v[kPre];
+    acc4_t v[kLoad];
+    auto load = [&](int k0) {
 #pragma unroll
-    for (int k = 0; k < kPre; ++k) v[k] = piece(k);
+      for (int k = 0; k < kLoad; ++k) v[k] = i0 + (k0 + k) * step < n ? *row_of(i0 + (k0 + k) * step) : acc4_t{};
+    };
+    load(0);
     float top = l;
 #pragma unroll
     for (int d = kBatch / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
@@ -390,19 +404,17 @@ __device__ __forceinline__ void add_pieces(Joined& j, int i0, int step, int n, L
     j.m = m_new;
     j.sum *= alpha;
     j.acc *= alpha;
-    const int nb = min(kBatch, (n - i0 + step - 1) / step);
-    for (int k0 = 0; k0 < nb; k0 += kPre) {
-      acc4_t next[kPre];
 #pragma unroll
-      for (int k = 0; k < kPre; ++k) next[k] = k0 + kPre < nb ? piece(k0 + kPre + k) : acc4_t{};
+    for (int k0 = 0; k0 < kBatch; k0 += kLoad) {
+      if (k0 > 0) {
+        if (i0 + k0 * step >= n) break;
+        load(k0);
+      }
 #pragma unroll
-      for (int k = 0; k < kPre; ++k) {
-        const float a = __shfl(wt, mine + (k0 + k) % kBatch);
-        if (k0 + k < nb) {
-          j.sum += a;
-          j.acc += a * v[k];
-        }
-        v[k] = next[k];
+      for (int k = 0; k < kLoad; ++k) {
+        const float a = __shfl(wt, mine + k0 + k);          // (0 past the last piece)
+        j.sum += a;
+        j.acc += a * v[k];
       }
     }
   }
@@ -457,196 +469,202 @@ __global__ __launch_bounds__(64 * WAVES, 3) void shared_tail_kernel(
   __shared__ float part_m[WAVES][kTailCols], part_l[WAVES][kTailCols];
   __shared__ acc4_t set_o[SHORT ? 1 : SETS][LANES];
   __shared__ float set_m[SETS], set_s[SETS];
-  Work w = {static_cast<int>(blockIdx.x), static_cast<int>(blockIdx.y), 0, 0, INT32_MAX, 0, 1, 0};
-  if constexpr (!SHORT) w = reinterpret_cast<const Work*>(plan + z.off_work_o)[blockIdx.x];
-  if (w.req < 0 || w.req >= n_reqs || w.kvh < 0 || w.kvh >= hkv || w.col_start < 0 || (!SHORT && w.slot >= z.items_o)) return;
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int i16 = lane & 15, g4 = lane >> 4;
-  const int32_t* bt = block_tables + static_cast<int64_t>(w.req) * bt_stride;
-  const int q0 = cu_q[w.req], S = cu_q[w.req + 1] - q0, L = seq_lens[w.req];
-  const int P = L - S, ncols = S * G, held = min(L, bt_stride * 16), nblk = (held + 15) >> 4;
-  const uint32_t nb32 = static_cast<uint32_t>(min(num_blocks, static_cast<int64_t>(INT32_MAX)));
-  const int64_t blk_stride = static_cast<int64_t>(hkv) * 16 * D;
-  const int64_t head = static_cast<int64_t>(w.kvh) * 16 * D;
-  Part group = {};
-  if constexpr (!SHORT) {
-    const int g = reinterpret_cast<const Part*>(plan + z.off_req)[w.req].group;
-    if (g >= 0 && g < n_groups && w.pad0 == 1) group = reinterpret_cast<const Part*>(plan + z.off_group)[g];
-  }
-  const int set = tid / LANES, d4 = tid % LANES;
-  for (int col0 = w.col_start; col0 < (SHORT ? ncols : w.col_start + 1); col0 += kTailCols) {
-    const int n_here = min(ncols - col0, kTailCols);      // columns that are there
-    if (n_here <= 0) return;                              // (uniform)
-    // ---- pieces over shared keys: sets_per sets of lanes have a column -------------------------
-    const int sets_per = n_here * 8 <= SETS ? 8 : n_here * 4 <= SETS ? 4 : n_here * 2 <= SETS ? 2 : 1;
-    auto shared = [&](int c, int from) -> Joined {
-      Joined j;
-      if constexpr (!SHORT) {
-        const int at = col0 + c;
-        const int64_t row = q0 + at / G - group.row0;
-        if (c < n_here && group.tiles > 0 && row >= 0 && row < group.rows) {
-          int64_t first, step;
-          const int n = pieces_of(group, row * G + at % G, w.kvh, hkv, z.tile_p, first, step);
-          add_pieces(j, from, sets_per, n, [&](int i) { return ws_lp[first + i * step]; },
-                     [&](int i) { return reinterpret_cast<const acc4_t*>(ws_op + (first + i * step) * D + 4 * d4); });
+  for (int item = blockIdx.x; SHORT || item < z.items_o; item += gridDim.x) {
+    Work w = {static_cast<int>(blockIdx.x), static_cast<int>(blockIdx.y), 0, 0, INT32_MAX, 0, 1, 0};
+    if constexpr (!SHORT) w = reinterpret_cast<const Work*>(plan + z.off_work_o)[item];
+    if (w.req < 0 || w.req >= n_reqs || w.kvh < 0 || w.kvh >= hkv || w.col_start < 0 || (!SHORT && w.slot >= z.items_o)) {
+      if constexpr (SHORT) return; else continue;
+    }
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int i16 = lane & 15, g4 = lane >> 4;
+    const int32_t* bt = block_tables + static_cast<int64_t>(w.req) * bt_stride;
+    const int q0 = cu_q[w.req], S = cu_q[w.req + 1] - q0, L = seq_lens[w.req];
+    const int P = L - S, ncols = S * G, held = min(L, bt_stride * 16), nblk = (held + 15) >> 4;
+    const uint32_t nb32 = static_cast<uint32_t>(min(num_blocks, static_cast<int64_t>(INT32_MAX)));
+    const int64_t blk_stride = static_cast<int64_t>(hkv) * 16 * D;
+    const int64_t head = static_cast<int64_t>(w.kvh) * 16 * D;
+    Part group = {};
+    if constexpr (!SHORT) {
+      const int g = reinterpret_cast<const Part*>(plan + z.off_req)[w.req].group;
+      if (g >= 0 && g < n_groups && w.pad0 == 1) group = reinterpret_cast<const Part*>(plan + z.off_group)[g];
+    }
+    const int set = tid / LANES, d4 = tid % LANES;
+    for (int col0 = w.col_start; col0 < (SHORT ? ncols : w.col_start + 1); col0 += kTailCols) {
+      const int n_here = min(ncols - col0, kTailCols);      // columns that are there
+      if (n_here <= 0) break;                               // (uniform)
+      // ---- pieces over shared keys: sets_per sets of lanes have a column -------------------------
+      const int sets_per = n_here * 8 <= SETS ? 8 : n_here * 4 <= SETS ? 4 : n_here * 2 <= SETS ? 2 : 1;
+      auto shared = [&](int c, int from) -> Joined {
+        Joined j;
+        if constexpr (!SHORT) {
+          const int at = col0 + c;
+          const int64_t row = q0 + at / G - group.row0;
+          if (c < n_here && group.tiles > 0 && row >= 0 && row < group.rows) {
+            int64_t first, step;
+            const int n = pieces_of(group, row * G + at % G, w.kvh, hkv, z.tile_p, first, step);
+            add_pieces(j, from, sets_per, n, [&](int i) { return ws_lp[first + i * step]; },
+                       [&](int i) { return reinterpret_cast<const acc4_t*>(ws_op + (first + i * step) * D + 4 * d4); });
+          }
+        }
+        return j;
+      };
+      // ---- the keys ------------------------------------------------------------------------------
+      const int col = col0 + i16, tok = col / G;
+      const bool cval = col < ncols && q0 + tok < n_q;
+      const int pos = cval ? P + tok : -1;
+      const int last_tok = (col0 + n_here - 1) / G;
+      const int kv_lo = max(w.kv_start, 0), kv_hi = min(min(w.kv_end, P + last_tok + 1), held);
+      const int min_pos = P + col0 / G;
+      const int steps = kv_hi > kv_lo ? (kv_hi - kv_lo + 31) / 32 : 0;
+      bf16x8_t qf[KS];
+      {
+        const int64_t at = cval ? (static_cast<int64_t>(q0 + tok) * hq + w.kvh * G + col % G) * D : 0;
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) {
+          u32x4_t v;
+          __builtin_memcpy(&v, q + at + 32 * ks + 8 * g4, 16);
+          qf[ks] = cval ? __builtin_bit_cast(bf16x8_t, v) : bf16x8_t{};
         }
       }
-      return j;
-    };
-    Joined mine = shared(set / sets_per, set % sets_per);
-    // ---- the keys ------------------------------------------------------------------------------
-    const int col = col0 + i16, tok = col / G;
-    const bool cval = col < ncols && q0 + tok < n_q;
-    const int pos = cval ? P + tok : -1;
-    const int last_tok = (col0 + n_here - 1) / G;
-    const int kv_lo = max(w.kv_start, 0), kv_hi = min(min(w.kv_end, P + last_tok + 1), held);
-    const int min_pos = P + col0 / G;
-    const int steps = kv_hi > kv_lo ? (kv_hi - kv_lo + 31) / 32 : 0;
-    bf16x8_t qf[KS];
-    {
-      const int64_t at = cval ? (static_cast<int64_t>(q0 + tok) * hq + w.kvh * G + col % G) * D : 0;
+      auto entry = [&](int b) -> int32_t { return b < nblk ? bt[b] : 0; };      // (uniform)
+      auto block_of = [&](int32_t ph) -> int64_t {
+        ARCKV_CHECK_WAVE(ph < 0 || ph >= num_blocks, ARCKV_CHECK_BLOCK);
+        return (static_cast<uint32_t>(ph) >= nb32 ? 0 : ph) * blk_stride + head;
+      };
+      acc4_t o[DM];
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-        u32x4_t v;
-        __builtin_memcpy(&v, q + at + 32 * ks + 8 * g4, 16);
-        qf[ks] = cval ? __builtin_bit_cast(bf16x8_t, v) : bf16x8_t{};
-      }
-    }
-    auto entry = [&](int b) -> int32_t { return b < nblk ? bt[b] : 0; };      // (uniform)
-    auto block_of = [&](int32_t ph) -> int64_t {
-      ARCKV_CHECK_WAVE(ph < 0 || ph >= num_blocks, ARCKV_CHECK_BLOCK);
-      return (static_cast<uint32_t>(ph) >= nb32 ? 0 : ph) * blk_stride + head;
-    };
-    acc4_t o[DM];
+      for (int d = 0; d < DM; ++d) o[d] = acc4_t{};
+      float m_run = -INFINITY, l_run = 0.f;
+      int32_t e0 = 0, e1 = 0;                               // the next step's table entries, read a step ahead
+      auto look_up = [&](int s) {
+        if (s < steps) {
+          e0 = entry((kv_lo + 32 * s) >> 4);
+          e1 = entry(((kv_lo + 32 * s) >> 4) + 1);
+        }
+      };
+      look_up(wave);
+      Joined mine = shared(set / sets_per, set % sets_per);
+      // (K/V a step ahead of their use, at 256 registers and two waves on a SIMD, measured no faster: 16.2 and 16.0 us for 23
+      // requests of 60 to 820 own tokens)
+      for (int s = wave; s < steps; s += WAVES) {
+        const int k0 = kv_lo + 32 * s;
+        const int64_t b0 = block_of(e0), b1 = block_of(e1);
+        bf16x8_t kf[2][KS], vf[DM];
 #pragma unroll
-    for (int d = 0; d < DM; ++d) o[d] = acc4_t{};
-    float m_run = -INFINITY, l_run = 0.f;
-    int32_t e0 = 0, e1 = 0;                               // the step's table entries, read a step ahead
-    if (wave < steps) {
-      e0 = entry((kv_lo + 32 * wave) >> 4);
-      e1 = entry(((kv_lo + 32 * wave) >> 4) + 1);
-    }
-    for (int s = wave; s < steps; s += WAVES) {
-      const int k0 = kv_lo + 32 * s;
-      const int64_t b0 = block_of(e0), b1 = block_of(e1);
-      bf16x8_t kf[2][KS], vf[DM];
+        for (int m = 0; m < 2; ++m) {
+          const int key = 8 * (i16 >> 2) + 4 * m + (i16 & 3);
+          const uint16_t* src = k_pool + (i16 >= 8 ? b1 : b0) + (key & 15) * D + 8 * g4;
 #pragma unroll
-      for (int m = 0; m < 2; ++m) {
-        const int key = 8 * (i16 >> 2) + 4 * m + (i16 & 3);
-        const uint16_t* src = k_pool + (i16 >= 8 ? b1 : b0) + (key & 15) * D + 8 * g4;
+          for (int ks = 0; ks < KS; ++ks) kf[m][ks] = *reinterpret_cast<const bf16x8_t*>(src + 32 * ks);
+        }
+        {
+          const uint16_t* src = v_pool + (g4 >= 2 ? b1 : b0) + i16 * 16 + 8 * (g4 & 1);
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[m][ks] = *reinterpret_cast<const bf16x8_t*>(src + 32 * ks);
-      }
-      {
-        const uint16_t* src = v_pool + (g4 >= 2 ? b1 : b0) + i16 * 16 + 8 * (g4 & 1);
+          for (int d = 0; d < DM; ++d) vf[d] = *reinterpret_cast<const bf16x8_t*>(src + d * 256);
+        }
+        look_up(s + WAVES);
+        acc4_t sc[2] = {acc4_t{}, acc4_t{}};
 #pragma unroll
-        for (int d = 0; d < DM; ++d) vf[d] = *reinterpret_cast<const bf16x8_t*>(src + d * 256);
-      }
-      if (s + WAVES < steps) {
-        e0 = entry((k0 + 32 * WAVES) >> 4);
-        e1 = entry(((k0 + 32 * WAVES) >> 4) + 1);
-      }
-      acc4_t sc[2] = {acc4_t{}, acc4_t{}};
+        for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks)
+          for (int m = 0; m < 2; ++m) sc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[m][ks], qf[ks], sc[m], 0, 0, 0);
+        const int key0 = k0 + 8 * g4;
+        if (k0 + 31 > min_pos || k0 + 32 > kv_hi) {         // (uniform) keys that some column does not see
 #pragma unroll
-        for (int m = 0; m < 2; ++m) sc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[m][ks], qf[ks], sc[m], 0, 0, 0);
-      const int key0 = k0 + 8 * g4;
-      if (k0 + 31 > min_pos || k0 + 32 > kv_hi) {         // (uniform) keys that some column does not see
+          for (int j = 0; j < 8; ++j)
+            if (key0 + j > pos || key0 + j >= kv_hi) sc[j / 4][j % 4] = -INFINITY;
+        }
+        if (k0 + 32 > held) {                               // past the request's end the block may hold anything, NaN too
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (key0 + j > pos || key0 + j >= kv_hi) sc[j / 4][j % 4] = -INFINITY;
-      }
-      if (k0 + 32 > held) {                               // past the request's end the block may hold anything, NaN too
+          for (int d = 0; d < DM; ++d) {
+            u32x4_t v = __builtin_bit_cast(u32x4_t, vf[d]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              v[j] = key0 + 2 * j >= held ? 0 : key0 + 2 * j + 1 >= held ? v[j] & 0xFFFFu : v[j];
+            vf[d] = __builtin_bit_cast(bf16x8_t, v);
+          }
+        }
+        float mx = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) mx = fmaxf(mx, sc[j / 4][j % 4]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = max_halves(mx) * scale_log2;
+        const float m_new = fmaxf(m_run, mx);
+        const float mu = m_new == -INFINITY ? 0.f : m_new;
+        const float alpha = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
+        m_run = m_new;
+        float p[8], sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[j] = fast_exp2(fmaf(sc[j / 4][j % 4], scale_log2, -mu));
+          sum += p[j];
+        }
+        l_run = l_run * alpha + sum;
+        // probabilities enter P.V as bf16 (off by at most 2^-8 of themselves); the sum is of the unrounded ones
+        u32x4_t pw;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          pw[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{p[2 * j], p[2 * j + 1]}, bf16x2_t));
 #pragma unroll
         for (int d = 0; d < DM; ++d) {
-          u32x4_t v = __builtin_bit_cast(u32x4_t, vf[d]);
-#pragma unroll
-          for (int j = 0; j < 4; ++j)
-            v[j] = key0 + 2 * j >= held ? 0 : key0 + 2 * j + 1 >= held ? v[j] & 0xFFFFu : v[j];
-          vf[d] = __builtin_bit_cast(bf16x8_t, v);
+          o[d] *= alpha;
+          o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], __builtin_bit_cast(bf16x8_t, pw), o[d], 0, 0, 0);
         }
       }
-      float mx = -INFINITY;
+      // ---- the waves' results: lane holds dims 16 d + 4 g .. + 3 of its column -------------------
+      l_run += __shfl_xor(l_run, 16);
+      l_run = sum_halves(l_run);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) mx = fmaxf(mx, sc[j / 4][j % 4]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = max_halves(mx) * scale_log2;
-      const float m_new = fmaxf(m_run, mx);
-      const float mu = m_new == -INFINITY ? 0.f : m_new;
-      const float alpha = m_run == -INFINITY ? 0.f : fast_exp2(m_run - m_new);
-      m_run = m_new;
-      float p[8], sum = 0.f;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        p[j] = fast_exp2(fmaf(sc[j / 4][j % 4], scale_log2, -mu));
-        sum += p[j];
+      for (int d = 0; d < DM; ++d) *reinterpret_cast<acc4_t*>(&part_o[wave][i16][16 * d + 4 * g4]) = o[d];
+      if (g4 == 0) {
+        part_m[wave][i16] = m_run;
+        part_l[wave][i16] = l_run;
       }
-      l_run = l_run * alpha + sum;
-      // probabilities enter P.V as bf16 (off by at most 2^-8 of themselves); the sum is of the unrounded ones
-      u32x4_t pw;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        pw[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{p[2 * j], p[2 * j + 1]}, bf16x2_t));
-#pragma unroll
-      for (int d = 0; d < DM; ++d) {
-        o[d] *= alpha;
-        o[d] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[d], __builtin_bit_cast(bf16x8_t, pw), o[d], 0, 0, 0);
-      }
-    }
-    // ---- the waves' results: lane holds dims 16 d + 4 g .. + 3 of its column -------------------
-    l_run += __shfl_xor(l_run, 16);
-    l_run = sum_halves(l_run);
-#pragma unroll
-    for (int d = 0; d < DM; ++d) *reinterpret_cast<acc4_t*>(&part_o[wave][i16][16 * d + 4 * g4]) = o[d];
-    if (g4 == 0) {
-      part_m[wave][i16] = m_run;
-      part_l[wave][i16] = l_run;
-    }
-    for (int c0 = 0; c0 < n_here; c0 += SETS / sets_per) {
-      if (c0 > 0) mine = shared(c0 + set / sets_per, set % sets_per);
-      if (!SHORT && sets_per > 1) {
-        set_o[set][d4] = mine.acc;
-        if (d4 == 0) {
-          set_m[set] = mine.m;
-          set_s[set] = mine.sum;
+      for (int c0 = 0; c0 < n_here; c0 += SETS / sets_per) {
+        if (c0 > 0) mine = shared(c0 + set / sets_per, set % sets_per);
+        if (!SHORT && sets_per > 1) {
+          set_o[set][d4] = mine.acc;
+          if (d4 == 0) {
+            set_m[set] = mine.m;
+            set_s[set] = mine.sum;
+          }
         }
-      }
-      __syncthreads();
-      const int c = c0 + set / sets_per;
-      if (c < n_here && set % sets_per == 0 && q0 + (col0 + c) / G < n_q) {
-        if (!SHORT)
-          for (int k = 1; k < sets_per; ++k) add_sum(mine, set_m[set + k], set_s[set + k], set_o[set + k][d4]);
-        Joined keys;
+        __syncthreads();
+        const int c = c0 + set / sets_per;
+        if (c < n_here && set % sets_per == 0 && q0 + (col0 + c) / G < n_q) {
+          if (!SHORT)
+            for (int k = 1; k < sets_per; ++k) add_sum(mine, set_m[set + k], set_s[set + k], set_o[set + k][d4]);
+          Joined keys;
 #pragma unroll
-        for (int v = 0; v < WAVES; ++v)
-          add_sum(keys, part_m[v][c], part_l[v][c], *reinterpret_cast<const acc4_t*>(&part_o[v][c][4 * d4]));
-        if (SHORT || w.pad0 == 1) {
-          add_sum(mine, keys.m, keys.sum, keys.acc);
-          const int at = col0 + c;
-          write_joined(mine, out, lse_out, static_cast<int64_t>(q0 + at / G) * hq + w.kvh * G + at % G, D, d4);
-        } else {
-          const float inv = keys.sum > 0.f ? 1.f / keys.sum : 0.f;
-          const int64_t at = static_cast<int64_t>(w.slot) * kTailCols + c;
-          *reinterpret_cast<acc4_t*>(ws_oo + at * D + 4 * d4) = keys.acc * inv;
-          if (d4 == 0) ws_lo[at] = keys.sum > 0.f ? keys.m + __log2f(keys.sum) : keys.sum == 0.f ? -INFINITY : keys.sum;
+          for (int v = 0; v < WAVES; ++v)
+            add_sum(keys, part_m[v][c], part_l[v][c], *reinterpret_cast<const acc4_t*>(&part_o[v][c][4 * d4]));
+          if (SHORT || w.pad0 == 1) {
+            add_sum(mine, keys.m, keys.sum, keys.acc);
+            const int at = col0 + c;
+            write_joined(mine, out, lse_out, static_cast<int64_t>(q0 + at / G) * hq + w.kvh * G + at % G, D, d4);
+          } else {
+            const float inv = keys.sum > 0.f ? 1.f / keys.sum : 0.f;
+            const int64_t at = static_cast<int64_t>(w.slot) * kTailCols + c;
+            *reinterpret_cast<acc4_t*>(ws_oo + at * D + 4 * d4) = keys.acc * inv;
+            if (d4 == 0) ws_lo[at] = keys.sum > 0.f ? keys.m + __log2f(keys.sum) : keys.sum == 0.f ? -INFINITY : keys.sum;
+          }
         }
+        __syncthreads();
       }
-      __syncthreads();
     }
+    if constexpr (SHORT) break;
   }
 }
 
 // ---- the join ------------------------------------------------------------------------------------
 // What the items have not joined: rows over shared and own keys in tiles, and own keys in several pieces.  plan[0] says
-// whether there is any.  With few rows (SPLIT) a work-group has one row and head and its sets of lanes take the pieces in turn;
+// how many rows that may be, and its list which.  With few rows (SPLIT) a work-group has one row and head and its sets of lanes take the pieces in turn;
 // otherwise it has a row and its sets take the heads.  What bounds it is reading the partial results (fp32).
 constexpr int64_t kSplitPairs = 8192;   // most (row, head) pairs whose pieces are split over a work-group
 template <int D, bool SPLIT>
 __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__ out, float* __restrict__ lse_out,
-                                                          const int32_t* __restrict__ plan, SharedSizes z,
-                                                          const int32_t* __restrict__ cu_q, int n_reqs, int n_groups,
+                                                          const int32_t* __restrict__ plan, SharedSizes z, int n_reqs, int n_groups,
                                                           int64_t n_q, int hq, int hkv, int G, const float* __restrict__ ws_op,
                                                           const float* __restrict__ ws_lp, const float* __restrict__ ws_oo,
                                                           const float* __restrict__ ws_lo) {
@@ -654,8 +672,10 @@ __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__
   __shared__ acc4_t set_o[SPLIT ? SETS : 1][LANES];
   __shared__ float set_m[SETS], set_s[SETS];
   const int set = threadIdx.x / LANES, d4 = threadIdx.x % LANES;
-  const int64_t t = SPLIT ? blockIdx.x / hq : blockIdx.x;
-  if (plan[0] == 0 || t >= n_q || t >= cu_q[n_reqs]) return;
+  const int64_t at = SPLIT ? blockIdx.x / hq : blockIdx.x;
+  if (at >= plan[0] || at >= n_q) return;
+  const int64_t t = plan[z.off_list + at];
+  if (t < 0 || t >= n_q) return;
   const int2 of = reinterpret_cast<const int2*>(plan + z.off_row)[t];
   auto part = [&](int64_t off, int i, int n) {
     const Part p = i >= 0 && i < n ? reinterpret_cast<const Part*>(plan + off)[i] : Part{};
@@ -816,15 +836,15 @@ extern "C" int32_t arckv_shared_prefix_attention(
     if (z.tile_o != kTailCols) {
       part(z.tile_o, z.items_o, plan + z.off_work_o, cu_q, seq_lens, ws_oo, ws_lo, lse);
     } else {
-      const dim3 grid(static_cast<unsigned>(z.items_o));
-      if (std::min<int64_t>(n_reqs, max_q) * num_kv_heads <= num_cus) tail(W8{}, std::false_type{}, grid);
-      else tail(W4{}, std::false_type{}, grid);
+      if (std::min<int64_t>(n_reqs, max_q) * num_kv_heads <= num_cus)
+        tail(W8{}, std::false_type{}, dim3(static_cast<unsigned>(std::min<int64_t>(num_cus, z.items_o))));
+      else tail(W4{}, std::false_type{}, dim3(static_cast<unsigned>(z.items_o)));
       if (bt_stride * 16 <= kTailWhole) return;           // no request's own keys can be cut
     }
     const int64_t pairs = max_q * num_q_heads;
     auto join = [&](auto split, int64_t groups) {
       hipLaunchKernelGGL((shared_join_kernel<D, decltype(split)::value>), dim3(static_cast<unsigned>(groups)), dim3(256), 0, st, op,
-                         lse, plan, z, cu_q, n_reqs, n_groups, max_q, num_q_heads, num_kv_heads, GG, ws_op, ws_lp, ws_oo, ws_lo);
+                         lse, plan, z, n_reqs, n_groups, max_q, num_q_heads, num_kv_heads, GG, ws_op, ws_lp, ws_oo, ws_lo);
     };
     if (pairs <= kSplitPairs) join(std::true_type{}, pairs); else join(std::false_type{}, max_q);
   };

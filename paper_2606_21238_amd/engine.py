@@ -461,9 +461,9 @@ class PrefillEngine:
         blocks and rows last (arckv_batch_maps).  Afterwards sb.seq_lens, cu_q, block_tables and slot_mapping are the step's,
         as is the plan of its shared_attention() calls."""
         b = sb.bounds
-        self._held(sb, stream)
         if self._bad(new_tokens, (b.n_reqs,), 4) or new_tokens.is_floating_point():
             raise ValueError(f"new_tokens must be contiguous int32 [{b.n_reqs}] on the device")
+        self._held(sb, stream)
         true = (None, None) if sb.true_lens is None else (sb.true_offset.data_ptr(), sb.true_lens.data_ptr())
         held, count, cu = sb.seq_lens.data_ptr(), sb.free_count.data_ptr(), sb.cu_q.data_ptr()
         self._call("arckv_batch_maps", stream, new_tokens.data_ptr(), held, b.n_reqs, sb.block_tables.data_ptr(), b.bt_stride,
