@@ -608,7 +608,8 @@ int32_t arckv_kv_compact_mx4(void* kv_pool, const int32_t* block_tables, int32_t
  * bf16, y = h / sqrt(mean(h^2) + eps) * weight (fp32, of the unrounded h), and out as out_format says:
  *   ARCKV_OUT_BF16  out: bf16 [n_tokens][hidden], y rounded to nearest even;
  *   ARCKV_OUT_E4M3  out: 8-bit floats (E4M3 without infinities) [n_tokens][hidden], scales: fp32 [n_tokens],
- *                   scale = max|y| / 448 over the row, out = y / scale rounded to nearest even (0 where scale is 0).
+ *                   scale = max|y| / 448 over the row (0 if that is no normal fp32 number), out = y / scale rounded
+ *                   to nearest even (0 where scale is 0).
  * A row with a NaN or an infinity gives what these formulas give (its scale may be NaN, its codes 0x7F).
  * x: device bf16, rows x_stride elements apart (x_stride >= hidden).  residual and residual_out: device bf16
  * [n_tokens][hidden], both or neither; weight: device bf16 [hidden].  residual_out may be residual or (x_stride =
@@ -662,7 +663,7 @@ int32_t arckv_shared_prefix_sizes(int32_t n_reqs, int32_t n_groups, int64_t max_
                                   int64_t* plan_ints, int64_t* ws_bytes);
 
 /* The plan of a step.  group_start [n_groups + 1], prefix_lens [n_groups], cu_q [n_reqs + 1], seq_lens [n_reqs], plan
- * [plan_ints]: device int32, the plan 16-byte aligned.  0 <= max_group_q, max_new <= max_q <= 2^24, n_groups <=
+ * [plan_ints]: device int32, the plan 16-byte aligned.  0 <= max_group_q, max_new <= max_q <= 2^23, n_groups <=
  * n_reqs <= 2^20 (else EINVAL); ENOSPC if plan_ints is too small. */
 int32_t arckv_shared_prefix_plan(const int32_t* group_start, const int32_t* prefix_lens, int32_t n_groups,
                                  const int32_t* cu_q, const int32_t* seq_lens, int32_t n_reqs, int64_t max_q,

@@ -13,6 +13,9 @@ namespace {
 
 constexpr int kNormMaxHidden = 32768;   // 1024 threads x 4 chunks x 8 values: all that 1024 threads' registers hold
 
+constexpr int64_t kNormMaxRows = int64_t{1} << 21;     // rows of a launch (2^32 threads would be too many)
+constexpr float kNormMinScale = 1.17549435e-38f;        // the smallest normal number: 1 / scale is finite
+
 // 8 values of a row: of an aligned row the 8 that follow each other, otherwise (ANY) every TH-th, so that 2-byte
 // loads of neighbouring lanes are neighbours.
 template <int TH, bool ANY>
@@ -120,7 +123,8 @@ __global__ __launch_bounds__(TH) void add_rms_norm_kernel(const uint16_t* x, int
 #pragma unroll
       for (int j = 0; j < 8; ++j) top = max(top, __builtin_bit_cast(uint32_t, h[c][j]) & 0x7FFFFFFFu);
     top = join_threads<TH>(top, top_of, [](uint32_t a, uint32_t b) { return max(a, b); });
-    const float scale = __builtin_bit_cast(float, top) / 448.f;
+    float scale = __builtin_bit_cast(float, top) / 448.f;
+    if (scale < kNormMinScale) scale = 0.f;
     if (threadIdx.x == 0) scales[row] = scale;
     // y / scale as a product with 1 / scale: off by 1.5 steps of fp32 from the quotient, far below e4m3's
     const float inv = scale == 0.f ? 0.f : 1.f / scale;
@@ -147,8 +151,7 @@ __global__ __launch_bounds__(TH) void add_rms_norm_kernel(const uint16_t* x, int
         if (norm_at<TH, ANY>(c, 0) < hidden) *reinterpret_cast<uint2*>(o + norm_at<TH, ANY>(c, 0)) = make_uint2(w[0], w[1]);
       }
     }
-  }
-}
+  }}
 
 template <bool ANY, bool E4M3>
 void add_rms_norm_launch(const uint16_t* x, int64_t x_stride, const uint16_t* residual, uint16_t* residual_out,
@@ -157,8 +160,11 @@ void add_rms_norm_launch(const uint16_t* x, int64_t x_stride, const uint16_t* re
   const int chunks = (hidden + 7) / 8;
   auto go = [&](auto th, auto ch) {
     constexpr int TH = decltype(th)::value, CH = decltype(ch)::value;
-    hipLaunchKernelGGL((add_rms_norm_kernel<TH, CH, ANY, E4M3>), dim3(static_cast<unsigned>(n_tokens)), dim3(TH), 0, st, x,
-                       x_stride, residual, residual_out, weight, hidden, eps, out, scales);
+    for (int64_t r = 0; r < n_tokens; r += kNormMaxRows)
+      hipLaunchKernelGGL((add_rms_norm_kernel<TH, CH, ANY, E4M3>), dim3(static_cast<unsigned>(std::min(n_tokens - r, kNormMaxRows))),
+                         dim3(TH), 0, st, x + r * x_stride, x_stride, residual == nullptr ? nullptr : residual + r * hidden,
+                         residual_out == nullptr ? nullptr : residual_out + r * hidden, weight, hidden, eps,
+                         static_cast<char*>(out) + r * hidden * (E4M3 ? 1 : 2), E4M3 ? scales + r : nullptr);
   };
   using std::integral_constant;
   using I1 = integral_constant<int, 1>;

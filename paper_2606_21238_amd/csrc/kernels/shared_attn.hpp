@@ -711,7 +711,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__
 // What the three calls check of the bounds that they share.
 int32_t check_shared(const char* fn, int32_t n_reqs, int32_t n_groups, int64_t max_q, int64_t max_group_q, int64_t max_new,
                      int32_t bt_stride, int32_t hq, int32_t hkv, int32_t head_dim, int32_t num_cus) {
-  if (n_reqs < 0 || n_reqs > (1 << 20) || n_groups < 0 || n_groups > std::max(n_reqs, 1) || max_q < 0 || max_q > (1 << 24) ||
+  if (n_reqs < 0 || n_reqs > (1 << 20) || n_groups < 0 || n_groups > std::max(n_reqs, 1) || max_q < 0 || max_q > (1 << 23) ||
       max_group_q < 0 || max_group_q > max_q || max_new < 0 || max_new > max_q || bt_stride < 0 || bt_stride > (1 << 26) ||
       hq < 1 || hkv < 1 || hq % hkv != 0 || num_cus < 1 || num_cus > (1 << 16))
     return arckv::fail(ARCKV_EINVAL, "%s: bad sizes", fn);

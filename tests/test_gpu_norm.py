@@ -170,6 +170,36 @@ def test_rows_of_zeros_infinities_and_nan():
     check_e4m3(codes[3:], scales[3:], y)
 
 
+def test_scales_that_are_no_normal_numbers():
+    """Rows so small that max|y| / 448 is below 2^-126 stand for zeros; the next larger ones are kept."""
+    print_case("norm tiny scales")
+    x = torch.ones(2, 64, dtype=torch.bfloat16)
+    w = torch.full((64,), 2.0 ** -118, dtype=torch.bfloat16)      # y = 2^-118, and 2^-118 / 448 < 2^-126
+    codes, scales = torch.full((2, 64), 0x55, dtype=torch.uint8, device=DEV), torch.ones(2, device=DEV)
+    ak.add_rms_norm(x.to(DEV), w.to(DEV), codes, 0.0, scales=scales)
+    assert (codes == 0).all() and (scales == 0).all()
+    ak.add_rms_norm(x.to(DEV), (w * 4).to(DEV), codes, 0.0, scales=scales)
+    assert (codes == 0x7E).all() and ((scales.double() * 448 - 2.0 ** -116).abs() <= SLACK * 2.0 ** -116).all()     # 448
+
+
+def test_more_rows_than_a_launch_takes():
+    """A launch has 2^21 rows at most."""
+    print_case("norm 2^21 + 9 rows")
+    n = (1 << 21) + 9
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.randn(n, 16, generator=g, device=DEV).to(torch.bfloat16)
+    w = torch.ones(16, dtype=torch.bfloat16, device=DEV)
+    out, codes, scales = torch.empty_like(x), torch.empty(n, 16, dtype=torch.uint8, device=DEV), torch.empty(n, device=DEV)
+    ak.add_rms_norm(x, w, out, EPS)
+    ak.add_rms_norm(x, w, codes, EPS, scales=scales)
+    at = torch.cat([torch.arange(64), torch.arange(n - 64, n)])
+    _, y = ref(x[at].cpu(), None, w.cpu())
+    check_bf16(out[at], y, "many rows")
+    check_e4m3(codes[at], scales[at], y)
+    ss = out.float().square().mean(1)
+    assert bool(((ss - 1).abs() < 0.05).all())       # every row was normed (16 roundings of 2^-8)
+
+
 def test_many_rows_other_stream_and_graph():
     print_case("norm 70001 rows, stream, graph")
     x, res, w = inputs(70001, 64, 11)

@@ -139,7 +139,7 @@ def sizes(n=3, g=2, q=6, gq=4, new=2, stride=5, hq=8, hkv=2, d=64, cus=256):
 def test_shared_prefix_calls_refuse():
     E, U, L = _lib.EINVAL, _lib.EUNSUPPORTED, _lib.load()
     assert sizes() == _lib.OK
-    for kw in (dict(n=-1), dict(n=(1 << 20) + 1), dict(g=4), dict(g=-1), dict(q=-1), dict(q=(1 << 24) + 1), dict(gq=7), dict(gq=-1), dict(new=7),
+    for kw in (dict(n=-1), dict(n=(1 << 20) + 1), dict(g=4), dict(g=-1), dict(q=-1), dict(q=(1 << 23) + 1), dict(gq=7), dict(gq=-1), dict(new=7),
                dict(stride=-1), dict(stride=(1 << 26) + 1), dict(hq=9), dict(hq=0), dict(hkv=0), dict(cus=0)):
         assert sizes(**kw) == E, kw
     assert sizes(d=96) == sizes(hq=6) == U
