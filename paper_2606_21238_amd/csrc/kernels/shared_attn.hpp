@@ -68,9 +68,14 @@ SharedSizes shared_sizes(int64_t n_reqs, int64_t n_groups, int64_t max_q, int64_
 }
 
 // Few and short requests read all of their keys in one launch, shared or not: the shared ones come from the caches
-// then, and the launches that would save them cost more.
+// then, and the launches that would save them cost more.  us, one launch and planned (32 / 8 heads of 128 unless stated;
+// prefix + own tokens): 4 x 280 of 4 / 2 heads of 64 5.1 and 15.6; 16 x (256 + 100) 7.4 and 18.0; 64 x (256 + 100), 93 MB by
+// request, 14.2 and 22.2; 64 x (512 + 300), 213 MB, 25.6 and 35.5; 64 x (896 + 100), 261 MB, 27.3 and 26.6; 256 x (64 + 30), 2048
+// work-groups, 31.1 and 30.8; 16 x 1688 20.9 and 21.0; 4 x 1988 22.5 and 20.0.
+constexpr int64_t kShortKeys = 1536, kShortBytes = int64_t{224} << 20, kShortGroups = 1024;
 bool short_route(const SharedSizes& z, int64_t n_reqs, int64_t bt_stride, int hkv, int head_dim) {
-  return z.tile_o == kTailCols && bt_stride * 16 <= 1024 && n_reqs * bt_stride * 16 * hkv * head_dim * 4 <= (int64_t{32} << 20);
+  return z.tile_o == kTailCols && bt_stride * 16 <= kShortKeys && n_reqs * hkv <= kShortGroups &&
+         n_reqs * bt_stride * 16 * hkv * head_dim * 4 <= kShortBytes;
 }
 
 // ---- the plan ---------------------------------------------------------------------------------
@@ -90,10 +95,13 @@ struct PlanShared {
 };
 
 // The most key tiles of a piece, for n parts (units to cut and key tiles of part i from `size`) in at most `most` items: of 64
-// candidates (the longest part in 1, 2, .. 64 pieces) the one whose rounds of the chip take least: a round of `units`
-// items takes its longest piece and `over` key tiles more.
+// candidates (the longest part in 1, 2, .. 64 pieces) the one that takes least, in key tiles: a round of `units` items takes
+// its longest piece and `over` tiles more, and an item's partial results take the chip w64 / 64 tiles to write and read (64
+// rows of 32 / 8 heads of 128 on a shared prefix of 2048, 4096 and 8192: 34.6, 36.6 and 42.1 us with pieces of 4, 4 and 8
+// tiles, 38.3, 39.5 and 44.3 with 8, 8 and 4).
 template <class Size>
-__device__ __forceinline__ int choose_cap(int n, int64_t most, int units, int min_cap, int over, Size size, PlanShared& sh) {
+__device__ __forceinline__ int choose_cap(int n, int64_t most, int units, int min_cap, int over, int w64, Size size,
+                                          PlanShared& sh) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int longest = 0;
   for (int i = tid; i < n; i += kPlanThreads) {
@@ -121,7 +129,7 @@ __device__ __forceinline__ int choose_cap(int n, int64_t most, int units, int mi
     items = 0;
     for (int w = 0; w < kPlanThreads / 64; ++w) items += sh.items[w][lane];
     const int64_t rounds = (items + units - 1) / units;
-    int64_t cost = items <= most ? rounds * (cap + over) : INT64_MAX / 2;
+    int64_t cost = items <= most ? rounds * (cap + over) * 64 + items * w64 : INT64_MAX / 2;
     int best = lane;
 #pragma unroll
     for (int d = 32; d > 0; d >>= 1) {
@@ -166,7 +174,7 @@ __device__ __forceinline__ int64_t sums_before(int64_t v, int64_t& total, PlanSh
 // units: 272 us, and 339 with every tile cut in two).  Units of the same keys lie `heads` apart: with 8 heads on one XCD.
 // DIRECT: a unit of one piece that nothing joins has slot -1, and its kernel writes the result.
 template <bool DIRECT, class ReqOf>
-__device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, int over, int tile_cols, int per, Work* work,
+__device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, int over, int w64, int tile_cols, int per, Work* work,
                            int64_t most, ReqOf req_of, PlanShared& sh) {
   const int tid = threadIdx.x;
   auto keys_of = [](const Part& p) { return p.tiles > 0 ? (p.keys1 - p.keys0 + kBK - 1) / kBK : 0; };
@@ -195,7 +203,7 @@ __device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, 
     at_w += total;
   }
   __syncthreads();
-  const int cap = choose_cap(n, most - at_w, units, min_cap, over, [=](int i, int& cut, int& keys) {
+  const int cap = choose_cap(n, most - at_w, units, min_cap, over, w64, [=](int i, int& cut, int& keys) {
     keys = keys_of(parts[i]);
     cut = keys > 0 ? parts[i].tiles * hkv - parts[i].whole : 0;
   }, sh);
@@ -342,20 +350,18 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
   }
   __syncthreads();
   // ---- the cuts and the items ------------------------------------------------------------------
-  auto per = [](int tile) { return tile == arckv::kNarrowCols ? arckv::kListItems : 1; };
+  auto tiles = [&](auto direct, Part* parts, int n, int tile, int64_t off, int64_t most, auto req_of) {
+    const bool wide = tile == arckv::kWideCols;
+    emit_items<decltype(direct)::value>(parts, n, hkv, num_cus, wide ? 4 : 2, wide ? 8 : 5, wide ? 2 : 1, tile,
+                                        wide ? 1 : arckv::kListItems, reinterpret_cast<Work*>(plan + off), most, req_of, sh);
+  };
   if (n_groups > 0)
-    emit_items<false>(groups, n_groups, hkv, num_cus, z.tile_p == arckv::kWideCols ? 8 : 4, z.tile_p == arckv::kWideCols ? 8 : 5,
-                      z.tile_p, per(z.tile_p), reinterpret_cast<Work*>(plan + z.off_work_p), z.items_p,
-                      [&](int g) { return groups[g].group; }, sh);
-  auto* own = reinterpret_cast<Work*>(plan + z.off_work_o);
-  if (z.tile_o == kTailCols) {
-    emit_items<false>(reqs, n_reqs, hkv, kTailPerUnit * num_cus, kTailWhole / kBK, 8, z.tile_o, 1,
-                      own, z.items_o, [](int r) { return r; }, sh);
-  } else {
-    const bool wide = z.tile_o == arckv::kWideCols;
-    emit_items<true>(reqs, n_reqs, hkv, num_cus, wide ? 8 : 4, wide ? 8 : 5, z.tile_o,
-                     per(z.tile_o), own, z.items_o, [](int r) { return r; }, sh);
-  }
+    tiles(std::false_type{}, groups, n_groups, z.tile_p, z.off_work_p, z.items_p, [&](int g) { return groups[g].group; });
+  if (z.tile_o == kTailCols)
+    emit_items<false>(reqs, n_reqs, hkv, kTailPerUnit * num_cus, kTailWhole / kBK, 8, 0, kTailCols, 1,
+                      reinterpret_cast<Work*>(plan + z.off_work_o), z.items_o, [](int r) { return r; }, sh);
+  else
+    tiles(std::true_type{}, reqs, n_reqs, z.tile_o, z.off_work_o, z.items_o, [](int r) { return r; });
   // ---- the rows that the join has to look at: those of several pieces, but for what the tail kernel joins itself
   if (tid == 0) sh.cap = 0;
   __syncthreads();
