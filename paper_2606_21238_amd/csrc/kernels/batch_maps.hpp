@@ -6,15 +6,17 @@
 // that want any, and the blocks taken are the top of the free stack, in order.
 //
 // A few thousand integers: what bounds it is latency.  One work-group scans the requests and writes lengths and
-// offsets; up to kMapsInOne slots (a decode step: 64 requests 6.3 us) it writes their table entries and slots too, more are
-// left to a second launch, which finds a slot's request in cu_q and counts the blocks of the requests before it anew
-// (they follow from seq_lens and cu_q): 4096 requests of 60 tokens took 50 us with the table entries in the scan.
+// offsets; up to kMapsInOne slots (a decode step: 64 requests 4.9 us) it writes their table entries and slots too, more are
+// left to a second launch, which counts the blocks of the requests before its own anew
+// (they follow from seq_lens and cu_q): 4096 requests of 60 tokens 8.0 and 9.7 us, 50 with the table entries in the scan.
 #pragma once
 
 namespace {
 
 constexpr int kMapsThreads = 1024;
-constexpr int kMapsInOne = 8192;      // most slots that the scanning work-group writes itself
+// Most slots and requests whose maps the scanning work-group writes whole.  us in one launch and in two (inside a graph): 64
+// requests of 16, 64 and 120 tokens 5.3, 7.4 and 9.4 against 10.7, 11.1 and 11.0; 2000 of one 9.3 and 14.6; 4000 of two 20.7 and 17.2.
+constexpr int kMapsInOne = 8192, kMapsInOneReqs = 2048;
 
 __device__ __forceinline__ int64_t shfl_up64(int64_t v, int d) {
   const int lo = __shfl_up(static_cast<int>(v), d), hi = __shfl_up(static_cast<int>(v >> 32), d);
@@ -283,7 +285,7 @@ extern "C" int32_t arckv_batch_maps(const int32_t* new_tokens, const int32_t* he
     return arckv::fail(ARCKV_EINVAL, "batch_maps: NULL pointer");
   auto* st = static_cast<hipStream_t>(stream);
   const int32_t cap = static_cast<int32_t>(slot_cap);
-  if (cap <= kMapsInOne) {
+  if (cap <= kMapsInOne && n_reqs <= kMapsInOneReqs) {
     hipLaunchKernelGGL(batch_maps_kernel<true>, dim3(1), dim3(kMapsThreads), 0, st, new_tokens, held, n_reqs, block_tables,
                        bt_stride, free_blocks, free_cap, free_count, free_left, cu_q, seq_lens, true_offset, true_lens,
                        slot_mapping, cap, num_blocks);

@@ -7,18 +7,26 @@
 //   o = sum_i 2^(l_i - M) o_i / sum_i 2^(l_i - M),  M = max_i l_i,  o_i = softmax over piece i, l_i its lse.
 //
 //  * shared_plan_kernel (once a step; the layers share its plan): how many keys the groups share in truth (all
-//    their rows must see them; whole tiles of 64), the cuts, and the work items, from lengths on the device.
+//    their rows must see them; whole tiles of 64), the cuts, and the work items, from lengths on the device.  One work-group,
+//    a chain of scans and searches: 21 to 24 us for 64 requests, 72 for 1000.
 //  * the shared keys: the attention kernels above, given a group as a request whose rows are those of
-//    all its requests and whose length is P + rows, so that every row sees all keys below P.
+//    all its requests and whose length is P + rows, so that every row sees all keys below P.  8192 tokens of 8 heads of 128
+//    for 92 columns (34 MB, narrow tiles) 16 us, of which the stream is 6; 32768 tokens for 184 columns (134 MB, wide tiles) 40
+//    us; 8192 tokens for 10240 columns (0.34 PFLOP, wide) 294 us, 1.17 PFLOP/s.
 //  * the own keys: shared_tail_kernel below for decode steps and few rows, the kernels above for more.
 //  * shared_join_kernel: the join, and log-sum-exp.
+// Against the plan that reads every request's keys by itself (the attention call of a planned batch), us: 64 rows on 8192 + 300
+// tokens (32 / 8 heads) 42 and 293; 32 on 32768 + 400 (64 / 8) 63 and 565; 96 in 8 groups on 4000 + 500 (40 / 8) 75 and 243; 16 x
+// 128 on 8192 (40 / 8) 329 and 367.  Where nothing is shared it costs the join: 64 groups of one, 2048 + 300 tokens, 128 and 116.
 #pragma once
 
 namespace {
 
 constexpr int kTailCols = 16;             // columns of an item of the tail kernel
 constexpr int kTailPerUnit = 3;           // tail work-groups (of four waves) that a compute unit holds at a time
-constexpr int kTailWhole = 1024;          // own keys of a request that are not cut
+// Own keys of a request that are not cut: at most this many key steps set the launch's end, and fewer cuts leave fewer rows to
+// the join.  us with 512 and 1024: 64 requests of 2000 own tokens 139 and 129, 32 of 900 79 and 73; 2 of 6000 31 and 34.
+constexpr int kTailWhole = 1024;
 constexpr int kPlanThreads = 1024;
 constexpr int kMaxPieceTiles = arckv::kMaxItemKeys / kBK;
 
@@ -88,7 +96,7 @@ __device__ __forceinline__ int64_t shfl64(int64_t v, int src) {
 constexpr int kPlanParts = 1024;          // groups and requests whose entries are made in LDS
 struct PlanShared {
   Part parts[kPlanParts];
-  int64_t wave[kPlanThreads / 64];
+  uint32_t wave[kPlanThreads / 64];
   int64_t items[kPlanThreads / 64][64];   // of every candidate cut, by the wave that counted
   int32_t top[kPlanThreads / 64];
   int32_t cap;
@@ -118,10 +126,16 @@ __device__ __forceinline__ int choose_cap(int n, int64_t most, int units, int mi
   for (int w = 0; w < kPlanThreads / 64; ++w) longest = max(longest, sh.top[w]);
   const int cap = min(max((longest + lane) / (lane + 1), min_cap), kMaxPieceTiles);
   int64_t items = 0;
+  const float inv = 1.f / static_cast<float>(cap);
+#pragma unroll 2
   for (int i = wave; i < n; i += kPlanThreads / 64) {
     int tiles, keys;
     size(i, tiles, keys);
-    items += static_cast<int64_t>(tiles) * ((keys + cap - 1) / cap);
+    const int x = keys + cap - 1;                       // below 2^24: the quotient by way of fp32 is at most 1 off
+    int pieces = static_cast<int>(static_cast<float>(x) * inv);
+    pieces -= pieces * cap > x;
+    pieces += (pieces + 1) * cap <= x;
+    items += static_cast<int64_t>(tiles) * pieces;
   }
   sh.items[wave][lane] = items;
   __syncthreads();
@@ -147,26 +161,30 @@ __device__ __forceinline__ int choose_cap(int n, int64_t most, int units, int mi
   return sh.cap;
 }
 
-// Exclusive sums over the threads of the work-group, and the total.
-__device__ __forceinline__ int64_t sums_before(int64_t v, int64_t& total, PlanShared& sh) {
+// Exclusive sums over the threads of the work-group, and the total; sums of more than 2^30 stay there (a batch within its bounds
+// has fewer of whatever is counted).
+__device__ __forceinline__ uint32_t add_sat(uint32_t a, uint32_t b) { return min(a + b, 1u << 30); }
+__device__ __forceinline__ int64_t sums_before(int64_t value, int64_t& total, PlanShared& sh) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int64_t s = v;
+  uint32_t s = static_cast<uint32_t>(min(value, int64_t{1} << 30));
 #pragma unroll
   for (int d = 1; d < 64; d <<= 1) {
-    const int64_t u = shfl64(s, max(lane - d, 0));
-    if (lane >= d) s += u;
+    const uint32_t u = __shfl_up(s, d);
+    if (lane >= d) s = add_sat(s, u);
   }
+  uint32_t before = __shfl_up(s, 1);
+  if (lane == 0) before = 0;
   __syncthreads();
   if (lane == 63) sh.wave[wave] = s;
   __syncthreads();
-  int64_t before = 0, all = 0;
+  uint32_t earlier = 0, all = 0;
 #pragma unroll
   for (int w = 0; w < kPlanThreads / 64; ++w) {
-    if (w == wave) before = all;
-    all += sh.wave[w];
+    if (w == wave) earlier = all;
+    all = add_sat(all, sh.wave[w]);
   }
   total = all;
-  return before + s - v;
+  return add_sat(earlier, before);
 }
 
 // Pieces and slots of the parts, then their work items.  With more units than the chip takes at a time, whole rounds of
@@ -178,18 +196,23 @@ __device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, 
                            int64_t most, ReqOf req_of, PlanShared& sh) {
   const int tid = threadIdx.x;
   auto keys_of = [](const Part& p) { return p.tiles > 0 ? (p.keys1 - p.keys0 + kBK - 1) / kBK : 0; };
-  int64_t all = 0, total;
+  int64_t all = 0, total, first_sum = 0;
+  bool longer = false;                                // a whole unit has several pieces
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
-    const int i = i0 + tid;
-    all += (sums_before(i < n && keys_of(parts[i]) > 0 ? static_cast<int64_t>(parts[i].tiles) * hkv : 0, total, sh), total);
+    const int i = i0 + tid, keys = i < n ? keys_of(parts[i]) : 0;
+    longer |= keys > kMaxPieceTiles;
+    first_sum = sums_before(keys > 0 ? static_cast<int64_t>(parts[i].tiles) * hkv : 0, total, sh);
+    all += total;
   }
   const int64_t first_cut = all / units * units;      // units before this one stay whole
-  int64_t at = 0, at_w = 0;
+  int64_t at = 0, at_w = first_cut;                   // items of the whole units
+  longer = __syncthreads_or(longer);
+  if (longer) at_w = 0;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
     const int i = i0 + tid;
     const int keys = i < n ? keys_of(parts[i]) : 0;
     const int64_t mine = keys > 0 ? static_cast<int64_t>(parts[i].tiles) * hkv : 0;
-    const int64_t before = at + sums_before(mine, total, sh);
+    const int64_t before = n <= kPlanThreads ? first_sum : at + sums_before(mine, total, sh);
     at += total;
     int64_t items = 0;
     if (i < n) {
@@ -199,8 +222,10 @@ __device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, 
       p.len_w = p.pieces_w > 0 ? (keys + p.pieces_w - 1) / p.pieces_w : 0;
       items = static_cast<int64_t>(p.whole) * p.pieces_w;
     }
-    sums_before(items, total, sh);
-    at_w += total;
+    if (longer) {
+      sums_before(items, total, sh);
+      at_w += total;
+    }
   }
   __syncthreads();
   const int cap = choose_cap(n, most - at_w, units, min_cap, over, w64, [=](int i, int& cut, int& keys) {
@@ -455,8 +480,10 @@ __device__ __forceinline__ int pieces_of(const Part& p, int64_t c, int kvh, int 
 // steps in turn, and nothing passes through LDS but the waves' results at the end.  An item that has all of its columns' own
 // keys joins them with the pieces over shared keys, which an earlier launch has written, and writes the result; one of
 // several pieces writes a partial result.  What bounds it is the
-// bytes of K and V, and the chain of waits (item, lengths, table, keys) of items of a few steps; three work-groups of four
-// waves share a compute unit.  With fewer items than units (WAVES = 8) an item's keys are spread over twice the waves.
+// bytes of K and V (78 requests of 56 to 6500 own tokens, 40 / 8 heads, 225 MB and the shared pieces: 51 us), and the chain of
+// waits (item, lengths, table, keys, join) of items of a few steps: 5 us without keys; three work-groups of four
+// waves share a compute unit.  With fewer requests and heads than units (WAVES = 8) an item's keys are spread over twice the
+// waves: 23 requests of 60 to 820 own tokens on a shared 8192 32.7 us in all, 33.7 with four; three times as many the same.
 //   S^T (16 keys x 16 columns, twice): lane (i = l % 16, g = l / 16) holds row i's dims 32 k + 8 g ..; row i of
 //   product m is key 8 (i / 4) + 4 m + i % 4, so that the lane's results, rows 4 g + e, are the keys 8 g + 4 m + e
 //   of its column: the eight keys that it holds as the operand of P.V.
@@ -666,7 +693,8 @@ __global__ __launch_bounds__(64 * WAVES, 3) void shared_tail_kernel(
 // ---- the join ------------------------------------------------------------------------------------
 // What the items have not joined: rows over shared and own keys in tiles, and own keys in several pieces.  plan[0] says
 // how many rows that may be, and its list which.  With few rows (SPLIT) a work-group has one row and head and its sets of lanes take the pieces in turn;
-// otherwise it has a row and its sets take the heads.  What bounds it is reading the partial results (fp32).
+// otherwise it has a row and its sets take the heads.  What bounds it is reading the partial results (fp32): 2048 rows of 40
+// heads of 128, 2.6 pieces each, 109 MB read and 21 written in 32 us; with few rows the two round trips (4 to 6 us).
 constexpr int64_t kSplitPairs = 8192;   // most (row, head) pairs whose pieces are split over a work-group
 template <int D, bool SPLIT>
 __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__ out, float* __restrict__ lse_out,
@@ -718,7 +746,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__
 int32_t check_shared(const char* fn, int32_t n_reqs, int32_t n_groups, int64_t max_q, int64_t max_group_q, int64_t max_new,
                      int32_t bt_stride, int32_t hq, int32_t hkv, int32_t head_dim, int32_t num_cus) {
   if (n_reqs < 0 || n_reqs > (1 << 20) || n_groups < 0 || n_groups > std::max(n_reqs, 1) || max_q < 0 || max_q > (1 << 23) ||
-      max_group_q < 0 || max_group_q > max_q || max_new < 0 || max_new > max_q || bt_stride < 0 || bt_stride > (1 << 26) ||
+      max_group_q < 0 || max_group_q > max_q || max_new < 0 || max_new > max_q || bt_stride < 0 || bt_stride > (1 << 25) ||
       hq < 1 || hkv < 1 || hq % hkv != 0 || num_cus < 1 || num_cus > (1 << 16))
     return arckv::fail(ARCKV_EINVAL, "%s: bad sizes", fn);
   if (head_dim != 64 && head_dim != 128)
