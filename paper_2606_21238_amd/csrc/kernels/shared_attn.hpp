@@ -8,7 +8,7 @@
 //
 //  * shared_plan_kernel (once a step; the layers share its plan): how many keys the groups share in truth (all
 //    their rows must see them; whole tiles of 64), the cuts, and the work items, from lengths on the device.  One work-group,
-//    a chain of scans and searches: 21 to 24 us for 64 requests, 72 for 1000.
+//    a chain of scans and searches: 20 us for 64 requests, 66 for 1000; none for short batches.
 //  * the shared keys: the attention kernels above, given a group as a request whose rows are those of
 //    all its requests and whose length is P + rows, so that every row sees all keys below P.  8192 tokens of 8 heads of 128
 //    for 92 columns (34 MB, narrow tiles) 16 us, of which the stream is 6; 32768 tokens for 184 columns (134 MB, wide tiles) 40
@@ -55,7 +55,7 @@ SharedSizes shared_sizes(int64_t n_reqs, int64_t n_groups, int64_t max_q, int64_
   const int64_t longest = (bt_stride * 16 + arckv::kMaxItemKeys - 1) / arckv::kMaxItemKeys;   // pieces at least
   auto items = [&](int64_t parts, int64_t cols, int64_t units) {
     const int64_t tiles = (max_q * G / cols + std::min(parts, max_q)) * hkv * std::max<int64_t>(longest, 1);
-    return 2 * tiles <= units ? units : tiles <= units ? 4 * tiles : tiles + units;
+    return 2 * tiles <= units ? units : tiles <= units ? 4 * tiles : tiles + 2 * units;
   };
   z.items_p = n_groups > 0 ? items(n_groups, z.tile_p, num_cus) : 0;
   z.items_o = items(n_reqs, z.tile_o, z.tile_o == kTailCols ? kTailPerUnit * num_cus : num_cus);
@@ -187,9 +187,22 @@ __device__ __forceinline__ int64_t sums_before(int64_t value, int64_t& total, Pl
   return add_sat(earlier, before);
 }
 
+// The sum of a value of every thread.
+__device__ __forceinline__ int64_t sum_threads(int64_t v, PlanShared& sh) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v += shfl64(v, (threadIdx.x & 63) ^ d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) sh.items[threadIdx.x >> 6][0] = v;
+  __syncthreads();
+  v = 0;
+  for (int w = 0; w < kPlanThreads / 64; ++w) v += sh.items[w][0];
+  __syncthreads();
+  return v;
+}
+
 // Pieces and slots of the parts, then their work items.  With more units than the chip takes at a time, whole rounds of
-// them stay whole, and only what is left is cut, so that it fills a last, shorter round (320 tiles of 128 key tiles on 256
-// units: 272 us, and 339 with every tile cut in two).  Units of the same keys lie `heads` apart: with 8 heads on one XCD.
+// them stay whole, but for those of more than a chip's unit's share of all keys, and only what is left is cut, so that it
+// fills a last, shorter round (320 tiles of 128 key tiles on 256 units: 272 us, and 339 with every tile cut in two).  Units of the same keys lie `heads` apart: with 8 heads on one XCD.
 // DIRECT: a unit of one piece that nothing joins has slot -1, and its kernel writes the result.
 template <bool DIRECT, class ReqOf>
 __device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, int over, int w64, int tile_cols, int per, Work* work,
@@ -197,14 +210,20 @@ __device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, 
   const int tid = threadIdx.x;
   auto keys_of = [](const Part& p) { return p.tiles > 0 ? (p.keys1 - p.keys0 + kBK - 1) / kBK : 0; };
   int64_t all = 0, total, first_sum = 0;
-  bool longer = false;                                // a whole unit has several pieces
+  int64_t load = 0;                                   // key tiles of this thread's parts
+  int longest = 0;
   for (int i0 = 0; i0 < n; i0 += kPlanThreads) {
     const int i = i0 + tid, keys = i < n ? keys_of(parts[i]) : 0;
-    longer |= keys > kMaxPieceTiles;
-    first_sum = sums_before(keys > 0 ? static_cast<int64_t>(parts[i].tiles) * hkv : 0, total, sh);
+    const int64_t mine = keys > 0 ? static_cast<int64_t>(parts[i].tiles) * hkv : 0;
+    load += mine * keys;
+    longest = max(longest, keys);
+    first_sum = sums_before(mine, total, sh);
     all += total;
   }
   const int64_t first_cut = all / units * units;      // units before this one stay whole
+  const int64_t share = first_cut > 0 ? (sum_threads(load, sh) + units - 1) / units : kMaxPieceTiles;
+  const int cap_w = static_cast<int>(min(max(share, static_cast<int64_t>(min_cap)), static_cast<int64_t>(kMaxPieceTiles)));
+  bool longer = longest > cap_w;                      // a whole unit has several pieces
   int64_t at = 0, at_w = first_cut;                   // items of the whole units
   longer = __syncthreads_or(longer);
   if (longer) at_w = 0;
@@ -218,8 +237,9 @@ __device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, 
     if (i < n) {
       Part& p = parts[i];
       p.whole = static_cast<int>(min(max(first_cut - before, int64_t{0}), mine));
-      p.pieces_w = (keys + kMaxPieceTiles - 1) / kMaxPieceTiles;
+      p.pieces_w = (keys + cap_w - 1) / cap_w;
       p.len_w = p.pieces_w > 0 ? (keys + p.pieces_w - 1) / p.pieces_w : 0;
+      p.pieces_w = p.pieces_w > 0 ? (keys + p.len_w - 1) / p.len_w : 0;
       items = static_cast<int64_t>(p.whole) * p.pieces_w;
     }
     if (longer) {
@@ -785,17 +805,18 @@ extern "C" int32_t arckv_shared_prefix_plan(const int32_t* group_start, const in
   const int32_t rc = check_shared("shared_prefix_plan", n_reqs, n_groups, max_q, max_group_q, max_new, bt_stride, num_q_heads,
                                   num_kv_heads, head_dim, num_cus);
   if (rc != ARCKV_OK) return rc;
+  const SharedSizes z = shared_sizes(n_reqs, n_groups, max_q, max_group_q, max_new, bt_stride, num_q_heads, num_kv_heads,
+                                     head_dim, num_cus);
   if (n_reqs == 0 || max_q == 0) return ARCKV_OK;
   if (cu_q == nullptr || seq_lens == nullptr || plan == nullptr ||
       (n_groups > 0 && (group_start == nullptr || prefix_lens == nullptr)))
     return arckv::fail(ARCKV_EINVAL, "shared_prefix_plan: NULL pointer");
   if (reinterpret_cast<uintptr_t>(plan) % 16 != 0)
     return arckv::fail(ARCKV_EINVAL, "shared_prefix_plan: the plan must be 16-byte aligned");
-  const SharedSizes z = shared_sizes(n_reqs, n_groups, max_q, max_group_q, max_new, bt_stride, num_q_heads, num_kv_heads,
-                                     head_dim, num_cus);
   if (plan_ints < z.n_ints)
     return arckv::fail(ARCKV_ENOSPC, "shared_prefix_plan: %lld ints, and the plan needs %lld", (long long)plan_ints,
                        (long long)z.n_ints);
+  if (short_route(z, n_reqs, bt_stride, num_kv_heads, head_dim)) return ARCKV_OK;     // the attention takes no plan
   hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, static_cast<hipStream_t>(stream), group_start,
                      prefix_lens, n_groups, cu_q, seq_lens, n_reqs, static_cast<int>(max_q), bt_stride,
                      num_q_heads / num_kv_heads, num_kv_heads, num_cus, z, plan);

@@ -197,6 +197,16 @@ def test_queries_and_outputs_at_any_address(shift):
         assert torch.isnan(obuf[:shift]).all() and torch.isnan(obuf[shift + n:]).all()
 
 
+@pytest.mark.parametrize("num_cus", [256, 16])
+def test_one_long_request_among_many(num_cus):
+    """More units than the chip takes at a time, and one with most of the keys: it is cut to a unit's share."""
+    for rows, what in ((1, "tail"), (30, "narrow"), (70, "wide")):
+        n = 20 if num_cus == 16 else 180
+        groups = [(128, [(rows + r % 9, rows) for r in range(n)] + [(9000, rows)]), (4096, [(rows, rows), (5000, rows)])]
+        b = shared_batch(groups, 8, 2, 64, 57)
+        run(b, f"one long among {n}, {what}, {num_cus} units", bounds=bounds_of(b, num_cus=num_cus))
+
+
 def test_very_long_prefix():
     """More keys than one item may hold (65536), of few and of many rows."""
     for rs in ([(3, 1)] * 3, [(90, 70)] * 2):
