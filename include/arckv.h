@@ -662,7 +662,8 @@ int32_t arckv_shared_prefix_sizes(int32_t n_reqs, int32_t n_groups, int64_t max_
                                   int32_t num_kv_heads, int32_t head_dim, int32_t num_cus,
                                   int64_t* plan_ints, int64_t* ws_bytes);
 
-/* The plan of a step (not read, and left as it is, where the attention of such bounds takes one launch).  group_start [n_groups + 1], prefix_lens [n_groups], cu_q [n_reqs + 1], seq_lens [n_reqs], plan
+/* The plan of a step (not read, and left as it is, where the attention of such bounds takes one launch).
+ * group_start [n_groups + 1], prefix_lens [n_groups], cu_q [n_reqs + 1], seq_lens [n_reqs], plan
  * [plan_ints]: device int32, the plan 16-byte aligned.  0 <= max_group_q, max_new <= max_q <= 2^23, n_groups <=
  * n_reqs <= 2^20, bt_stride <= 2^25 (else EINVAL); ENOSPC if plan_ints is too small. */
 int32_t arckv_shared_prefix_plan(const int32_t* group_start, const int32_t* prefix_lens, int32_t n_groups,

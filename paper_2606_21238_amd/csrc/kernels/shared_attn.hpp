@@ -485,12 +485,14 @@ __device__ __forceinline__ void write_joined(const Joined& j, uint16_t* out, flo
     lse_out[row_head] = j.sum > 0.f ? (j.m + __log2f(j.sum)) * kLn2 : j.sum == 0.f ? -INFINITY : j.sum;
 }
 // Pieces of column `c` (row - row0 times G, and the head of the group) of a part, and where its first piece lies and how far
-// apart they are, in columns.
-__device__ __forceinline__ int pieces_of(const Part& p, int64_t c, int kvh, int hkv, int tile_cols, int64_t& first, int64_t& step) {
-  const int64_t unit = c / tile_cols * hkv + kvh;
+// apart they are, in columns.  (Tiles have a power of two of columns; fewer than 2^31 units and columns.)
+__device__ __forceinline__ int pieces_of(const Part& p, uint32_t c, int kvh, int hkv, int tile_cols, int64_t& first, int64_t& step) {
+  const int log_cols = __builtin_ctz(tile_cols);
+  const int unit = static_cast<int>(c >> log_cols) * hkv + kvh, cut = p.tiles * hkv - p.whole;
   const bool whole = unit < p.whole;
-  first = (p.base + (whole ? unit : static_cast<int64_t>(p.whole) * p.pieces_w + unit - p.whole)) * tile_cols + c % tile_cols;
-  step = (whole ? p.whole : static_cast<int64_t>(p.tiles) * hkv - p.whole) * tile_cols;
+  const int slot = p.base + (whole ? unit : p.whole * p.pieces_w + unit - p.whole);
+  first = static_cast<int64_t>(slot) * tile_cols + (c & static_cast<uint32_t>(tile_cols - 1));
+  step = static_cast<int64_t>(whole ? p.whole : cut) * tile_cols;
   return p.tiles == 0 ? 0 : whole ? p.pieces_w : p.pieces;
 }
 
@@ -555,7 +557,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void shared_tail_kernel(
           const int64_t row = q0 + at / G - group.row0;
           if (c < n_here && group.tiles > 0 && row >= 0 && row < group.rows) {
             int64_t first, step;
-            const int n = pieces_of(group, row * G + at % G, w.kvh, hkv, z.tile_p, first, step);
+            const int n = pieces_of(group, static_cast<uint32_t>(row * G + at % G), w.kvh, hkv, z.tile_p, first, step);
             add_pieces(j, from, sets_per, n, [&](int i) { return ws_lp[first + i * step]; },
                        [&](int i) { return reinterpret_cast<const acc4_t*>(ws_op + (first + i * step) * D + 4 * d4); });
           }
@@ -726,7 +728,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__
   __shared__ acc4_t set_o[SPLIT ? SETS : 1][LANES];
   __shared__ float set_m[SETS], set_s[SETS];
   const int set = threadIdx.x / LANES, d4 = threadIdx.x % LANES;
-  const int64_t at = SPLIT ? blockIdx.x / hq : blockIdx.x;
+  const int at = SPLIT ? blockIdx.x / hq : blockIdx.x;
   if (at >= plan[0] || at >= n_q) return;
   const int64_t t = plan[z.off_list + at];
   if (t < 0 || t >= n_q) return;
@@ -739,8 +741,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__
   for (int h = SPLIT ? blockIdx.x % hq : set; h < hq; h += SPLIT ? hq : SETS) {
     const int kvh = h / G;
     int64_t p0, ps, r0, rs;
-    const int np = pieces_of(pg, (t - pg.row0) * G + h % G, kvh, hkv, z.tile_p, p0, ps);
-    const int nr = pieces_of(pr, (t - pr.row0) * G + h % G, kvh, hkv, z.tile_o, r0, rs);
+    const int np = pieces_of(pg, static_cast<uint32_t>((t - pg.row0) * G + h % G), kvh, hkv, z.tile_p, p0, ps);
+    const int nr = pieces_of(pr, static_cast<uint32_t>((t - pr.row0) * G + h % G), kvh, hkv, z.tile_o, r0, rs);
     if (nr == 1 && (np == 0 || z.tile_o == kTailCols)) continue;     // its item has written the result
     Joined j;
     add_pieces(j, SPLIT ? set : 0, SPLIT ? SETS : 1, np + nr,
