@@ -6,8 +6,9 @@
 //
 // One work-group has a row and holds it in registers as h, so each value is read once; what bounds it is
 // the bytes of x, residual, residual_out and out: 25600 x 5120 in bf16 (1.05 GB) 180 us, 5.8 TB/s, 16384 x 4096 to 8 bits (0.47
-// GB) 82 us, 5.7 TB/s, above a copy's 4.7 since more is read than written; 64 x 4096 3.3 us, a launch and two round trips (2.9 inside a graph).  A row's squares are added in fp32: up to 40 in a thread, then
-// by a tree of lanes and waves, always in the same order.
+// GB) 82 us, 5.7 TB/s, above a copy's 4.7 since more is read than written; 64 x 4096 3.0 us, a launch and two round trips (2.9
+// inside a graph).  A row's squares are added in fp32: up to 40 in a thread, then by a tree of lanes and waves, always in the
+// same order.
 #pragma once
 
 namespace {
@@ -17,34 +18,42 @@ constexpr int kNormMaxHidden = 32768;   // 1024 threads x 4 chunks x 8 values: a
 constexpr int64_t kNormMaxRows = int64_t{1} << 21;     // rows of a launch (2^32 threads would be too many)
 constexpr float kNormMinScale = 1.17549435e-38f;        // the smallest normal number: 1 / scale is finite
 
-// 8 values of a row: of an aligned row the 8 that follow each other, otherwise (ANY) every TH-th, so that 2-byte
-// loads of neighbouring lanes are neighbours.
-template <int TH, bool ANY>
-__device__ __forceinline__ int norm_at(int c, int j) {
-  return ANY ? c * 8 * TH + j * TH + static_cast<int>(threadIdx.x) : (c * TH + static_cast<int>(threadIdx.x)) * 8 + j;
+// 8 values of a row that follow each other.  ANY: at any bf16 address, 16 unaligned bytes in one access (5000 x 4097 in bf16
+// takes 30 us, 93 with 2-byte accesses of neighbouring lanes; 5000 x 4096, aligned, 25), and the row may end inside the chunk.
+template <int TH>
+__device__ __forceinline__ int norm_at(int c) {
+  return (c * TH + static_cast<int>(threadIdx.x)) * 8;
 }
 template <int TH, bool ANY>
 __device__ __forceinline__ u32x4_t norm_load(const uint16_t* row, int c, int hidden) {
+  const int at = norm_at<TH>(c);
   u32x4_t v = {0, 0, 0, 0};
   if constexpr (ANY) {
-    uint16_t e[8];
+    if (at + 8 <= hidden) {
+      __builtin_memcpy(&v, row + at, 16);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = norm_at<TH, ANY>(c, j) < hidden ? row[norm_at<TH, ANY>(c, j)] : uint16_t{0};
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = e[2 * j] | static_cast<uint32_t>(e[2 * j + 1]) << 16;
+      for (int j = 0; j < 7; ++j)
+        if (at + j < hidden) v[j / 2] |= static_cast<uint32_t>(row[at + j]) << (16 * (j % 2));
+    }
   } else {
-    if (norm_at<TH, ANY>(c, 0) < hidden) v = *reinterpret_cast<const u32x4_t*>(row + norm_at<TH, ANY>(c, 0));
+    if (at < hidden) v = *reinterpret_cast<const u32x4_t*>(row + at);
   }
   return v;
 }
 template <int TH, bool ANY>
 __device__ __forceinline__ void norm_store(uint16_t* row, int c, int hidden, const u32x4_t& v) {
+  const int at = norm_at<TH>(c);
   if constexpr (ANY) {
+    if (at + 8 <= hidden) {
+      __builtin_memcpy(row + at, &v, 16);
+    } else {
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (norm_at<TH, ANY>(c, j) < hidden) row[norm_at<TH, ANY>(c, j)] = static_cast<uint16_t>(v[j / 2] >> (16 * (j % 2)));
+      for (int j = 0; j < 7; ++j)
+        if (at + j < hidden) row[at + j] = static_cast<uint16_t>(v[j / 2] >> (16 * (j % 2)));
+    }
   } else {
-    if (norm_at<TH, ANY>(c, 0) < hidden) *reinterpret_cast<u32x4_t*>(row + norm_at<TH, ANY>(c, 0)) = v;
+    if (at < hidden) *reinterpret_cast<u32x4_t*>(row + at) = v;
   }
 }
 
@@ -144,15 +153,22 @@ __global__ __launch_bounds__(TH) void add_rms_norm_kernel(const uint16_t* x, int
         int b = __builtin_amdgcn_cvt_pk_fp8_f32(e[0], e[1], 0, false);
         w[k] = __builtin_amdgcn_cvt_pk_fp8_f32(e[2], e[3], b, true);
       }
+      const int at = norm_at<TH>(c);
+      const uint2 codes = make_uint2(w[0], w[1]);
       if constexpr (ANY) {
+        if (at + 8 <= hidden) {
+          __builtin_memcpy(o + at, &codes, 8);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (norm_at<TH, ANY>(c, j) < hidden) o[norm_at<TH, ANY>(c, j)] = static_cast<uint8_t>(w[j / 4] >> (8 * (j % 4)));
+          for (int j = 0; j < 7; ++j)
+            if (at + j < hidden) o[at + j] = static_cast<uint8_t>(w[j / 4] >> (8 * (j % 4)));
+        }
       } else {
-        if (norm_at<TH, ANY>(c, 0) < hidden) *reinterpret_cast<uint2*>(o + norm_at<TH, ANY>(c, 0)) = make_uint2(w[0], w[1]);
+        if (at < hidden) *reinterpret_cast<uint2*>(o + at) = codes;
       }
     }
-  }}
+  }
+}
 
 template <bool ANY, bool E4M3>
 void add_rms_norm_launch(const uint16_t* x, int64_t x_stride, const uint16_t* residual, uint16_t* residual_out,

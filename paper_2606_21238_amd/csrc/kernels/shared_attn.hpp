@@ -716,7 +716,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void shared_tail_kernel(
 // What the items have not joined: rows over shared and own keys in tiles, and own keys in several pieces.  plan[0] says
 // how many rows that may be, and its list which.  With few rows (SPLIT) a work-group has one row and head and its sets of lanes take the pieces in turn;
 // otherwise it has a row and its sets take the heads.  What bounds it is reading the partial results (fp32): 2048 rows of 40
-// heads of 128, 2.6 pieces each, 109 MB read and 21 written in 32 us; with few rows the two round trips (4 to 6 us).
+// heads of 128, 2.6 pieces each, 109 MB read and 21 written in 30 us; with few rows the two round trips (4 to 6 us).
 constexpr int64_t kSplitPairs = 8192;   // most (row, head) pairs whose pieces are split over a work-group
 template <int D, bool SPLIT>
 __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__ out, float* __restrict__ lse_out,
