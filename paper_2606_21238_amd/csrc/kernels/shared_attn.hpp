@@ -485,14 +485,14 @@ __device__ __forceinline__ void write_joined(const Joined& j, uint16_t* out, flo
     lse_out[row_head] = j.sum > 0.f ? (j.m + __log2f(j.sum)) * kLn2 : j.sum == 0.f ? -INFINITY : j.sum;
 }
 // Pieces of column `c` (row - row0 times G, and the head of the group) of a part, and where its first piece lies and how far
-// apart they are, in columns.  (Tiles have a power of two of columns; fewer than 2^31 units and columns.)
-__device__ __forceinline__ int pieces_of(const Part& p, uint32_t c, int kvh, int hkv, int tile_cols, int64_t& first, int64_t& step) {
+// apart they are, in columns.  (Tiles have a power of two of columns; the columns of all items are fewer than 2^31.)
+__device__ __forceinline__ int pieces_of(const Part& p, uint32_t c, int kvh, int hkv, int tile_cols, int& first, int& step) {
   const int log_cols = __builtin_ctz(tile_cols);
   const int unit = static_cast<int>(c >> log_cols) * hkv + kvh, cut = p.tiles * hkv - p.whole;
   const bool whole = unit < p.whole;
   const int slot = p.base + (whole ? unit : p.whole * p.pieces_w + unit - p.whole);
-  first = static_cast<int64_t>(slot) * tile_cols + (c & static_cast<uint32_t>(tile_cols - 1));
-  step = static_cast<int64_t>(whole ? p.whole : cut) * tile_cols;
+  first = (slot << log_cols) + static_cast<int>(c & static_cast<uint32_t>(tile_cols - 1));
+  step = (whole ? p.whole : cut) << log_cols;
   return p.tiles == 0 ? 0 : whole ? p.pieces_w : p.pieces;
 }
 
@@ -550,19 +550,23 @@ __global__ __launch_bounds__(64 * WAVES, 3) void shared_tail_kernel(
       if (n_here <= 0) break;                               // (uniform)
       // ---- pieces over shared keys: sets_per sets of lanes have a column -------------------------
       const int sets_per = n_here * 8 <= SETS ? 8 : n_here * 4 <= SETS ? 4 : n_here * 2 <= SETS ? 2 : 1;
-      auto shared = [&](int c, int from) -> Joined {
-        Joined j;
+      auto shared = [&](int c, int from) {                  // into LDS: registers are short while the keys are read
         if constexpr (!SHORT) {
+          Joined j;
           const int at = col0 + c;
           const int64_t row = q0 + at / G - group.row0;
           if (c < n_here && group.tiles > 0 && row >= 0 && row < group.rows) {
-            int64_t first, step;
+            int first, step;
             const int n = pieces_of(group, static_cast<uint32_t>(row * G + at % G), w.kvh, hkv, z.tile_p, first, step);
             add_pieces(j, from, sets_per, n, [&](int i) { return ws_lp[first + i * step]; },
-                       [&](int i) { return reinterpret_cast<const acc4_t*>(ws_op + (first + i * step) * D + 4 * d4); });
+                       [&](int i) { return reinterpret_cast<const acc4_t*>(ws_op + static_cast<int64_t>(first + i * step) * D + 4 * d4); });
+          }
+          set_o[set][d4] = j.acc;
+          if (d4 == 0) {
+            set_m[set] = j.m;
+            set_s[set] = j.sum;
           }
         }
-        return j;
       };
       // ---- the keys ------------------------------------------------------------------------------
       const int col = col0 + i16, tok = col / G;
@@ -599,7 +603,7 @@ __global__ __launch_bounds__(64 * WAVES, 3) void shared_tail_kernel(
         }
       };
       look_up(wave);
-      Joined mine = shared(set / sets_per, set % sets_per);
+      shared(set / sets_per, set % sets_per);
       // (K/V a step ahead of their use, at 256 registers and two waves on a SIMD, measured no faster: 16.2 and 16.0 us for 23
       // requests of 60 to 820 own tokens)
       for (int s = wave; s < steps; s += WAVES) {
@@ -677,19 +681,13 @@ __global__ __launch_bounds__(64 * WAVES, 3) void shared_tail_kernel(
         part_l[wave][i16] = l_run;
       }
       for (int c0 = 0; c0 < n_here; c0 += SETS / sets_per) {
-        if (c0 > 0) mine = shared(c0 + set / sets_per, set % sets_per);
-        if (!SHORT && sets_per > 1) {
-          set_o[set][d4] = mine.acc;
-          if (d4 == 0) {
-            set_m[set] = mine.m;
-            set_s[set] = mine.sum;
-          }
-        }
+        if (c0 > 0) shared(c0 + set / sets_per, set % sets_per);
         __syncthreads();
         const int c = c0 + set / sets_per;
         if (c < n_here && set % sets_per == 0 && q0 + (col0 + c) / G < n_q) {
-          if (!SHORT)
-            for (int k = 1; k < sets_per; ++k) add_sum(mine, set_m[set + k], set_s[set + k], set_o[set + k][d4]);
+          Joined mine;
+          if constexpr (!SHORT)
+            for (int k = 0; k < sets_per; ++k) add_sum(mine, set_m[set + k], set_s[set + k], set_o[set + k][d4]);
           Joined keys;
 #pragma unroll
           for (int v = 0; v < WAVES; ++v)
@@ -740,7 +738,7 @@ __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__
   const Part pg = part(z.off_group, of.y, n_groups), pr = part(z.off_req, of.x, n_reqs);
   for (int h = SPLIT ? blockIdx.x % hq : set; h < hq; h += SPLIT ? hq : SETS) {
     const int kvh = h / G;
-    int64_t p0, ps, r0, rs;
+    int p0, ps, r0, rs;
     const int np = pieces_of(pg, static_cast<uint32_t>((t - pg.row0) * G + h % G), kvh, hkv, z.tile_p, p0, ps);
     const int nr = pieces_of(pr, static_cast<uint32_t>((t - pr.row0) * G + h % G), kvh, hkv, z.tile_o, r0, rs);
     if (nr == 1 && (np == 0 || z.tile_o == kTailCols)) continue;     // its item has written the result
@@ -748,7 +746,8 @@ __global__ __launch_bounds__(256) void shared_join_kernel(uint16_t* __restrict__
     add_pieces(j, SPLIT ? set : 0, SPLIT ? SETS : 1, np + nr,
                [&](int i) { return i < np ? ws_lp[p0 + i * ps] : ws_lo[r0 + (i - np) * rs]; },
                [&](int i) {
-                 return reinterpret_cast<const acc4_t*>((i < np ? ws_op + (p0 + i * ps) * D : ws_oo + (r0 + (i - np) * rs) * D) + 4 * d4);
+                 return reinterpret_cast<const acc4_t*>((i < np ? ws_op : ws_oo) +
+                                                        static_cast<int64_t>(i < np ? p0 + i * ps : r0 + (i - np) * rs) * D + 4 * d4);
                });
     if constexpr (SPLIT) {
       set_o[set][d4] = j.acc;
