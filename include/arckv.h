@@ -649,8 +649,9 @@ int32_t arckv_batch_maps(const int32_t* new_tokens, const int32_t* held, int32_t
  * computes is what arckv_prefill_attention computes (the same softmax over all of a request's keys [0, j]); only the
  * order of the sums differs.  Requests group_start[g] .. group_start[g + 1] - 1 (in order, groups apart) are group g, and its
  * requests hold the same first prefix_lens[g] tokens: their table rows name the same blocks for them.  Of these the
- * whole tiles of 64 keys that every row of the group sees are read through the first request's table, for all rows at
- * once; the rest, and requests in no group, go through their own tables.
+ * whole tiles of 64 keys that every row of the group sees are read through the table of the group's first request that has
+ * rows, for all rows at once (one without rows may have ended, and its table say anything); the rest, and requests in no
+ * group, go through their own tables.
  * No host plan: shared_prefix_plan writes the work items on the device, from lengths on the device (once a
  * step; layers share it), so that a captured step holds while the requests grow.  What the host has to know are bounds:
  * max_q, the rows of q (cu_q[n_reqs] may be less); max_group_q, the most rows of a group, and max_new, of a request (a step that

@@ -328,7 +328,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
     Part p = {};
     p.row0 = row(r0);
     p.rows = max(row(r1) - p.row0, 0);
-    p.group = r0;                                      // of a group: its first request
+    p.group = INT32_MAX;                               // of a group: its first request that has rows (below)
     p.keys1 = static_cast<int32_t>(min(static_cast<int64_t>(max(prefix_lens[g], 0)), room));
     groups[g] = p;
   }
@@ -352,6 +352,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
     const int L = max(seq_lens[r], 0), q0 = row(r), S = max(row(r + 1) - q0, 0);
     if (g >= 0 && S > 0) {
       atomicMin(&groups[g].keys1, max(L - S, 0));
+      atomicMin(&groups[g].group, r);
       atomicAdd(&groups[g].whole, static_cast<int>((static_cast<int64_t>(S) * G + z.tile_o - 1) / z.tile_o));
     }
     Part p = {};
@@ -365,7 +366,11 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
   for (int g = tid; g < n_groups; g += kPlanThreads) {
     int shared = __hip_atomic_load(&groups[g].keys1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) / kBK * kBK;
     const int apart = __hip_atomic_load(&groups[g].whole, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    const int first = __hip_atomic_load(&groups[g].group, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     Part& p = groups[g];
+    // The shared keys are read through this request's table: one without rows may have ended, and its table name other blocks
+    p.group = first;
+    if (first >= n_reqs) shared = 0;
     const int together = static_cast<int>((static_cast<int64_t>(p.rows) * G + z.tile_p - 1) / z.tile_p);
     // Requests that fill their own wide tiles read their keys once for 256 columns anyhow: sharing that saves no more than
     // an eighth of the tiles is not worth a second item and the join (2 x 1024 rows on 16384: 978 us shared)
