@@ -208,7 +208,8 @@ template <bool DIRECT, class ReqOf>
 __device__ void emit_items(Part* parts, int n, int hkv, int units, int min_cap, int over, int w64, int tile_cols, int per, Work* work,
                            int64_t most, ReqOf req_of, PlanShared& sh) {
   const int tid = threadIdx.x;
-  auto keys_of = [](const Part& p) { return p.tiles > 0 ? (p.keys1 - p.keys0 + kBK - 1) / kBK : 0; };
+  // (tiles of no keys count as one: the tail kernel's items of rows that see none)
+  auto keys_of = [](const Part& p) { return p.tiles > 0 ? max((p.keys1 - p.keys0 + kBK - 1) / kBK, 1) : 0; };
   int64_t all = 0, total, first_sum = 0;
   int64_t load = 0;                                   // key tiles of this thread's parts
   int longest = 0;
@@ -387,7 +388,8 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
   for (int r = tid; r < n_reqs; r += kPlanThreads) {
     Part& p = reqs[r];
     p.keys0 = p.group >= 0 && p.rows > 0 ? groups[p.group].keys1 : 0;
-    p.tiles = p.keys1 > p.keys0 ? static_cast<int>((static_cast<int64_t>(p.rows) * G + z.tile_o - 1) / z.tile_o) : 0;
+    // Rows without own keys: the tail kernel writes them too (there may be no join); in tiles they are the join's
+    p.tiles = p.keys1 > p.keys0 || z.tile_o == kTailCols ? static_cast<int>((static_cast<int64_t>(p.rows) * G + z.tile_o - 1) / z.tile_o) : 0;
   }
   const int total = row(n_reqs);
   for (int t = tid; t < total; t += kPlanThreads) {    // a row's request and group
