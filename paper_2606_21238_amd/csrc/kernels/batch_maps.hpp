@@ -293,8 +293,9 @@ extern "C" int32_t arckv_batch_maps(const int32_t* new_tokens, const int32_t* he
     hipLaunchKernelGGL(batch_maps_kernel<false>, dim3(1), dim3(kMapsThreads), 0, st, new_tokens, held, n_reqs, block_tables,
                        bt_stride, free_blocks, free_cap, free_count, free_left, cu_q, seq_lens, true_offset, true_lens,
                        slot_mapping, cap, num_blocks);
-    hipLaunchKernelGGL(batch_slots_kernel, dim3(static_cast<unsigned>((cap + kSlots - 1) / kSlots)), dim3(kSlotThreads), 0, st,
-                       cu_q, seq_lens, n_reqs, block_tables, bt_stride, free_blocks, free_left, slot_mapping, cap, num_blocks);
+    if (cap > 0)                                       // without slots nobody has a token, nor takes a block
+      hipLaunchKernelGGL(batch_slots_kernel, dim3(static_cast<unsigned>((cap + kSlots - 1) / kSlots)), dim3(kSlotThreads), 0, st,
+                         cu_q, seq_lens, n_reqs, block_tables, bt_stride, free_blocks, free_left, slot_mapping, cap, num_blocks);
   }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return arckv::fail(ARCKV_EDEVICE, "batch_maps: %s", hipGetErrorString(e));
