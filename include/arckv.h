@@ -616,7 +616,7 @@ int32_t arckv_kv_compact_mx4(void* kv_pool, const int32_t* block_tables, int32_t
  * hidden) x, a bf16 out may be any of them that residual_out is not; no other overlap.  Rows may start at
  * any bf16 address and hidden may be odd (hidden a multiple of 8 and 16-byte aligned rows run faster); scales 4-byte
  * aligned.  hidden at most 32768 (EUNSUPPORTED), n_tokens at most 2^31 - 1; n_tokens = 0 is a no-op.  h^2 is summed
- * in fp32, so h beyond 1e18 gives a y of 0. */
+ * in fp32, of a row whose squares fp32 does not hold times a power of two. */
 #define ARCKV_OUT_BF16 0
 #define ARCKV_OUT_E4M3 1
 int32_t arckv_add_rms_norm(const void* x, int64_t x_stride, const void* residual, void* residual_out,

@@ -8,7 +8,8 @@
 // the bytes of x, residual, residual_out and out: 25600 x 5120 in bf16 (1.05 GB) 180 us, 5.8 TB/s, 16384 x 4096 to 8 bits (0.47
 // GB) 82 us, 5.7 TB/s, above a copy's 4.7 since more is read than written; 64 x 4096 3.0 us, a launch and two round trips (2.9
 // inside a graph).  A row's squares are added in fp32: up to 40 in a thread, then by a tree of lanes and waves, always in the
-// same order.
+// same order; where the sum leaves [2^-80, 2^100] (squares below or above fp32's numbers may be among them), once more of
+// the row times a power of two, which rounds nothing.
 #pragma once
 
 namespace {
@@ -17,6 +18,11 @@ constexpr int kNormMaxHidden = 32768;   // 1024 threads x 4 chunks x 8 values: a
 
 constexpr int64_t kNormMaxRows = int64_t{1} << 21;     // rows of a launch (2^32 threads would be too many)
 constexpr float kNormMinScale = 1.17549435e-38f;        // the smallest normal number: 1 / scale is finite
+
+// Sums of squares outside these are taken again, of the row times 2^80 or 2^-80.  Below: a row's largest value is under 2^-40 (its
+// square times 2^160 under 2^80) and at least bf16's smallest, 2^-133 (2^-106), and eps times 2^160 is under 2^80.  Above: it is at
+// least 2^42 (the sum has 2^15 squares at most), so 2^-76 to 2^96 after, and eps times 2^-160 under 2^-32.
+constexpr float kNormSmallSum = 0x1p-80f, kNormLargeSum = 0x1p100f, kNormUp = 0x1p80f, kNormDown = 0x1p-80f;
 
 // 8 values of a row that follow each other.  ANY: at any bf16 address, 16 unaligned bytes in one access (5000 x 4097 in bf16
 // takes 30 us, 93 with 2-byte accesses of neighbouring lanes; 5000 x 4096, aligned, 25), and the row may end inside the chunk.
@@ -78,7 +84,7 @@ template <int TH, int CH, bool ANY, bool E4M3>
 __global__ __launch_bounds__(TH) void add_rms_norm_kernel(const uint16_t* x, int64_t x_stride, const uint16_t* residual,
                                                           uint16_t* residual_out, const uint16_t* __restrict__ weight,
                                                           int hidden, float eps, void* out, float* scales) {
-  __shared__ float sum_of[TH / 64];
+  __shared__ float sum_of[TH / 64], again_of[TH / 64];
   __shared__ uint32_t top_of[TH / 64];
   const int64_t row = blockIdx.x;
   const uint16_t* xr = x + row * x_stride;
@@ -111,11 +117,29 @@ __global__ __launch_bounds__(TH) void add_rms_norm_kernel(const uint16_t* x, int
       norm_store<TH, ANY>(residual_out + row * hidden, c, hidden, v);
     }
   }
+  // Where eps >= 2^-80 what squares below 2^-126 lose does not count beside it.  A row times 2^80 is exact and stays so; times
+  // 2^-80 its small values would lose bits, which y's factor takes up in the place.
+  float down = 1.f;
+  if (ss > kNormLargeSum || (ss < kNormSmallSum && eps < kNormSmallSum)) {        // (uniform, and not for a NaN)
+    const float f = ss > kNormLargeSum ? kNormDown : kNormUp;
+    ss = 0.f;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float hf = h[c][j] * f;
+        ss = fmaf(hf, hf, ss);
+        if (f == kNormUp) h[c][j] = hf;
+      }
+    ss = join_threads<TH>(ss, again_of, [](float a, float b) { return a + b; });
+    eps = eps * f * f;
+    if (f == kNormDown) down = f;
+  }
   const float r = 1.f / sqrtf(ss / static_cast<float>(hidden) + eps);
 #pragma unroll
   for (int c = 0; c < CH; ++c)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * r * bf16_to_f32(wv[c][j / 2] >> (16 * (j % 2)));
+    for (int j = 0; j < 8; ++j) h[c][j] = h[c][j] * r * down * bf16_to_f32(wv[c][j / 2] >> (16 * (j % 2)));
   if constexpr (!E4M3) {
     auto* o = static_cast<uint16_t*>(out) + row * hidden;
 #pragma unroll
