@@ -488,9 +488,11 @@ class PrefillEngine:
                    sb.cu_q.data_ptr(), sb.seq_lens.data_ptr(), b.n_reqs, b.n_groups, b.max_q, b.max_group_q, b.max_new,
                    self.num_blocks, *b.heads(), self.scale, sb.work_plan.data_ptr(), sb.workspace.data_ptr(), sb.ws_bytes)
 
-    def _held(self, sb: StepBatch, stream):
+    def _held(self, sb: DeviceBatch, stream):
         """A StepBatch's memory, which may be let go of right after a call, is not given away before the call's stream is
-        done with it, where that is not the stream that it was allocated on."""
+        done with it, where that is not the stream that it was allocated on.  (A planned batch lies in the engine's ring.)"""
+        if not isinstance(sb, StepBatch):
+            return
         handle = self._stream(stream)
         if handle != sb.home and not self._capturing(handle):
             ts = self._handle(handle)
@@ -507,6 +509,7 @@ class PrefillEngine:
         if self._bad(k_new, shape) or self._bad(v_new, shape):
             raise ValueError(f"k_new / v_new must be contiguous 16-bit {shape}")
         self._captured(db)
+        self._held(db, stream)
         rows = (k_new.data_ptr(), v_new.data_ptr(), db.slot_mapping.data_ptr(), db.n_tokens, self.num_blocks,
                 self.hkv, self.d)
         if self.kv_format == "mx4":
@@ -543,6 +546,7 @@ class PrefillEngine:
             if self._bad(a, (t, c, self.d)):
                 raise ValueError("q / k_new / v_new must be contiguous 16-bit [n_tokens, heads, D]")
         y = self._rope_table(db, stream)
+        self._held(db, stream)
         self._call("arckv_qkv_rope", stream, x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
                    db.cu_q.data_ptr(), self._position_lens(db), db.plan.n_reqs, float(rope_theta), y.data_ptr(), y.numel(),
                    q.data_ptr(), k_new.data_ptr(), v_new.data_ptr())
@@ -559,6 +563,7 @@ class PrefillEngine:
         if self._bad(q, (t, self.hq, self.d)):
             raise ValueError("q must be contiguous 16-bit [n_tokens, heads, D]")
         y = self._rope_table(db, stream)
+        self._held(db, stream)
         self._call("arckv_qkv_rope_to_pool", stream, x.data_ptr(), w_qkv.data_ptr(), t, h, self.hq, self.hkv, self.d,
                    db.cu_q.data_ptr(), self._position_lens(db), db.plan.n_reqs, float(rope_theta), y.data_ptr(), y.numel(),
                    q.data_ptr(), self.k_pool.data_ptr(), self.v_pool.data_ptr(), self.num_blocks, db.slot_mapping.data_ptr())
@@ -614,6 +619,7 @@ class PrefillEngine:
         n = db.plan.n_reqs
         self._check_weights(n, weights)
         self._captured(db)
+        self._held(db, stream)
         mx4 = self.kv_format == "mx4"
         self._call("arckv_attention_weights", stream, (self.kv_pool if mx4 else self.k_pool).data_ptr(),
                    _lib.LAYOUT_MX4 if mx4 else _lib.LAYOUT_V1, q.data_ptr(), lse.data_ptr(), db.block_tables.data_ptr(),
