@@ -83,7 +83,8 @@ extern "C" {
 /* Device checks (a debug build: paper_2606_21238_amd.build with checked=True writes
  * lib/libarckv_checked.so, its kernels compiled with ARCKV_DEVICE_CHECKS).  Where a kernel
  * clamps or skips an out-of-range index it also records the kind, per device:
- *   ARCKV_CHECK_SLOT   a KV scatter slot outside [0, 16 num_blocks) (the token is skipped);
+ *   ARCKV_CHECK_SLOT   a KV scatter slot outside [0, 16 num_blocks) (the token is skipped), but for
+ *                      -1, which names no slot (a row behind a step's tokens);
  *   ARCKV_CHECK_BLOCK  an attention block-table entry outside [0, num_blocks) among the blocks
  *                      of a request (block 0 is read in its place);
  *   ARCKV_CHECK_WORK   an attention or combine work item naming no request, KV head or

@@ -30,7 +30,7 @@ __global__ __launch_bounds__(kMx4Threads) void kv_scatter_mx4_kernel(
   const int c = threadIdx.x % CH;
   const bool there = t < n_tokens;
   const int32_t s = there ? slots[t] : -1;
-  ARCKV_CHECK_LANE(there && !(s >= 0 && s < n_slots), ARCKV_CHECK_SLOT);
+  ARCKV_CHECK_LANE(s != -1 && !(s >= 0 && s < n_slots), ARCKV_CHECK_SLOT);        // -1 names no slot
   uint32_t k[4] = {}, v[4] = {};
   if (there) {
     const int64_t src = (t * hkv + h) * D + c * 8;
@@ -89,7 +89,7 @@ __global__ __launch_bounds__(kMx4Threads) void kv_scatter_mx4_runs_kernel(
     const int64_t t = t0 + tid;
     const int32_t s = t < n_tokens ? slots[t] : -1;
     const bool ok = s >= 0 && s < n_slots;
-    ARCKV_CHECK_LANE(t < n_tokens && !ok, ARCKV_CHECK_SLOT);
+    ARCKV_CHECK_LANE(s != -1 && !ok, ARCKV_CHECK_SLOT);
     sslot[tid] = ok ? s : -1;
   }
   __syncthreads();

@@ -15,7 +15,8 @@
 // the two runs of one block and then on consecutive dimensions, so that a wave's stores fill
 // whole lines.  Every other token is written the coalesced 2-byte way: lane = token, 64
 // consecutive tokens of one dimension per store instruction.  Bytes are copied, never converted:
-// the result is bit-exact.  Slots outside the pool are skipped.
+// the result is bit-exact.  Slots outside the pool are skipped (-1 names none: a row behind a
+// step's tokens).
 //
 // What bounds it is memory, and the chain slots -> barrier -> load -> store: the rows do not depend
 // on the slots, so a thread asks for all of its chunks first.  Whole rows are read once and
@@ -88,7 +89,7 @@ __global__ __launch_bounds__(kThreads) void kv_scatter_kernel(
   if (tid < kTok) {
     const int64_t t = t0 + tid;
     const int32_t s = t < n_tokens ? slots[t] : -1;
-    ARCKV_CHECK_LANE(t < n_tokens && !(s >= 0 && s < n_slots), ARCKV_CHECK_SLOT);
+    ARCKV_CHECK_LANE(s != -1 && !(s >= 0 && s < n_slots), ARCKV_CHECK_SLOT);      // -1 names no slot
     sslot[tid] = (s >= 0 && s < n_slots) ? s : -1;
   }
   __syncthreads();
