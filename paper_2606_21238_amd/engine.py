@@ -247,8 +247,10 @@ class PrefillEngine:
         """Running requests for steps that need nothing from the host: request r holds held[r] tokens in the blocks
         tables[r] (host integers [n_reqs, stride]; entries behind them are room for advance()).  Consecutive requests form
         groups of group_sizes[g] requests (of all of them, or () for none) whose first prefix_lens[g] tokens are in the same blocks.
-        max_tokens: the most new tokens of a step, max_new: of a request in it (a step that passes that is right, but
-        slower).  free_blocks: private blocks for the tokens to come, the last one is taken first.  true_lens: of cut sessions,
+        max_tokens: the most new tokens of a step, max_new: of a request in it (None: of max_tokens dealt out evenly, one for a batch
+        of decodes; a step that passes it is right, but slower).  It chooses the kernels, and the memory: partial results of
+        16, 128 or 256 columns for every request and KV head, so 1000 requests with tables of 8192 tokens, 32 / 8 heads of 128 and
+        max_tokens 1000 take 123 MiB with max_new 1 and 1120 with 1000.  free_blocks: private blocks for the tokens to come, the last one is taken first.  true_lens: of cut sessions,
         as for resume(): project() counts positions by them.
         The blocks stay the caller's, who keeps them from other requests as long as the steps run (blocks of the block cache: by
         not releasing their batch); a request's last block, if it is not full, is written and must be its own."""
@@ -292,7 +294,7 @@ class PrefillEngine:
                 raise ValueError(f"group {g} cannot share {p} tokens: one of its requests holds fewer")
             if (tables[rows, :-(-int(p) // 16)] != tables[start[g], :-(-int(p) // 16)]).any():
                 raise ValueError(f"the requests of group {g} hold their first {p} tokens in different blocks")
-        max_new = max_tokens if max_new is None else min(max_new, max_tokens)
+        max_new = -(-max_tokens // max(n, 1)) if max_new is None else min(max_new, max_tokens)
         bounds = SharedBounds(n, len(sizes), max_tokens, min(max_tokens, int(sizes.max(initial=0)) * max_new), max_new, stride,
                               self.hq, self.hkv, self.d, self.num_cus)
         ints, ws_bytes = shared_prefix_sizes(bounds)
