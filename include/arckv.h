@@ -614,7 +614,8 @@ int32_t arckv_kv_compact_mx4(void* kv_pool, const int32_t* block_tables, int32_t
  * A row with a NaN or an infinity gives what these formulas give (its scale may be NaN, its codes 0x7F).
  * x: device bf16, rows x_stride elements apart (x_stride >= hidden).  residual and residual_out: device bf16
  * [n_tokens][hidden], both or neither; weight: device bf16 [hidden].  residual_out may be residual or (x_stride =
- * hidden) x, a bf16 out may be any of them that residual_out is not; no other overlap.  Rows may start at
+ * hidden) x, a bf16 out may be residual or (x_stride = hidden) x, but not residual_out; no other overlap (EINVAL where these
+ * begin at one address).  Rows may start at
  * any bf16 address and hidden may be odd (hidden a multiple of 8 and 16-byte aligned rows run faster); scales 4-byte
  * aligned.  hidden at most 32768 (EUNSUPPORTED), n_tokens at most 2^31 - 1; n_tokens = 0 is a no-op.  h^2 is summed
  * in fp32, of a row whose squares fp32 does not hold times a power of two. */

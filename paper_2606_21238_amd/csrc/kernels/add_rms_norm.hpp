@@ -255,6 +255,11 @@ extern "C" int32_t arckv_add_rms_norm(const void* x, int64_t x_stride, const voi
   const bool e4m3 = out_format == ARCKV_OUT_E4M3;
   if (x == nullptr || weight == nullptr || out == nullptr || (e4m3 && scales == nullptr))
     return arckv::fail(ARCKV_EINVAL, "add_rms_norm: NULL pointer");
+  // outputs in the place of an input: only where a work-group writes what it alone has read, and not two in one place
+  const bool apart = x_stride != hidden && n_tokens > 1;
+  if (out == residual_out || (apart && (out == x || (residual_out != nullptr && residual_out == x))) ||
+      (e4m3 && (out == x || out == residual)))
+    return arckv::fail(ARCKV_EINVAL, "add_rms_norm: out, residual_out and the inputs overlap");
   uintptr_t all = reinterpret_cast<uintptr_t>(scales);
   if (all % 4 != 0) return arckv::fail(ARCKV_EINVAL, "add_rms_norm: scales must be 4-byte aligned");
   all = 0;
