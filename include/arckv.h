@@ -678,7 +678,7 @@ int32_t arckv_shared_prefix_plan(const int32_t* group_start, const int32_t* pref
 /* The attention.  Pools (layout V1), q, out, tables, head counts, scale and what out-of-range table entries do as for
  * arckv_prefill_attention; lse (may be NULL) as for arckv_prefill_attention_lse.  Rows of q and out: max_q, of which
  * those behind cu_q[n_reqs] are neither read nor written.  Rows of a request of length 0 (places of a batch of fixed size
- * that nobody has) see no key: out 0, lse -infinity.  workspace: device, 16-byte aligned, ws_bytes as
+ * that nobody has) see no key: out 0, lse -infinity (a group that they are in shares nothing).  workspace: device, 16-byte aligned, ws_bytes as
  * arckv_shared_prefix_sizes says (ENOSPC); calls that overlap in time must not share it.  num_blocks in [1, 2^27]. */
 int32_t arckv_shared_prefix_attention(const void* k_pool, const void* v_pool, const void* q, void* out,
                                       float* lse, const int32_t* block_tables, int32_t bt_stride,

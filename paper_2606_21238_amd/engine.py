@@ -55,8 +55,8 @@ class StepPlan:
 class StepBatch(DeviceBatch):
     """Running requests whose lengths, tables and maps live on the device (PrefillEngine.step_batch).  n_tokens is the
     most tokens of a step; rows behind cu_q[-1] belong to no request: their slots are -1.  seq_lens (the tokens
-    held), block_tables, free_blocks, free_count and what else is here may be changed between steps by the caller, in the order of
-    the engine's calls.  Calls for one StepBatch must not overlap in time."""
+    held), block_tables, free_blocks, free_count and what else is here may be changed in place between steps by the caller, in the
+    order of the engine's calls (a member of a group keeps naming the group's blocks for what it shares, or has no rows).  Calls for one StepBatch must not overlap in time."""
     bounds: SharedBounds = None
     group_start: object = None
     prefix_lens: object = None
@@ -252,8 +252,11 @@ class PrefillEngine:
         16, 128 or 256 columns for every request and KV head, so 1000 requests with tables of 8192 tokens, 32 / 8 heads of 128 and
         max_tokens 1000 take 123 MiB with max_new 1 and 1120 with 1000.  free_blocks: private blocks for the tokens to come, the last one is taken first.  true_lens: of cut sessions,
         as for resume(): project() counts positions by them.
-        The blocks stay the caller's, who keeps them from other requests as long as the steps run (blocks of the block cache: by
-        not releasing their batch); a request's last block, if it is not full, is written and must be its own."""
+        The blocks stay the caller's, who keeps them from other requests as long as the steps run; a request's last block, if it is
+        not full, is written and must be its own.  Blocks of the block cache are kept by not releasing their batch, and meanwhile the cache
+        plans no other (prepare() raises ESTATE; after release() it may give the blocks away).  Where requests are admitted while steps run,
+        the shared prefix lies in private blocks: evict() of a batch that holds it, with keep = its length, moves all of it there, and
+        requests behind it come in by resume()."""
         import torch
         if self.kv_format != "bf16":
             raise ValueError("step_batch works on bf16 pools")
