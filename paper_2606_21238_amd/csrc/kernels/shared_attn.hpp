@@ -353,7 +353,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
     const int L = max(seq_lens[r], 0), q0 = row(r), S = max(row(r + 1) - q0, 0);
     if (g >= 0 && S > 0) {
       atomicMin(&groups[g].keys1, max(L - S, 0));
-      atomicMin(&groups[g].group, r);
+      if (q0 == row(start(g))) groups[g].group = r;    // the first of its group that has rows
       atomicAdd(&groups[g].whole, static_cast<int>((static_cast<int64_t>(S) * G + z.tile_o - 1) / z.tile_o));
     }
     Part p = {};
@@ -367,11 +367,9 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(
   for (int g = tid; g < n_groups; g += kPlanThreads) {
     int shared = __hip_atomic_load(&groups[g].keys1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) / kBK * kBK;
     const int apart = __hip_atomic_load(&groups[g].whole, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    const int first = __hip_atomic_load(&groups[g].group, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     Part& p = groups[g];
     // The shared keys are read through this request's table: one without rows may have ended, and its table name other blocks
-    p.group = first;
-    if (first >= n_reqs) shared = 0;
+    if (p.group >= n_reqs) shared = 0;
     const int together = static_cast<int>((static_cast<int64_t>(p.rows) * G + z.tile_p - 1) / z.tile_p);
     // Requests that fill their own wide tiles read their keys once for 256 columns anyhow: sharing that saves no more than
     // an eighth of the tiles is not worth a second item and the join (2 x 1024 rows on 16384: 978 us shared)

@@ -56,7 +56,8 @@ class StepBatch(DeviceBatch):
     """Running requests whose lengths, tables and maps live on the device (PrefillEngine.step_batch).  n_tokens is the
     most tokens of a step; rows behind cu_q[-1] belong to no request: their slots are -1.  seq_lens (the tokens
     held), block_tables, free_blocks, free_count and what else is here may be changed in place between steps by the caller, in the
-    order of the engine's calls (a member of a group keeps naming the group's blocks for what it shares, or has no rows).  Calls for one StepBatch must not overlap in time."""
+    order of the engine's calls (a member of a group keeps naming the group's blocks for what it shares, or has no rows).
+    Calls for one StepBatch must not overlap in time."""
     bounds: SharedBounds = None
     group_start: object = None
     prefix_lens: object = None
