@@ -5,8 +5,8 @@
 //   out = bf16(y), or scale = max|y| / 448 for every row and out = e4m3(y / scale)
 //
 // One work-group has a row and holds it in registers as h, so each value is read once; what bounds it is
-// the bytes of x, residual, residual_out and out: 25600 x 5120 in bf16 (1.05 GB) 180 us, 5.8 TB/s, 16384 x 4096 to 8 bits (0.47
-// GB) 82 us, 5.7 TB/s, above a copy's 4.7 since more is read than written; 64 x 4096 3.0 us, a launch and two round trips (2.9
+// the bytes of x, residual, residual_out and out: 25600 x 5120 in bf16 (1.05 GB) 178 us, 5.9 TB/s, 16384 x 4096 to 8 bits (0.47
+// GB) 82 us, 5.8 TB/s, above a copy's 4.7 since more is read than written; 64 x 4096 3.0 us, a launch and two round trips (2.9
 // inside a graph).  A row's squares are added in fp32: up to 40 in a thread, then by a tree of lanes and waves, always in the
 // same order; where the sum leaves [2^-80, 2^100] (squares below or above fp32's numbers may be among them), once more of
 // the row times a power of two, which rounds nothing.

@@ -8,7 +8,7 @@
 //
 //  * shared_plan_kernel (once a step; the layers share its plan): how many keys the groups share in truth (all
 //    their rows must see them; whole tiles of 64), the cuts, and the work items, from lengths on the device.  One work-group,
-//    a chain of scans and searches: 20 us for 64 requests, 66 for 1000; none for short batches.
+//    a chain of scans and searches: 20 us for 64 requests, 69 for 1000; none for short batches.
 //  * the shared keys: the attention kernels above, given a group as a request whose rows are those of
 //    all its requests and whose length is P + rows, so that every row sees all keys below P.  8192 tokens of 8 heads of 128
 //    for 92 columns (34 MB, narrow tiles) 16 us, of which the stream is 6; 32768 tokens for 184 columns (134 MB, wide tiles) 40
