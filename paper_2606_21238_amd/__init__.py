@@ -732,7 +732,8 @@ def _launch(name: str, index: int, stream, *args):
 
 def add_rms_norm(x, weight, out, eps: float, residual=None, residual_out=None, scales=None, stream=None):
     """out <- h / sqrt(mean(h^2) + eps) * weight, h = x + residual, which goes to residual_out as bf16 (None:
-    into residual itself, which out then is not).  x bf16 [n, hidden] (rows may lie further apart), weight bf16 [hidden], residual bf16 [n, hidden].
+    into residual itself, which out then is not).  x bf16 [n, hidden] (rows may lie further apart), weight bf16 [hidden],
+    residual bf16 [n, hidden].
     out: bf16 [n, hidden]; with scales (fp32 [n]) 8-bit codes (torch.float8_e4m3fn or uint8 [n, hidden]) that
     stand for code * scale."""
     shape, kinds = x.shape, _kinds()

@@ -9,7 +9,7 @@
 // GB) 82 us, 5.8 TB/s, above a copy's 4.7 since more is read than written; 64 x 4096 3.0 us, a launch and two round trips (2.9
 // inside a graph).  A row's squares are added in fp32: up to 40 in a thread, then by a tree of lanes and waves, always in the
 // same order; where the sum leaves [2^-80, 2^100] (squares below or above fp32's numbers may be among them), once more of
-// the row times a power of two, which rounds nothing.
+// the row times a power of two, which rounds nothing that counts in it.
 #pragma once
 
 namespace {

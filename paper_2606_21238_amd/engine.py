@@ -251,8 +251,8 @@ class PrefillEngine:
         max_tokens: the most new tokens of a step, max_new: of a request in it (None: of max_tokens dealt out evenly, one for a batch
         of decodes; a step that passes it is right, but slower).  It chooses the kernels, and the memory: partial results of
         16, 128 or 256 columns for every request and KV head, so 1000 requests with tables of 8192 tokens, 32 / 8 heads of 128 and
-        max_tokens 1000 take 123 MiB with max_new 1 and 1120 with 1000.  free_blocks: private blocks for the tokens to come, the last one is taken first.  true_lens: of cut sessions,
-        as for resume(): project() counts positions by them.
+        max_tokens 1000 take 123 MiB with max_new 1 and 1120 with 1000.  free_blocks: private blocks for the tokens to come, the
+        last one is taken first.  true_lens: of cut sessions, as for resume(): project() counts positions by them.
         The blocks stay the caller's, who keeps them from other requests as long as the steps run; a request's last block, if it is
         not full, is written and must be its own.  Blocks of the block cache are kept by not releasing their batch, and meanwhile the cache
         plans no other (prepare() raises ESTATE; after release() it may give the blocks away).  Where requests are admitted while steps run,
